@@ -41,7 +41,7 @@ typedef enum {
     NNC_ERR_WORKSPACE = -2,     /* workspace smaller than nnc_workspace_bytes(), or misaligned */
     NNC_ERR_CAPACITY = -3,      /* cache length + new tokens > max_seq, batch > max_batch, tokens > max_tokens */
     NNC_ERR_CUDA = -4,          /* a CUDA runtime / driver call failed; see nnc_last_error */
-    NNC_ERR_DEVICE_STATUS = -5  /* a kernel reported a bounded wait that ran out */
+    NNC_ERR_DEVICE_STATUS = -5  /* a kernel reported a bounded wait that ran out, or a cache address out of range */
 } nnc_status;
 
 typedef struct nnc_model nnc_model; /* opaque; host struct owned by the library */
@@ -220,8 +220,10 @@ int nnc_op_gemm_swiglu_f16(const void *X, const void *W, void *Y, int32_t T, int
  * scratch_word: DEVICE uint32 used during the call. */
 int nnc_op_to_f16_scaled(const void *src, void *dst, size_t n, float *scales, uint32_t *scratch_word, void *cuda_stream);
 
-/* Status word of the nnc_op_* tensor-core kernels (0 = no bounded wait ran out); synchronises the device and
- * clears the word.  status_out is a HOST pointer. */
+/* Status word of the nnc_op_* kernels (0 = no tensor-core kernel's bounded wait ran out and no paged-cache kernel met
+ * an address out of range: NNC_STATUS_PAGED_ADDRESS); synchronises the device and clears the word.  status_out is a
+ * HOST pointer. */
+#define NNC_STATUS_PAGED_ADDRESS 0x100
 int nnc_op_status(int32_t *status_out);
 
 /* y[n_out] = W[n_out][n_in] x (batch-1 streaming GEMV, fp32 accumulate).  x fp32 [n_in]; y fp32.
@@ -287,6 +289,101 @@ int nnc_op_attn_prefill_f16(const float *qkv, const void *k16, const void *v16, 
 int nnc_op_attn_decode_static(const float *q, const void *kcache, const void *vcache, float *out, int32_t batch,
                               int32_t n_q_heads, int32_t n_kv_heads, int32_t max_seq, int32_t n_ctx,
                               void *cuda_stream);
+
+/* ---- rotary positions and the paged key-value cache ------------------------------------------------------
+ * Single operations for serving sequences of different lengths: rotate queries and keys (nnc_op_rope), append rows to a
+ * cache whose memory is handed out in pages (nnc_op_kv_write_paged), attend from one new token per sequence
+ * (nnc_op_attn_decode_paged), read rows back (nnc_op_kv_read_paged).  Positions, sequences, page tables and lengths
+ * are DEVICE arrays that a kernel reads when it runs, so a captured graph follows them from replay to replay.  Like
+ * the other operations, each launches on `cuda_stream` of the current device, allocates nothing and writes only the
+ * rows it names. */
+
+typedef enum { NNC_F32 = 0, NNC_BF16 = 1, NNC_F16 = 2, NNC_E4M3 = 3 } nnc_type;
+
+/* Angles per position of the rotary pairs: freq[i] (HOST, rotary_dim / 2 doubles) = radians by which pair i turns per
+ * position, theta^(-2i / rotary_dim), stretched for contexts longer than the one a model was made for:
+ *   NNC_ROPE_PLAIN      unchanged
+ *   NNC_ROPE_LINEAR     all divided by `factor`
+ *   NNC_ROPE_BASE       theta grown to theta * factor^(rotary_dim / (rotary_dim - 2)): the slowest pair is divided by `factor`
+ *   NNC_ROPE_RAMP_TURNS pairs that make at least `fast` turns over `original` positions stay, pairs that make at most
+ *                       `slow` are divided by `factor`, between them f * (g + (1 - g) / factor) with g linear in the turns
+ *   NNC_ROPE_RAMP_INDEX the same with g linear in the pair's index, between floor(index that makes `fast` turns) and
+ *                       ceil(index that makes `slow`), both kept inside [0, rotary_dim - 1]; the upper one is moved 0.001 up
+ *                       where they coincide
+ * amplitude (HOST, may be NULL): what queries and keys are multiplied by, 0.1 ln(factor) + 1 for the ramp by index (1 for
+ * factor <= 1), 1 for the others.  Pure host arithmetic.  rotary_dim even and positive (BASE: at least 4), theta > 0, factor >= 1,
+ * original > 0 and 0 < slow < fast where they are used; NNC_ERR_INVALID_ARG otherwise. */
+enum { NNC_ROPE_PLAIN = 0, NNC_ROPE_LINEAR = 1, NNC_ROPE_BASE = 2, NNC_ROPE_RAMP_TURNS = 3, NNC_ROPE_RAMP_INDEX = 4 };
+int nnc_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original, double slow,
+                         double fast, double *freq, float *amplitude);
+
+/* y = the rotation of x by its positions: x, y of `type` (NNC_F32, NNC_BF16 or NNC_F16), element (t, h, i) of token t and head h
+ * at t * row_stride + h * head_stride + i (strides in elements, may be 0 or negative for x).  positions: int32 [n_tokens], any value.  freq: DEVICE
+ * double [rotary_dim / 2].  The first rotary_dim elements of each head turn (rotary_dim even, 2 <= rotary_dim <=
+ * head_dim <= 1024), in pairs (i, i + rotary_dim / 2), or (2i, 2i + 1) with interleaved != 0; the others are copied.
+ *   y_a = amplitude * (x_a cos - x_b sin),  y_b = amplitude * (x_b cos + x_a sin),  angle = position * freq[i]
+ * inverse != 0 turns the other way: given the gradient with respect to y it is the gradient with respect to x.  The
+ * angle is reduced in 64 bits, the arithmetic is fp32, one rounding to `type` at the end.  y may be x itself (with the
+ * same strides); other overlaps of x and y, and rows of y that overlap each other, are not allowed.  n_tokens or n_heads of 0 is a call that
+ * does nothing. */
+int nnc_op_rope(const void *x, void *y, int32_t type, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                int64_t x_row_stride, int64_t x_head_stride, int64_t y_row_stride, int64_t y_head_stride,
+                const int32_t *positions, const double *freq, int32_t rotary_dim, int32_t interleaved, int32_t inverse,
+                float amplitude, void *cuda_stream);
+
+/* A paged cache (HOST struct, DEVICE pointers; the caller owns all memory and hands out the pages).  Position n of
+ * sequence s lies in slot n % page_size of page page_table[s * pages_per_seq + n / page_size].
+ *   k, v             [n_pages][n_kv_heads][page_size][head_dim] of `type` (NNC_BF16, NNC_F16 or NNC_E4M3), 16-byte aligned
+ *   k_scale, v_scale NNC_E4M3 only: one byte a row, [n_pages][n_kv_heads][page_size], 16-byte aligned: the row's values
+ *                    are code * 2^(byte - 127).  NULL otherwise
+ *   page_table       int32 [n_seqs][pages_per_seq]; entries that no call reaches may hold anything.  Sequences may share pages
+ *                    (a common prefix) that no call writes
+ *   page_size 16, 32, 64, 128 or 256; head_dim 64 or 128.
+ * An address that a call reaches and that lies outside (a sequence >= n_seqs, a position >= pages_per_seq * page_size, a
+ * page outside [0, n_pages)) is neither read nor written; the call goes on without it and sets NNC_STATUS_PAGED_ADDRESS in
+ * nnc_op_status's word. */
+typedef struct {
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+    const int32_t *page_table;
+    int32_t type, n_pages, page_size, n_kv_heads, head_dim, n_seqs, pages_per_seq;
+} nnc_paged_kv;
+
+/* Writes the key and value rows of n_tokens tokens: token t goes to position pos[t] of sequence seq[t] (int32 [n_tokens];
+ * seq NULL: sequence t, and n_tokens <= n_seqs).  Tokens whose seq or pos is negative are padding and are left out.  No two tokens of
+ * a call may name the same slot.  Element (t, h, i) of k and v, of `type` (NNC_F32, NNC_BF16, NNC_F16), lies at t * row_stride +
+ * h * head_stride + i.  16-bit caches hold the value rounded to nearest even (a row of the cache's own type is copied); an E4M3
+ * row holds codes for the scale 2^e, e the smallest integer with max|x| <= 448 * 2^e over the row's finite values, kept
+ * inside [-60, 60] (0 for a row without any but zeros), rounded to nearest even, saturating (infinities too); NaN stays NaN.  Pointers and
+ * strides of k and v are multiples of 16 bytes. */
+int nnc_op_kv_write_paged(const nnc_paged_kv *cache, const void *k, const void *v, int32_t type, int32_t n_tokens,
+                          int64_t row_stride, int64_t head_stride, const int32_t *pos, const int32_t *seq, void *cuda_stream);
+
+/* Reads rows back, addressed the same way: the values of position pos[t] of sequence seq[t] to k and v, rounded to `type`
+ * (exact for NNC_F32, and for a scaled code in NNC_BF16).  Rows of padding tokens and of addresses out of range are left as
+ * they are.  The same position may be read by several tokens. */
+int nnc_op_kv_read_paged(const nnc_paged_kv *cache, void *k, void *v, int32_t type, int32_t n_tokens, int64_t row_stride,
+                         int64_t head_stride, const int32_t *pos, const int32_t *seq, void *cuda_stream);
+
+/* Attention of one new token per sequence over the paged cache, which already holds that token's own row.
+ *   q, out  of `type` (NNC_F32, or the cache's own 16-bit type; NNC_F32, NNC_BF16 or NNC_F16 for an E4M3 cache): row b (of
+ *           sequence b, batch <= n_seqs) holds n_q_heads heads of head_dim at b * q_stride / b * out_stride elements.  Query head i
+ *           uses KV head i / (n_q_heads / n_kv_heads); any whole ratio
+ *   lens    int32 [batch]: sequence b attends to positions max(0, lens[b] - window) .. lens[b] - 1 (window 0: from 0).  Rows of
+ *           the cache outside that range are never read into the result (they may hold anything)
+ *   scale   multiplies q.k before the softmax
+ *   lse     fp32 [batch][n_q_heads] or NULL: log(sum exp) of the scaled scores, natural logarithm
+ * A sequence with nothing to attend to (lens <= 0) gets a row of zeros and lse = -infinity.  A length beyond the table's
+ * reach counts as the longest the table holds, and a page out of range as absent; both set the status word.
+ * scratch: DEVICE, 256-byte aligned, NNC_ATTN_PAGED_SCRATCH_BYTES; its first NNC_ATTN_PAGED_TICKET_BYTES must be zero before
+ * the first call and are left zero by every call.  Calls that share a scratch must not overlap on the device (captured
+ * graphs included).  Results do not depend on scheduling: partial results are joined in a fixed order.  q, out and
+ * their strides are multiples of 16 bytes. */
+#define NNC_ATTN_PAGED_SCRATCH_BYTES (16u << 20)
+#define NNC_ATTN_PAGED_TICKET_BYTES 4096
+int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, void *out, float *lse, int32_t type,
+                             int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
+                             void *scratch, size_t scratch_bytes, void *cuda_stream);
 
 #ifdef __cplusplus
 }

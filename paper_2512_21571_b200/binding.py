@@ -40,6 +40,11 @@ class nnc_weights(C.Structure):
                 ("layers", C.POINTER(nnc_layer_weights))]
 
 
+class nnc_paged_kv(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "page_table")] + \
+               [(n, C.c_int32) for n in ("type", "n_pages", "page_size", "n_kv_heads", "head_dim", "n_seqs", "pages_per_seq")]
+
+
 EXPORTS = {
     "nnc_workspace_bytes": (C.c_size_t, [C.POINTER(nnc_config)]),
     "nnc_model_create": (C.c_int, [C.POINTER(nnc_config), C.POINTER(nnc_weights), C.c_void_p, C.c_size_t, C.c_void_p,
@@ -88,6 +93,18 @@ EXPORTS = {
                                           C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
     "nnc_op_attn_decode_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                             C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
+    "nnc_rope_frequencies": (C.c_int, [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                       C.c_void_p, C.POINTER(C.c_float)]),
+    "nnc_op_rope": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+                              C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_float,
+                              C.c_void_p]),
+    "nnc_op_kv_write_paged": (C.c_int, [C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int64,
+                                        C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "nnc_op_kv_read_paged": (C.c_int, [C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int64,
+                                       C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "nnc_op_attn_decode_paged": (C.c_int, [C.c_void_p, C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                           C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_float, C.c_int32, C.c_void_p,
+                                           C.c_size_t, C.c_void_p]),
 }
 for _name, (_res, _args) in EXPORTS.items():
     _fn = getattr(lib, _name)
@@ -402,3 +419,187 @@ def op_attn_prefill_f16(qkv: torch.Tensor, k16: torch.Tensor, v16: torch.Tensor,
     _ok(lib.nnc_op_attn_prefill_f16(_dev(qkv, torch.float32), _dev(k16, torch.float16), _dev(v16, torch.float16), out.data_ptr(),
                                     batch, T, n_q_heads, nkv, max_seq, n_past, _stream_ptr()), "nnc_op_attn_prefill_f16")
     return out
+
+
+# ---- rotary positions and the paged key-value cache --------------------------------------------------------------
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp_turns": 3, "ramp_index": 4}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
+ATTN_PAGED_SCRATCH_BYTES = 16 << 20
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _same_device(device: torch.device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device} in one call")
+
+
+def _launch(fn, what: str, device: torch.device, *args):
+    """The C call on the tensors' own device and that device's current stream, whichever device is current."""
+    if device.index == torch._C._cuda_getDevice():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if rc:
+        raise NncError(rc, what)
+
+
+def _disjoint(t: torch.Tensor) -> bool:
+    """No two elements of t share memory (as far as sorted strides show it)."""
+    span = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
+        if stride < span:
+            return False
+        span += stride * (n - 1)
+    return True
+
+
+def _rows(t: torch.Tensor, what: str):
+    _need(t.is_cuda and t.dim() == 3 and t.stride(2) == 1, f"{what}: a CUDA tensor [tokens][heads][head_dim] with contiguous heads")
+
+
+def _index(t: torch.Tensor, n: int, what: str) -> int:
+    _need(t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), f"{what}: {n} contiguous int32 numbers")
+    return t.data_ptr()
+
+
+def rope_frequencies(rotary_dim: int, theta: float = 1e6, scaling: str = "plain", factor: float = 1.0, original: float = 0.0,
+                     slow: float = 1.0, fast: float = 32.0, device="cuda"):
+    """nnc_rope_frequencies: (float64 [rotary_dim / 2] on `device`, amplitude)."""
+    _need(scaling in ROPE_SCALINGS, f"scaling: one of {', '.join(ROPE_SCALINGS)}")
+    freq = torch.empty(max(0, rotary_dim) // 2, dtype=torch.float64)
+    amplitude = C.c_float(1.0)
+    _ok(lib.nnc_rope_frequencies(rotary_dim, theta, ROPE_SCALINGS[scaling], factor, original, slow, fast, freq.data_ptr(),
+                                 C.byref(amplitude)), "nnc_rope_frequencies")
+    return freq.to(device), amplitude.value
+
+
+def op_rope(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0,
+            inverse: bool = False, out: Optional[torch.Tensor] = None):
+    """nnc_op_rope: x [tokens][heads][head_dim] (any strides between rows and heads) turned by int32 `positions`; the first
+    2 * len(freq) elements of each head turn.  out: None, x itself, or a tensor of x's shape and type that x does not overlap."""
+    _rows(x, "x")
+    _need(x.dtype in _TYPES and x.dtype is not torch.float8_e4m3fn, "x: float32, bfloat16 or float16")
+    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: contiguous float64 numbers")
+    tokens, heads, d = x.shape
+    if out is None:
+        out = torch.empty((tokens, heads, d), dtype=x.dtype, device=x.device)
+    else:
+        _rows(out, "out")
+        _need(out.shape == x.shape and out.dtype == x.dtype and _disjoint(out), "out: x's shape and type, no rows that overlap")
+    _same_device(x.device, positions, freq, out)
+    xs, ys = x.stride(), out.stride()
+    _launch(lib.nnc_op_rope, "nnc_op_rope", x.device, x.data_ptr(), out.data_ptr(), _TYPES[x.dtype], tokens, heads, d, xs[0], xs[1],
+            ys[0], ys[1], _index(positions, tokens, "positions"), freq.data_ptr(), 2 * freq.shape[0], interleaved, inverse,
+            amplitude)
+    return out
+
+
+class PagedKV:
+    """nnc_paged_kv: a cache's pools and page table, described once and passed to the calls below.
+
+    k, v [n_pages][n_kv_heads][page_size][head_dim], bfloat16, float16 or float8_e4m3fn (then with uint8 scales
+    [n_pages][n_kv_heads][page_size]: code * 2^(byte - 127)); page_table int32 [n_seqs][pages_per_seq].  The tensors' contents
+    may change between calls; the tensors themselves stay."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        _need(k.is_cuda and k.dim() == 4 and k.dtype in (torch.bfloat16, torch.float16, torch.float8_e4m3fn) and k.is_contiguous(),
+              "k: a contiguous CUDA tensor [n_pages][n_kv_heads][page_size][head_dim] of bfloat16, float16 or float8_e4m3fn")
+        _need(v.shape == k.shape and v.dtype is k.dtype and v.is_contiguous(), "v: k's shape and type, contiguous")
+        _need(page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(), "page_table: contiguous int32 [n_seqs][pages_per_seq]")
+        codes = k.dtype is torch.float8_e4m3fn
+        for s in (k_scale, v_scale):
+            _need((s is not None) == codes, "k_scale and v_scale belong to float8_e4m3fn caches, and to no other")
+            _need(s is None or (s.dtype is torch.uint8 and s.shape == k.shape[:3] and s.is_contiguous()), "scales: contiguous uint8 [n_pages][n_kv_heads][page_size]")
+        _same_device(k.device, v, page_table, k_scale, v_scale)
+        self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
+        self.device, self.dtype = k.device, k.dtype
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.n_seqs, self.pages_per_seq = page_table.shape
+        self.c = nnc_paged_kv(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if codes else None, v_scale.data_ptr() if codes else None,
+                              page_table.data_ptr(), _TYPES[k.dtype], self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
+                              self.n_seqs, self.pages_per_seq)
+        self.ref = C.byref(self.c)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_seqs: int, pages_per_seq: int,
+              device="cuda"):
+        """Pools of zeros and a page table of -1."""
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        pools = [torch.zeros(shape, dtype=torch.uint8 if dtype is torch.float8_e4m3fn else dtype, device=device).view(dtype) for _ in range(2)]
+        scales = [torch.full(shape[:3], 127, dtype=torch.uint8, device=device) if dtype is torch.float8_e4m3fn else None for _ in range(2)]
+        return cls(*pools, torch.full((n_seqs, pages_per_seq), -1, dtype=torch.int32, device=device), *scales)
+
+
+def op_kv_write_paged(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, seq: Optional[torch.Tensor] = None):
+    """nnc_op_kv_write_paged: rows k, v [tokens][n_kv_heads][head_dim] to positions `pos` of sequences `seq` (None: token t is
+    sequence t's).  k and v have the same strides (slices of one fused projection do)."""
+    _rows(k, "k")
+    _rows(v, "v")
+    _need(k.dtype is v.dtype and k.dtype in _TYPES and k.dtype is not torch.float8_e4m3fn, "k, v: float32, bfloat16 or float16")
+    ks = k.stride()
+    tokens = k.shape[0]
+    _need(v.shape == k.shape and v.stride() == ks and k.shape[1] == cache.n_kv_heads and k.shape[2] == cache.head_dim,
+          "k, v: [tokens][n_kv_heads][head_dim] of the cache, with the same strides")
+    _same_device(cache.device, k, v, pos, seq)
+    _launch(lib.nnc_op_kv_write_paged, "nnc_op_kv_write_paged", cache.device, cache.ref, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], tokens,
+            ks[0], ks[1], _index(pos, tokens, "pos"), _index(seq, tokens, "seq") if seq is not None else None)
+
+
+def op_kv_read_paged(cache: PagedKV, pos: torch.Tensor, seq: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+                     out=None):
+    """nnc_op_kv_read_paged: (k, v), [tokens][n_kv_heads][head_dim], of positions `pos` of sequences `seq`.  out: None (then
+    padding tokens' rows hold anything), or a pair of tensors with the same strides."""
+    tokens = pos.shape[0]
+    shape = (tokens, cache.n_kv_heads, cache.head_dim)
+    if out is None:
+        dtype = dtype or (torch.bfloat16 if cache.dtype is torch.float8_e4m3fn else cache.dtype)
+        k, v = torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device)
+    else:
+        k, v = out
+        _rows(k, "out")
+        _rows(v, "out")
+        _need(k.shape == shape and v.shape == shape and k.stride() == v.stride() and k.dtype is v.dtype and (dtype or k.dtype) is k.dtype and _disjoint(k) and _disjoint(v),
+              "out: two tensors [tokens][n_kv_heads][head_dim] of one type with the same strides, no rows that overlap")
+    _need(k.dtype in _TYPES and k.dtype is not torch.float8_e4m3fn, "dtype: float32, bfloat16 or float16")
+    _same_device(cache.device, k, v, pos, seq)
+    _launch(lib.nnc_op_kv_read_paged, "nnc_op_kv_read_paged", cache.device, cache.ref, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], tokens,
+            k.stride(0), k.stride(1), _index(pos, tokens, "pos"), _index(seq, tokens, "seq") if seq is not None else None)
+    return k, v
+
+
+def attn_paged_scratch(device="cuda") -> torch.Tensor:
+    """A scratch buffer for op_attn_decode_paged, to be made once and kept; calls that share one must not overlap."""
+    return torch.zeros(ATTN_PAGED_SCRATCH_BYTES, dtype=torch.uint8, device=device)
+
+
+def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, scale: Optional[float] = None, window: int = 0,
+                         scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """nnc_op_attn_decode_paged: q [batch][n_q_heads][head_dim] (rows may be apart) against the first lens[b] positions of each
+    sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  Returns out, or (out, lse)."""
+    _rows(q, "q")
+    batch, nq, d = q.shape
+    _need(q.dtype in _TYPES and q.dtype is not torch.float8_e4m3fn and d == cache.head_dim and (q.stride(1) == d or nq == 1),
+          "q: [batch][n_q_heads][head_dim] of float32, bfloat16 or float16, heads next to each other")
+    if out is None:
+        out = torch.empty((batch, nq, d), dtype=q.dtype, device=q.device)
+    else:
+        _rows(out, "out")
+        _need(out.shape == q.shape and out.dtype is q.dtype and (out.stride(1) == d or nq == 1) and _disjoint(out),
+              "out: q's shape and type, heads next to each other, no rows that overlap")
+    lse = torch.empty((batch, nq), dtype=torch.float32, device=q.device) if want_lse else None
+    if scratch is None:
+        scratch = attn_paged_scratch(q.device)
+    _need(scratch.is_contiguous(), "scratch: a contiguous tensor (attn_paged_scratch)")
+    _same_device(cache.device, q, lens, out, scratch)
+    _launch(lib.nnc_op_attn_decode_paged, "nnc_op_attn_decode_paged", cache.device, q.data_ptr(), cache.ref, _index(lens, batch, "lens"), out.data_ptr(),
+            lse.data_ptr() if want_lse else None, _TYPES[q.dtype], batch, nq, q.stride(0), out.stride(0),
+            d ** -0.5 if scale is None else scale, window, scratch.data_ptr(), scratch.nbytes)
+    return (out, lse) if want_lse else out

@@ -657,7 +657,7 @@ const char *nnc_status_string(int status) {
         case NNC_ERR_WORKSPACE: return "workspace too small or misaligned";
         case NNC_ERR_CAPACITY: return "capacity exceeded";
         case NNC_ERR_CUDA: return "CUDA error";
-        case NNC_ERR_DEVICE_STATUS: return "a kernel reported a bounded wait that ran out";
+        case NNC_ERR_DEVICE_STATUS: return "a kernel reported a bounded wait that ran out, or a cache address out of range";
     }
     return "unknown status";
 }
@@ -921,6 +921,117 @@ int nnc_op_attn_prefill(const float *qkv, const void *kcache, const void *vcache
     cudaError_t e = launch_attn_prefill(lc, qkv, batch * T, T, kcache, vcache, false, out, out_lo, false, n_q_heads, n_kv_heads,
                                         max_seq, n_past);
     if (e == cudaErrorInvalidValue) return NNC_ERR_INVALID_ARG;
+    return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+// ---- rotary positions and the paged cache -------------------------------------------------------------
+
+int nnc_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, double original, double slow,
+                         double fast, double *freq, float *amplitude) {
+    if (!freq || rotary_dim <= 0 || rotary_dim % 2 || !(theta > 0.0) || scaling < NNC_ROPE_PLAIN || scaling > NNC_ROPE_RAMP_INDEX)
+        return NNC_ERR_INVALID_ARG;
+    const bool ramp = scaling == NNC_ROPE_RAMP_TURNS || scaling == NNC_ROPE_RAMP_INDEX;
+    if (scaling != NNC_ROPE_PLAIN && !(factor >= 1.0)) return NNC_ERR_INVALID_ARG;
+    if (scaling == NNC_ROPE_BASE && rotary_dim < 4) return NNC_ERR_INVALID_ARG;
+    if (ramp && !(original > 0.0 && slow > 0.0 && fast > slow)) return NNC_ERR_INVALID_ARG;
+    if (scaling == NNC_ROPE_RAMP_INDEX && theta == 1.0) return NNC_ERR_INVALID_ARG;
+    constexpr double kTwoPi = 6.283185307179586476925286766559;
+    const double d = rotary_dim;
+    const double base = scaling == NNC_ROPE_BASE ? theta * pow(factor, d / (d - 2.0)) : theta;
+    double lo = 0.0, hi = 0.0;
+    if (scaling == NNC_ROPE_RAMP_INDEX) {
+        // the (fractional) index whose pair makes n turns over the original context: theta^(-2i/d) * original = 2 pi n
+        auto index_of = [&](double turns) { return d * log(original / (kTwoPi * turns)) / (2.0 * log(theta)); };
+        lo = fmin(fmax(floor(index_of(fast)), 0.0), d - 1.0);
+        hi = fmin(fmax(ceil(index_of(slow)), 0.0), d - 1.0);
+        if (hi <= lo) hi = lo + 0.001;
+    }
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / d), g = 1.0;
+        if (scaling == NNC_ROPE_LINEAR) g = 0.0;
+        if (scaling == NNC_ROPE_RAMP_TURNS) g = (original * f / kTwoPi - slow) / (fast - slow);
+        if (scaling == NNC_ROPE_RAMP_INDEX) g = 1.0 - (i - lo) / (hi - lo);
+        g = fmin(fmax(g, 0.0), 1.0);
+        if (scaling != NNC_ROPE_PLAIN && scaling != NNC_ROPE_BASE) f *= g + (1.0 - g) / factor;
+        freq[i] = f;
+    }
+    if (amplitude) *amplitude = scaling == NNC_ROPE_RAMP_INDEX && factor > 1.0 ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+    return NNC_OK;
+}
+
+int nnc_op_rope(const void *x, void *y, int32_t type, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                int64_t x_row_stride, int64_t x_head_stride, int64_t y_row_stride, int64_t y_head_stride,
+                const int32_t *positions, const double *freq, int32_t rotary_dim, int32_t interleaved, int32_t inverse,
+                float amplitude, void *cuda_stream) {
+    if (type != NNC_F32 && type != NNC_BF16 && type != NNC_F16) return NNC_ERR_INVALID_ARG;
+    if (n_tokens < 0 || n_heads < 0 || head_dim > 1024 || rotary_dim < 2 || rotary_dim % 2 || rotary_dim > head_dim) return NNC_ERR_INVALID_ARG;
+    if (n_tokens == 0 || n_heads == 0) return NNC_OK;
+    if (!x || !y || !positions || !freq) return NNC_ERR_INVALID_ARG;
+    const uintptr_t el = type == NNC_F32 ? 4 : 2;
+    if ((uintptr_t)x % el || (uintptr_t)y % el || (uintptr_t)positions % 4 || (uintptr_t)freq % 8) return NNC_ERR_INVALID_ARG;
+    if ((int64_t)n_heads * head_dim > 0x3fffffff) return NNC_ERR_CAPACITY;
+    if (x == y && (x_row_stride != y_row_stride || x_head_stride != y_head_stride)) return NNC_ERR_INVALID_ARG;
+    LaunchCtx lc;
+    if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    cudaError_t e = launch_rope(lc, x, y, type, n_tokens, n_heads, head_dim, x_row_stride, x_head_stride, y_row_stride, y_head_stride,
+                                positions, freq, rotary_dim, interleaved != 0, inverse != 0, amplitude);
+    return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+static bool paged_ok(const nnc_paged_kv *c) {
+    if (!c || !c->k || !c->v || !c->page_table) return false;
+    if (c->type != NNC_BF16 && c->type != NNC_F16 && c->type != NNC_E4M3) return false;
+    if ((c->type == NNC_E4M3) != (c->k_scale != nullptr) || (c->type == NNC_E4M3) != (c->v_scale != nullptr)) return false;
+    if (((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 15) return false;
+    if ((uintptr_t)c->page_table & 3) return false;
+    if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1))) return false;
+    if (c->head_dim != 64 && c->head_dim != 128) return false;
+    if (c->n_pages <= 0 || c->n_kv_heads <= 0 || c->n_seqs <= 0 || c->pages_per_seq <= 0) return false;
+    return (int64_t)c->pages_per_seq * c->page_size <= 0x7fffffff - 1024;   // positions are 32-bit numbers
+}
+
+static int kv_rows_paged(const nnc_paged_kv *cache, bool write, void *k, void *v, int type, int n_tokens, int64_t row_stride,
+                         int64_t head_stride, const int32_t *pos, const int32_t *seq, void *cuda_stream) {
+    if (!paged_ok(cache) || n_tokens < 0 || (type != NNC_F32 && type != NNC_BF16 && type != NNC_F16)) return NNC_ERR_INVALID_ARG;
+    if (n_tokens == 0) return NNC_OK;
+    if (!k || !v || !pos || (!seq && n_tokens > cache->n_seqs)) return NNC_ERR_INVALID_ARG;
+    const int64_t el = type == NNC_F32 ? 4 : 2;
+    if ((((uintptr_t)k | (uintptr_t)v) & 15) || (row_stride * el) % 16 || (head_stride * el) % 16) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)pos | (uintptr_t)seq) & 3) return NNC_ERR_INVALID_ARG;
+    if ((int64_t)n_tokens * cache->n_kv_heads > (int64_t)1 << 33) return NNC_ERR_CAPACITY;   // blocks of one launch
+    LaunchCtx lc;
+    if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    return launch_kv_paged(lc, *cache, write, k, v, type, n_tokens, row_stride, head_stride, pos, seq) == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+int nnc_op_kv_write_paged(const nnc_paged_kv *cache, const void *k, const void *v, int32_t type, int32_t n_tokens,
+                          int64_t row_stride, int64_t head_stride, const int32_t *pos, const int32_t *seq, void *cuda_stream) {
+    return kv_rows_paged(cache, true, const_cast<void *>(k), const_cast<void *>(v), type, n_tokens, row_stride, head_stride, pos, seq, cuda_stream);
+}
+
+int nnc_op_kv_read_paged(const nnc_paged_kv *cache, void *k, void *v, int32_t type, int32_t n_tokens, int64_t row_stride,
+                         int64_t head_stride, const int32_t *pos, const int32_t *seq, void *cuda_stream) {
+    return kv_rows_paged(cache, false, k, v, type, n_tokens, row_stride, head_stride, pos, seq, cuda_stream);
+}
+
+int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, void *out, float *lse, int32_t type,
+                             int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
+                             void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    if (!paged_ok(cache) || batch < 0 || batch > cache->n_seqs || window < 0) return NNC_ERR_INVALID_ARG;
+    if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads) return NNC_ERR_INVALID_ARG;
+    if (type != NNC_F32 && type != NNC_BF16 && type != NNC_F16) return NNC_ERR_INVALID_ARG;
+    if (cache->type != NNC_E4M3 && type != NNC_F32 && type != cache->type) return NNC_ERR_INVALID_ARG;
+    if (batch == 0) return NNC_OK;
+    if (!q || !lens || !out || !scratch) return NNC_ERR_INVALID_ARG;
+    const int64_t el = type == NNC_F32 ? 4 : 2;
+    if ((((uintptr_t)q | (uintptr_t)out) & 15) || (q_stride * el) % 16 || (out_stride * el) % 16) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)lens | (uintptr_t)lse) & 3) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)scratch & 255) || scratch_bytes < NNC_ATTN_PAGED_SCRATCH_BYTES) return NNC_ERR_WORKSPACE;
+    LaunchCtx lc;
+    if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    cudaError_t e = launch_attn_paged(lc, q, *cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, window, scratch,
+                                      scratch_bytes);
+    if (e == cudaErrorInvalidValue) return NNC_ERR_CAPACITY;
     return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
 }
 

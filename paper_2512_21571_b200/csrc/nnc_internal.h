@@ -121,6 +121,19 @@ cudaError_t launch_attn_prefill(const LaunchCtx &lc, const float *qkv, int rows,
 // fp16 image of cache rows [0, n_pos) of every (sequence, KV head): dst and src share the [heads][max_seq][128] layout
 cudaError_t launch_kv_rows_to_f16(const LaunchCtx &lc, const bf16 *src, void *dst, int heads, int max_seq, int n_pos);
 
+// ---- rotary positions and the paged cache (rope.cu, kv_paged.cu, attn_paged.cu) -----------------------------------
+// All of them expect arguments that nnc_api.cu has checked.
+cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, int n_tokens, int n_heads, int head_dim, int64_t x_row,
+                        int64_t x_head, int64_t y_row, int64_t y_head, const int32_t *positions, const double *freq,
+                        int rotary_dim, bool interleaved, bool inverse, float amplitude);
+// write: rows go from k, v into the cache; otherwise from the cache to k, v (`type` is theirs either way)
+cudaError_t launch_kv_paged(const LaunchCtx &lc, const nnc_paged_kv &cache, bool write, void *k, void *v, int type, int n_tokens,
+                            int64_t row_stride, int64_t head_stride, const int32_t *pos, const int32_t *seq);
+constexpr int kPagedMaxCtas = NNC_ATTN_PAGED_TICKET_BYTES / 4;   // one ticket word per CTA of the attention's grid
+cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, void *out, float *lse,
+                              int type, int batch, int n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int window,
+                              void *scratch, size_t scratch_bytes);
+
 // ---- GEMM (gemm_tc.cu) --------------------------------------------------------------------------------
 enum GemmEpi { kEpiStoreF32 = 0, kEpiStoreBf16 = 1, kEpiAccumF32 = 2, kEpiSwigluBf16 = 3 };
 bool gemm_tc_available();
