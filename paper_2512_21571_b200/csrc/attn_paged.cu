@@ -29,6 +29,10 @@ namespace nnc {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr float kLn2 = 0.69314718055994530942f;
+// partial results that one CTA joins: up to kMaxJoin at once, in groups of kJoinGroup first where there are more (one SM reads
+// them at some 100 GB/s, so a long list is cheaper in two rounds)
+constexpr int kMaxJoin = 48, kJoinGroup = 24;
 
 struct PagedAttnParams {
     PagedView c;
@@ -56,15 +60,18 @@ struct Shape {
     static constexpr int kStages = kData == 8192 ? 3 : 5;
     static constexpr int kTilesD = D / 16;                   // 16-row tiles of O^T
     static constexpr int kOwn = kTilesD / kWarps;            // tiles that a warp merges
-    static constexpr int kComb = kWarps * 3 * kOwn * 4 * 32 * 4;   // bytes: the pieces that warps hand to one another
+    static constexpr int kHand = kWarps * 3 * kOwn * 4 * 32 * 4;   // bytes: the pieces that warps hand to one another,
+    static constexpr int kJoin = 8 * NT * kMaxJoin * 12 + 8 * NT * 8;   // or (m, l), weights and sums where results are joined
+    static constexpr int kComb = kHand > kJoin ? kHand : kJoin;
     static constexpr int kSmem = kWarps * kStages * kStage + kComb;
-    static constexpr int kSlotFloats = NT * (kTilesD * 128 + 16);   // a partial result: O^T fragments, (m, l) of 8 heads
+    static constexpr int kSlotFloats = 8 * NT * (D + 2);     // a partial result: o~ of 8 NT heads, then their (m, l)
 };
 
 struct AttnShared {
     float ml[kWarps][8][2];
     int sums[kWarps];
-    int first_b, first_rest, is_last;
+    int first_b, first_rest;
+    struct { int c_lo, c_hi, q_head, heads_here, b, last; } split[2];   // this CTA's partial results: slot 0's and slot 1's
 };
 
 // byte offset of 16-byte piece c of row r, arranged so that eight rows of one column of pieces lie in different banks
@@ -73,7 +80,10 @@ template <int ROW> __device__ __forceinline__ int swizzled(int r, int c) {
     else return (r >> 1) * 128 + ((((r & 1) << 2 | c) ^ ((r >> 1) & 7)) << 4);
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_or_zeros(uint32_t dst, const void *src, bool live) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -91,10 +101,10 @@ __device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t addr) {
 template <bool BF>
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b)[2]) {
     if constexpr (BF)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b[0]), "r"(b[1]));
 }
 
@@ -103,6 +113,18 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
+}
+
+// 2^x; what is below 2^-126 is 0
+__device__ __forceinline__ float exp2_flush(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// four E4M3 codes as two fp16 pairs: the low two, the high two
+__device__ __forceinline__ void codes_to_f16(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+    asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 
 // x, y as sums of N terms of 16 bits (each term the rounding of what the ones before it leave)
@@ -123,6 +145,8 @@ template <bool BF, int N> __device__ __forceinline__ void split(float x, float y
 // what a sequence attends to: positions [start, end), and its tiles, counted from `start` rounded down to 16
 struct Reach {
     int start, end, tiles;
+    // places of a (sequence, head) in the list: its tiles and one for what it costs to begin and to end
+    __device__ __forceinline__ int places() const { return tiles ? tiles + 1 : 0; }
 };
 template <int TILE> __device__ __forceinline__ Reach reach_of(const PagedAttnParams &p, int b) {
     const int most = p.c.pages_per_seq << p.c.page_shift;
@@ -135,13 +159,16 @@ template <int TILE> __device__ __forceinline__ Reach reach_of(const PagedAttnPar
     return r;
 }
 
-// a place in the list of tiles
+// a tile, and its place in the list
 struct Place {
     Reach r;
     int b, hh, tile;   // hh: KV head * chunks + chunk of its query heads
+    int index;
 };
 template <int TILE> __device__ __forceinline__ void step(const PagedAttnParams &p, Place &at, int heads) {
+    ++at.index;
     if (++at.tile < at.r.tiles) return;
+    ++at.index;
     at.tile = 0;
     if (++at.hh < heads) return;
     at.hh = 0;
@@ -161,13 +188,14 @@ __device__ __forceinline__ void store_out(const PagedAttnParams &p, long long at
 template <int D, int NT, int KV, int QT, int PT>
 __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedAttnParams p) {
     typedef Shape<D, NT, KV> S;
-    constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3;
+    constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3, kFresh = QT > 1;
     constexpr int PB = S::kPB, TILE = S::kTile, ROW = S::kRow;
     // fp16 probabilities are scaled by 2^14, so that small ones keep their bits (the sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 14.f;
     extern __shared__ __align__(128) char smem[];
     __shared__ AttnShared sh;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     const int g8 = lane >> 2, t4 = lane & 3;
     const int heads = p.c.n_kv * p.chunks;
 
@@ -175,7 +203,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
     const int per = (p.batch + kWarps * 32 - 1) / (kWarps * 32);
     const int b_lo = min(tid * per, p.batch), b_hi = min(b_lo + per, p.batch);
     int mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += reach_of<TILE>(p, b).tiles;
+    for (int b = b_lo; b < b_hi; ++b) mine += reach_of<TILE>(p, b).places();
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -188,7 +216,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sh.sums[w]; all += sh.sums[w]; }
     const int excl = before + incl - mine;
-    const long long total = (long long)all * heads;   // the host bounds it by 2^31
+    const long long total = (long long)all * heads;   // places; the host bounds them by 2^31
     const int n_ctas = (int)min((long long)gridDim.x, total);
     const int cta = blockIdx.x;
 
@@ -209,7 +237,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
             long long rest = t0 - lo;
             int b = b_lo;
             for (; b < b_hi; ++b) {
-                const long long n = (long long)reach_of<TILE>(p, b).tiles * heads;
+                const long long n = (long long)reach_of<TILE>(p, b).places() * heads;
                 if (rest < n) break;
                 rest -= n;
             }
@@ -221,8 +249,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
     Place ahead;   // where the copies are
     ahead.b = sh.first_b;
     ahead.r = reach_of<TILE>(p, ahead.b);
-    ahead.hh = sh.first_rest / ahead.r.tiles;
-    ahead.tile = sh.first_rest - ahead.hh * ahead.r.tiles;
+    ahead.hh = sh.first_rest / ahead.r.places();
+    ahead.tile = sh.first_rest - ahead.hh * ahead.r.places();
+    ahead.index = t0;
+    if (ahead.tile == ahead.r.tiles) { --ahead.index; --ahead.tile; step<TILE>(p, ahead, heads); }   // the place after its tiles
+    if (ahead.index >= t1) return;
     Place now = ahead;   // where the products are
 
     // ---- copies of this warp's block of a tile ----
@@ -238,10 +269,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         }
     };
     uint32_t present = 0;   // a bit per 16 positions of each stage: its page exists
+    constexpr int kPieces = ROW / 16, kRowsPerStep = 32 / kPieces, kSteps = 16 / kRowsPerStep;
+    const int r0 = lane / kPieces, c0 = lane % kPieces;   // this lane's row and piece in the first step of 16 rows
     auto request = [&](int stage) {
-        constexpr int kPieces = ROW / 16, kRowsPerStep = 32 / kPieces;
         const int p0 = (ahead.r.start & ~15) + ahead.tile * TILE + warp * PB;
-        const int r0 = lane / kPieces, c0 = lane % kPieces, head = ahead.hh / p.chunks;
+        const int head = ahead.hh / p.chunks;
         const uint32_t base = ring + stage * S::kStage;
         present &= ~(((1u << S::kSub) - 1u) << (stage * S::kSub));
 #pragma unroll
@@ -249,73 +281,98 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
             const int pb = p0 + 16 * u;
             if (pb >= ahead.r.end) break;
             const bool there = (unsigned)pages[u] < (unsigned)p.c.n_pages;
-            if (there) present |= 1u << (stage * S::kSub + u);
-            else if (lane == 0) paged_complain(p.c);
             const long long row = there ? paged_row(p.c, pages[u], head, pb & ((1 << p.c.page_shift) - 1)) : 0;
-            const char *ks = p.c.k + row * ROW + r0 * ROW + c0 * 16, *vs = p.c.v + row * ROW + r0 * ROW + c0 * 16;
+            const char *ks = p.c.k + row * ROW + lane * 16, *vs = p.c.v + row * ROW + lane * 16;   // 16 rows are one run of bytes
+            if (there && pb >= ahead.r.start && pb + 16 <= ahead.r.end) {
 #pragma unroll
-            for (int i = 0; i < 16 / kRowsPerStep; ++i) {
-                const int r = r0 + i * kRowsPerStep;
-                const bool live = there && pb + r >= ahead.r.start && pb + r < ahead.r.end;
-                const int dst = swizzled<ROW>(16 * u + r, c0);
-                copy16(base + dst, live ? ks + i * kRowsPerStep * ROW : p.c.k, live);
-                copy16(base + PB * ROW + dst, live ? vs + i * kRowsPerStep * ROW : p.c.v, live);
+                for (int i = 0; i < kSteps; ++i) {
+                    const uint32_t dst = base + swizzled<ROW>(16 * u + r0 + i * kRowsPerStep, c0);
+                    copy16(dst, ks + i * 512);
+                    copy16(dst + PB * ROW, vs + i * 512);
+                }
+            } else {
+                if (!there && lane == 0) paged_complain(p.c);
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const int r = r0 + i * kRowsPerStep;
+                    const bool live = there && pb + r >= ahead.r.start && pb + r < ahead.r.end;
+                    const uint32_t dst = base + swizzled<ROW>(16 * u + r, c0);
+                    copy16_or_zeros(dst, live ? ks + i * 512 : p.c.k, live);
+                    copy16_or_zeros(dst + PB * ROW, live ? vs + i * 512 : p.c.v, live);
+                }
             }
+            if (there) present |= 1u << (stage * S::kSub + u);
             if constexpr (CODES) {
                 if (lane < 2)
-                    copy16(base + S::kData + lane * PB + 16 * u, there ? (lane ? p.c.v_scale : p.c.k_scale) + row : p.c.k_scale, there);
+                    copy16_or_zeros(base + S::kData + lane * PB + 16 * u, there ? (lane ? p.c.v_scale : p.c.k_scale) + row : p.c.k_scale, there);
             }
         }
     };
-
-    const int n = t1 - t0;
-    find_pages();
-    int asked = 0;
-#pragma unroll
-    for (int st = 0; st < S::kStages - 1; ++st) {
-        if (asked < n) {
-            request(st);
-            ++asked;
-            step<TILE>(p, ahead, heads);
-            if (asked < n) find_pages();
-        }
-        copy_commit();
-    }
 
     // ---- per (sequence, head) state ----
     uint32_t qf[NT][QT][D / 16][2];
     float qmul[NT][2];
     float o[NT][S::kTilesD][4], m_run[NT][2], l_run[NT][2];
-    int piece_first = 0;   // list index of the piece's first tile, in this CTA's share
+    int piece_first = now.index;   // place of the piece's first tile
 
-    auto begin_piece = [&]() {
+    // Queries of the (sequence, head) at `now`: lane (g8, t4) holds head g8's elements of contraction columns 2 t4, 2 t4 + 1, 2 t4 + 8,
+    // 2 t4 + 9 of every step of 16; with codes, a key's four neighbouring codes 4 t4 .. 4 t4 + 3 stand in those columns.
+    // All of them are requested before any is used.
+    uint32_t raw[NT][D / 16][4];
+    auto load_queries = [&]() {
         const int kv_head = now.hh / p.chunks, chunk = now.hh - kv_head * p.chunks;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            // queries: lane (g8, t4) holds head g8's elements of contraction columns 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9 of
-            // every step of 16; with codes, a key's four neighbouring codes 4 t4 .. 4 t4 + 3 stand in those columns
             const int g = chunk * (8 * NT) + nt * 8 + g8;
-            const bool there = g < p.group;
-            const long long at = now.b * p.q_stride + (long long)(kv_head * p.group + (there ? g : 0)) * D;
+            const long long at = now.b * p.q_stride + (long long)(kv_head * p.group + (g < p.group ? g : 0)) * D + (CODES ? 4 : 2) * t4;
+            constexpr int kApart = CODES ? 2 : 8;
+            if (p.type == NNC_F32) {
+                const float *src = reinterpret_cast<const float *>(p.q) + at;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    const uint2 a = *reinterpret_cast<const uint2 *>(src + 16 * s), b = *reinterpret_cast<const uint2 *>(src + 16 * s + kApart);
+                    raw[nt][s][0] = a.x; raw[nt][s][1] = a.y; raw[nt][s][2] = b.x; raw[nt][s][3] = b.y;
+                }
+            } else {
+                const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q) + at;
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    raw[nt][s][0] = *reinterpret_cast<const uint32_t *>(src + 16 * s);
+                    raw[nt][s][1] = *reinterpret_cast<const uint32_t *>(src + 16 * s + kApart);
+                }
+            }
+        }
+    };
+    auto begin_piece = [&]() {
+        const int chunk = now.hh % p.chunks;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool there = chunk * (8 * NT) + nt * 8 + g8 < p.group;
             float f[D / 16][4];
+            if (p.type == NNC_F32) {
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[s][e] = __uint_as_float(raw[nt][s][e]);
+            } else if (p.type == NNC_BF16) {
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) { f[s][2 * e] = bf16_lo(raw[nt][s][e]); f[s][2 * e + 1] = bf16_hi(raw[nt][s][e]); }
+            } else {
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const __half2 h = *reinterpret_cast<const __half2 *>(&raw[nt][s][e]);
+                        f[s][2 * e] = __low2float(h); f[s][2 * e + 1] = __high2float(h);
+                    }
+            }
             float top = 0.f;
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                const int ia = CODES ? 16 * s + 4 * t4 : 16 * s + 2 * t4, ib = CODES ? ia + 2 : ia + 8;
-                if (p.type == NNC_F32) {
-                    const float2 a = *reinterpret_cast<const float2 *>(p.q + (at + ia) * 4), b = *reinterpret_cast<const float2 *>(p.q + (at + ib) * 4);
-                    f[s][0] = a.x; f[s][1] = a.y; f[s][2] = b.x; f[s][3] = b.y;
-                } else {
-                    const uint32_t a = *reinterpret_cast<const uint32_t *>(p.q + (at + ia) * 2), b = *reinterpret_cast<const uint32_t *>(p.q + (at + ib) * 2);
-                    if (p.type == NNC_BF16) { f[s][0] = bf16_lo(a); f[s][1] = bf16_hi(a); f[s][2] = bf16_lo(b); f[s][3] = bf16_hi(b); }
-                    else {
-                        f[s][0] = __half2float(__ushort_as_half((uint16_t)a)); f[s][1] = __half2float(__ushort_as_half((uint16_t)(a >> 16)));
-                        f[s][2] = __half2float(__ushort_as_half((uint16_t)b)); f[s][3] = __half2float(__ushort_as_half((uint16_t)(b >> 16)));
-                    }
-                }
+            for (int s = 0; s < D / 16; ++s)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) { if (!there) f[s][e] = 0.f; top = fmaxf(top, fabsf(f[s][e])); }
-            }
             float undo = 1.f;
             if constexpr (!BF) {
                 // fp16 operands: the row times the power of two that brings its largest magnitude into [2^14, 2^15)
@@ -349,6 +406,29 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         }
     };
 
+    // asks L2 for the queries of the (sequence, head) that the copies have reached
+    auto prefetch_queries = [&]() {
+        const int kv_head = ahead.hh / p.chunks, chunk = ahead.hh - kv_head * p.chunks;
+        const int size = p.type == NNC_F32 ? 4 : 2, at = (warp * 32 + lane) * 128;   // a line each
+        const int q_head = kv_head * p.group + chunk * (8 * NT), heads_here = min(8 * NT, p.group - chunk * (8 * NT));
+        if (at < heads_here * D * size)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.q + (ahead.b * p.q_stride + (long long)q_head * D) * size + at));
+    };
+
+    if (tid < 2) sh.split[tid].c_lo = -1;
+    find_pages();
+    load_queries();   // before the rows: behind them in the memory system they would come last
+#pragma unroll
+    for (int st = 0; st < S::kStages - 1; ++st) {
+        if (ahead.index < t1) {
+            request(st);
+            step<TILE>(p, ahead, heads);
+            if (ahead.index < t1) find_pages();
+        }
+        copy_commit();
+    }
+    begin_piece();
+
     // lane's row and piece in the four 8x8 matrices of an ldmatrix: K (rows = positions) and V (transposed)
     const int lr = lane & 7, lm = lane >> 3;
     auto products = [&](int stage) {
@@ -356,64 +436,93 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         if (p0 >= now.r.end) return;
         const uint32_t kb = ring + stage * S::kStage, vb = kb + PB * ROW;
         const char *scales = smem + warp * (S::kStages * S::kStage) + stage * S::kStage + S::kData;
-        float s[S::kSub][NT][4], ev[S::kSub][2];
+        // scores.  Even and odd steps (and the lower terms of fp32 queries) have sums of their own: shorter chains, and the tensor
+        // cores cut what they add, so shorter chains of large partial sums are nearer to fp32 as well
+        float s[S::kSub][NT][4];
+        {
+            constexpr int kSums = QT > 1 ? 3 : 2;
+            float acc[kSums][S::kSub][NT][4];
 #pragma unroll
-        for (int u = 0; u < S::kSub; ++u) {
+            for (int x = 0; x < kSums; ++x)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[u][nt][0] = s[u][nt][1] = s[u][nt][2] = s[u][nt][3] = 0.f;
-            if constexpr (!CODES) {
+                for (int u = 0; u < S::kSub; ++u)
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t a[4];
-                    ldsm4(a, kb + swizzled<ROW>(16 * u + lr + (lm & 1) * 8, 2 * c + (lm >> 1)));
+                    for (int nt = 0; nt < NT; ++nt) acc[x][u][nt][0] = acc[x][u][nt][1] = acc[x][u][nt][2] = acc[x][u][nt][3] = 0.f;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+            for (int c = 0; c < D / 16; c += 2) {
 #pragma unroll
-                        for (int i = 0; i < QT; ++i) mma16816<BF>(s[u][nt], a[0], a[1], a[2], a[3], qf[nt][i][c]);
-                }
-            } else {
+                for (int u = 0; u < S::kSub; ++u) {
+                    uint32_t a[2][4];
+                    if constexpr (!CODES) {
 #pragma unroll
-                for (int c = 0; c < D / 16; c += 2) {
-                    uint32_t a[4];
-                    ldsm4(a, kb + swizzled<ROW>(16 * u + lr + (lm & 1) * 8, c + (lm >> 1)));
+                        for (int e = 0; e < 2; ++e) ldsm4(a[e], kb + swizzled<ROW>(16 * u + lr + (lm & 1) * 8, 2 * (c + e) + (lm >> 1)));
+                    } else {
+                        uint32_t x[4];
+                        ldsm4(x, kb + swizzled<ROW>(16 * u + lr + (lm & 1) * 8, c + (lm >> 1)));
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t a0 = e4m3x2_to_f16x2(a[2 * e] & 0xffffu), a2 = e4m3x2_to_f16x2(a[2 * e] >> 16);
-                        const uint32_t a1 = e4m3x2_to_f16x2(a[2 * e + 1] & 0xffffu), a3 = e4m3x2_to_f16x2(a[2 * e + 1] >> 16);
+                        for (int e = 0; e < 2; ++e) {
+                            codes_to_f16(x[2 * e], a[e][0], a[e][2]);
+                            codes_to_f16(x[2 * e + 1], a[e][1], a[e][3]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int i = 0; i < QT; ++i) mma16816<false>(s[u][nt], a0, a1, a2, a3, qf[nt][i][c + e]);
-                    }
+                            for (int i = 0; i < QT; ++i)
+                                mma16816<BF>(acc[i == 0 ? e : 2][u][nt], a[e][0], a[e][1], a[e][2], a[e][3], qf[nt][i][c + e]);
                 }
             }
-            const bool there = present >> (stage * S::kSub + u) & 1u;
+#pragma unroll
+            for (int u = 0; u < S::kSub; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        s[u][nt][x] = acc[0][u][nt][x] + acc[1][u][nt][x];
+                        if constexpr (QT > 1) s[u][nt][x] += acc[2][u][nt][x];
+                    }
+        }
+        const uint32_t here = present >> (stage * S::kSub) & ((1u << S::kSub) - 1u);
+        const bool full = p0 >= now.r.start && p0 + PB <= now.r.end && here == (1u << S::kSub) - 1u;
+        float back[S::kSub][2];   // 2^-exponent of the value rows
+#pragma unroll
+        for (int u = 0; u < S::kSub; ++u)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {   // rows g8 and g8 + 8
-                const int pos = p0 + 16 * u + g8 + 8 * r;
-                const bool live = there && pos >= now.r.start && pos < now.r.end;
-                float ks = 1.f;
-                ev[u][r] = 0.f;
+                float ks = 1.f, ev = 0.f;
                 if constexpr (CODES) {
-                    const int at = 16 * u + g8 + 8 * r;
-                    const uint32_t bk = live ? (uint8_t)scales[at] : 127u, bv = live ? (uint8_t)scales[PB + at] : 127u;
-                    ks = scale_from_byte(bk);
-                    ev[u][r] = (float)((int)bv - 127);
+                    const uint32_t bk = (uint8_t)scales[16 * u + g8 + 8 * r], bv = (uint8_t)scales[PB + 16 * u + g8 + 8 * r];
+                    ks = __uint_as_float(bk << 23);
+                    ev = __uint_as_float(0x4b000000u | bv) - 8388735.f;   // bv - 127: 2^23 + bv as fp32, no conversion
+                    back[u][r] = __uint_as_float(0x7f000000u - (bv << 23));
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float x = s[u][nt][2 * r + e] * qmul[nt][e] * ks + ev[u][r];
-                        s[u][nt][2 * r + e] = live ? x : -INFINITY;
+                        float &x = s[u][nt][2 * r + e];
+                        x = CODES ? fmaf(x, qmul[nt][e] * ks, ev) : x * qmul[nt][e];
                     }
             }
+        if (!full) {
+#pragma unroll
+            for (int u = 0; u < S::kSub; ++u)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int pos = p0 + 16 * u + g8 + 8 * r;
+                    if ((here >> u & 1u) && pos >= now.r.start && pos < now.r.end) continue;
+                    back[u][r] = 1.f;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) s[u][nt][2 * r] = s[u][nt][2 * r + 1] = -INFINITY;
+                }
         }
         // ---- online softmax; with codes, of the scores plus the value rows' exponents ----
         uint32_t pf[S::kSub][NT][PT][2];
+        float alpha[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float alpha[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float mx = -INFINITY;
@@ -424,22 +533,18 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
                 const float m_new = fmaxf(m_run[nt][e], mx);
                 const float ref = (m_new == -INFINITY ? 0.f : m_new) - kLift;   // nothing attended so far: every weight is 0
-                alpha[e] = exp2f(m_run[nt][e] - kLift - ref);
+                alpha[nt][e] = exp2_flush(m_run[nt][e] - kLift - ref);
                 m_run[nt][e] = m_new;
                 float sum = 0.f;
 #pragma unroll
                 for (int u = 0; u < S::kSub; ++u)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float w = exp2f(s[u][nt][2 * r + e] - ref);
+                        const float w = exp2_flush(s[u][nt][2 * r + e] - ref);
                         s[u][nt][2 * r + e] = w;
-                        sum += CODES ? w * __uint_as_float((uint32_t)(127 - (int)ev[u][r]) << 23) : w;
+                        sum = CODES ? fmaf(w, back[u][r], sum) : sum + w;
                     }
-                l_run[nt][e] = l_run[nt][e] * alpha[e] + sum;
-            }
-            if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-#pragma unroll
-                for (int i = 0; i < S::kTilesD; ++i) { o[nt][i][0] *= alpha[0]; o[nt][i][1] *= alpha[1]; o[nt][i][2] *= alpha[0]; o[nt][i][3] *= alpha[1]; }
+                l_run[nt][e] = fmaf(l_run[nt][e], alpha[nt][e], sum);
             }
 #pragma unroll
             for (int u = 0; u < S::kSub; ++u) {
@@ -449,72 +554,76 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
 #pragma unroll
                 for (int i = 0; i < PT; ++i) { pf[u][nt][i][0] = transpose8(lo[i]); pf[u][nt][i][1] = transpose8(hi[i]); }
             }
+            // fp32 results: a block's products get a sum of their own that is then added in fp32 (the tensor cores' cut of every
+            // addition would pile up over a long share); 16-bit results are rounded far above that
+            if (!kFresh && __any_sync(0xffffffffu, alpha[nt][0] != 1.f || alpha[nt][1] != 1.f)) {
+#pragma unroll
+                for (int i = 0; i < S::kTilesD; ++i) {
+                    o[nt][i][0] *= alpha[nt][0]; o[nt][i][1] *= alpha[nt][1]; o[nt][i][2] *= alpha[nt][0]; o[nt][i][3] *= alpha[nt][1];
+                }
+            }
         }
         // ---- O^T += V^T P^T.  o[nt][i]: columns are heads 2 t4, 2 t4 + 1; rows are elements 16 i + g8 and 16 i + 8 + g8, or
         //      with codes 16 i + 2 g8 and 16 i + 2 g8 + 1 ----
+        int subs = 1;   // 16-position parts that hold anything: what was not copied may be no number
+        if constexpr (S::kSub > 1) subs = min(S::kSub, (now.r.end - p0 + 15) >> 4);
 #pragma unroll
-        for (int u = 0; u < S::kSub; ++u) {
-            if (p0 + 16 * u >= now.r.end) break;   // nothing was copied there: what the stage holds may be no number
-            if constexpr (!CODES) {
+        for (int i = 0; i < S::kTilesD; i += 2) {
+            float fresh[NT][2][4];
+            if constexpr (kFresh) {
 #pragma unroll
-                for (int i = 0; i < S::kTilesD; ++i) {
-                    uint32_t a[4];
-                    ldsm4_trans(a, vb + swizzled<ROW>(16 * u + lr + (lm >> 1) * 8, 2 * i + (lm & 1)));
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int e = 0; e < 2; ++e) fresh[nt][e][0] = fresh[nt][e][1] = fresh[nt][e][2] = fresh[nt][e][3] = 0.f;
+            }
 #pragma unroll
-                        for (int j = 0; j < PT; ++j) mma16816<BF>(o[nt][i], a[0], a[1], a[2], a[3], pf[u][nt][j]);
-                }
-            } else {
+            for (int u = 0; u < S::kSub; ++u) {
+                if (u >= subs) break;
+                uint32_t a[2][4];
+                if constexpr (!CODES) {
 #pragma unroll
-                for (int i = 0; i < S::kTilesD; i += 2) {
-                    uint32_t a[4];   // positions 0-7 and 8-15 of piece i, then of piece i + 1
-                    ldsm4_trans(a, vb + swizzled<ROW>(16 * u + lr + (lm & 1) * 8, i + (lm >> 1)));
+                    for (int e = 0; e < 2; ++e) ldsm4_trans(a[e], vb + swizzled<ROW>(16 * u + lr + (lm >> 1) * 8, 2 * (i + e) + (lm & 1)));
+                } else {
+                    uint32_t x[4];   // positions 0-7 and 8-15 of piece i, then of piece i + 1
+                    ldsm4_trans(x, vb + swizzled<ROW>(16 * u + lr + (lm & 1) * 8, i + (lm >> 1)));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         // a lane holds two neighbouring codes of two positions: pair them by code
-                        const uint32_t x = __byte_perm(a[2 * e], 0, 0x3120), y = __byte_perm(a[2 * e + 1], 0, 0x3120);
-                        const uint32_t a0 = e4m3x2_to_f16x2(x & 0xffffu), a1 = e4m3x2_to_f16x2(x >> 16);
-                        const uint32_t a2 = e4m3x2_to_f16x2(y & 0xffffu), a3 = e4m3x2_to_f16x2(y >> 16);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int j = 0; j < PT; ++j) mma16816<false>(o[nt][i + e], a0, a1, a2, a3, pf[u][nt][j]);
+                        codes_to_f16(__byte_perm(x[2 * e], 0, 0x3120), a[e][0], a[e][1]);
+                        codes_to_f16(__byte_perm(x[2 * e + 1], 0, 0x3120), a[e][2], a[e][3]);
                     }
                 }
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < PT; ++j) {
+                            if constexpr (kFresh) mma16816<BF>(fresh[nt][e], a[e][0], a[e][1], a[e][2], a[e][3], pf[u][nt][j]);
+                            else mma16816<BF>(o[nt][i + e], a[e][0], a[e][1], a[e][2], a[e][3], pf[u][nt][j]);
+                        }
+            }
+            if constexpr (kFresh) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) o[nt][i + e][x] = fmaf(o[nt][i + e][x], alpha[nt][x & 1], fresh[nt][e][x]);
             }
         }
     };
 
-    // ---- writing results: o_own, M, L hold this warp's tiles of the joined result ----
-    auto write_head_tiles = [&](int nt, const float (&own)[S::kOwn][4], const float (&M)[2], const float (&L)[2]) {
-        const int kv_head = now.hh / p.chunks, chunk = now.hh - kv_head * p.chunks;
-        const int n_q = p.c.n_kv * p.group;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int g = chunk * (8 * NT) + nt * 8 + 2 * t4 + e;
-            if (g >= p.group) continue;
-            const float inv = L[e] == 0.f ? 0.f : 1.f / L[e];
-            const long long at = now.b * p.out_stride + (long long)(kv_head * p.group + g) * D;
-#pragma unroll
-            for (int j = 0; j < S::kOwn; ++j) {
-                const int i = warp * S::kOwn + j;
-                const int d0 = CODES ? 16 * i + 2 * g8 : 16 * i + g8, d1 = CODES ? d0 + 1 : d0 + 8;
-                store_out(p, at + d0, own[j][e] * inv);
-                store_out(p, at + d1, own[j][2 + e] * inv);
-            }
-            if (p.lse && warp == 0 && g8 == 0)
-                p.lse[(long long)now.b * n_q + kv_head * p.group + g] =
-                    L[e] == 0.f ? -INFINITY : (M[e] + log2f(L[e])) * 0.69314718055994530942f;
-        }
-    };
-
+    // ---- results.  A warp's fragments of O^T tile i: rows d0 (and d1) of two heads ----
     float (*comb)[3][S::kOwn][32][4] = reinterpret_cast<float (*)[3][S::kOwn][32][4]>(smem + kWarps * S::kStages * S::kStage);
 
-    auto end_piece = [&](int last_index) {   // list indices, counted from the list's begin
-        const int item_lo = last_index - now.tile, item_hi = item_lo + now.r.tiles;   // this (sequence, head)'s tiles
-        const int first = t0 + piece_first;
-        const bool whole = first == item_lo && last_index + 1 == item_hi;
+    auto end_piece = [&]() {
+        const int item_lo = now.index - now.tile, item_hi = item_lo + now.r.tiles;   // places of this (sequence, head)'s tiles
+        const int first = piece_first;
+        const bool whole = first == item_lo && now.index + 1 == item_hi;
+        const int kv_head = now.hh / p.chunks, chunk = now.hh - kv_head * p.chunks;
+        const int q_head = kv_head * p.group + chunk * (8 * NT), heads_here = min(8 * NT, p.group - chunk * (8 * NT));
+        const long long out_at = now.b * p.out_stride + (long long)q_head * D, lse_at = (long long)now.b * (p.c.n_kv * p.group) + q_head;
         // partial results: slot 0 of a CTA for a piece that continues an earlier CTA's, slot 1 for one that starts here
         float *slot = p.part + (size_t)(2 * cta + (first == item_lo ? 1 : 0)) * S::kSlotFloats;
         if (!whole && !NNC_BC((size_t)(2 * cta + 2) * S::kSlotFloats <= p.part_floats, 3201)) return;
@@ -563,91 +672,177 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
                     sum[j][0] = fmaf(wgt[w][0], v.x, sum[j][0]); sum[j][1] = fmaf(wgt[w][1], v.y, sum[j][1]);
                     sum[j][2] = fmaf(wgt[w][0], v.z, sum[j][2]); sum[j][3] = fmaf(wgt[w][1], v.w, sum[j][3]);
                 }
-            if (whole) {
-                write_head_tiles(nt, sum, M, L);
-            } else {
-                float *o_part = slot + nt * (S::kTilesD * 128 + 16);
 #pragma unroll
-                for (int j = 0; j < S::kOwn; ++j)
-                    *reinterpret_cast<float4 *>(o_part + ((warp * S::kOwn + j) * 32 + lane) * 4) = make_float4(sum[j][0], sum[j][1], sum[j][2], sum[j][3]);
-                if (warp == 0 && g8 == 0)
-                    *reinterpret_cast<float4 *>(o_part + S::kTilesD * 128 + 4 * t4) = make_float4(M[0], L[0], M[1], L[1]);
+            for (int e = 0; e < 2; ++e) {
+                const int h = nt * 8 + 2 * t4 + e;
+                if (h >= heads_here) continue;
+                const float inv = L[e] == 0.f ? 0.f : 1.f / L[e];
+#pragma unroll
+                for (int j = 0; j < S::kOwn; ++j) {
+                    const int i = warp * S::kOwn + j;
+                    const int d0 = CODES ? 16 * i + 2 * g8 : 16 * i + g8, d1 = CODES ? d0 + 1 : d0 + 8;
+                    if (whole) {
+                        store_out(p, out_at + h * D + d0, sum[j][e] * inv);
+                        store_out(p, out_at + h * D + d1, sum[j][2 + e] * inv);
+                    } else {
+                        slot[h * D + d0] = sum[j][e];
+                        slot[h * D + d1] = sum[j][2 + e];
+                    }
+                }
+                if (warp == 0 && g8 == 0) {
+                    if (!whole) *(reinterpret_cast<float2 *>(slot + 8 * NT * D) + h) = make_float2(M[e], L[e]);
+                    else if (p.lse) p.lse[lse_at + h] = L[e] == 0.f ? -INFINITY : (M[e] + log2f(L[e])) * kLn2;
+                }
             }
             __syncthreads();
         }
-        if (whole) return;
-        // ---- the CTAs of this (sequence, head): the one that finishes last joins the pieces, in order ----
-        const int c_lo = (int)(((item_lo + 1ll) * n_ctas - 1) / total), c_hi = (int)(((long long)item_hi * n_ctas - 1) / total);
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-            const int last = atomicAdd(&p.tickets[c_lo], 1u) == (unsigned)(c_hi - c_lo);
-            if (last) p.tickets[c_lo] = 0u;
-            sh.is_last = last;
-        }
-        __syncthreads();
-        if (!sh.is_last) return;
-        __threadfence();
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            auto piece = [&](int c) {   // the first piece lies in its CTA's slot 1, the others in slot 0
-                return p.part + (size_t)(2 * c + (c == c_lo ? 1 : 0)) * S::kSlotFloats + nt * (S::kTilesD * 128 + 16);
-            };
-            float M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f};
-            for (int c = c_lo + g8; c <= c_hi; c += 8) {
-                const float4 ml = __ldcg(reinterpret_cast<const float4 *>(piece(c) + S::kTilesD * 128 + 4 * t4));
-                M[0] = fmaxf(M[0], ml.x); M[1] = fmaxf(M[1], ml.z);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                M[e] = fmaxf(M[e], __shfl_xor_sync(0xffffffffu, M[e], 4));
-                M[e] = fmaxf(M[e], __shfl_xor_sync(0xffffffffu, M[e], 8));
-                M[e] = fmaxf(M[e], __shfl_xor_sync(0xffffffffu, M[e], 16));
-            }
-            const float ref0 = M[0] == -INFINITY ? 0.f : M[0], ref1 = M[1] == -INFINITY ? 0.f : M[1];
-            float sum[S::kOwn][4];
-#pragma unroll
-            for (int j = 0; j < S::kOwn; ++j) sum[j][0] = sum[j][1] = sum[j][2] = sum[j][3] = 0.f;
-#pragma unroll 4
-            for (int c = c_lo; c <= c_hi; ++c) {
-                const float *pc = piece(c);
-                const float4 ml = __ldcg(reinterpret_cast<const float4 *>(pc + S::kTilesD * 128 + 4 * t4));
-                const float w0 = exp2f(ml.x - ref0), w1 = exp2f(ml.z - ref1);
-                L[0] = fmaf(w0, ml.y, L[0]); L[1] = fmaf(w1, ml.w, L[1]);
-#pragma unroll
-                for (int j = 0; j < S::kOwn; ++j) {
-                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(pc + ((warp * S::kOwn + j) * 32 + lane) * 4));
-                    sum[j][0] = fmaf(w0, v.x, sum[j][0]); sum[j][1] = fmaf(w1, v.y, sum[j][1]);
-                    sum[j][2] = fmaf(w0, v.z, sum[j][2]); sum[j][3] = fmaf(w1, v.w, sum[j][3]);
-                }
-            }
-            write_head_tiles(nt, sum, M, L);
+        if (!whole && tid == 0) {
+            auto &s = sh.split[first == item_lo ? 1 : 0];
+            s.c_lo = (int)(((item_lo + 1ll) * n_ctas - 1) / total);      // the CTAs that have a piece of it
+            s.c_hi = (int)(((long long)item_hi * n_ctas - 1) / total);
+            s.q_head = q_head;
+            s.heads_here = heads_here;
+            s.b = now.b;
         }
     };
 
-    begin_piece();
-    for (int it = 0, stage = 0; it < n; ++it) {
+    for (int stage = 0; now.index < t1;) {
         copy_wait<S::kStages - 2>();
         __syncwarp();
         const int refill = stage == 0 ? S::kStages - 1 : stage - 1;   // the stage that the step before this one used
-        if (asked < n) {
+        if (ahead.index < t1) {
             request(refill);
-            ++asked;
             step<TILE>(p, ahead, heads);
-            if (asked < n) find_pages();
+            if (ahead.index < t1) {
+                find_pages();
+                if (ahead.tile == 0) prefetch_queries();
+            }
         }
         copy_commit();
         products(stage);
         __syncwarp();
-        const bool ends = it + 1 == n || now.tile + 1 == now.r.tiles;
-        if (ends) end_piece(t0 + it);
-        if (it + 1 < n) {
-            step<TILE>(p, now, heads);
-            if (ends) { piece_first = it + 1; begin_piece(); }
+        const bool ends = now.tile + 1 == now.r.tiles || now.index + 1 == t1;
+        if (ends) end_piece();
+        step<TILE>(p, now, heads);
+        if (ends && now.index < t1) {
+            piece_first = now.index;
+            load_queries();
+            begin_piece();
         }
         stage = stage + 1 == S::kStages ? 0 : stage + 1;
     }
     copy_wait<0>();
+
+    // ---- (sequence, head)s that several CTAs share: whoever finishes last joins the pieces, in order.  This waits until the
+    //      CTA's own list is done, so that its copies never stand still for another's results ----
+    __threadfence();
+    __syncthreads();
+    if (sh.split[0].c_lo < 0 && sh.split[1].c_lo < 0) return;
+    if (tid < 2 && sh.split[tid].c_lo >= 0) {
+        auto &s = sh.split[tid];
+        const int pieces = s.c_hi - s.c_lo + 1, group = pieces <= kMaxJoin ? 0 : (cta - s.c_lo) / kJoinGroup;
+        const int g_lo = s.c_lo + group * kJoinGroup;
+        const int expected = pieces <= kMaxJoin ? pieces : min(kJoinGroup, s.c_hi - g_lo + 1);
+        // tickets: [0, max) for an item's first (or only) group, [max, 2 max) for its later ones (their first CTA may start another
+        // item's first group), [2 max, 3 max) for the groups' results
+        uint32_t *ticket = p.tickets + (group ? kPagedMaxCtas : 0) + g_lo;
+        s.last = atomicAdd(ticket, 1u) == (unsigned)(expected - 1);
+        if (s.last) *ticket = 0u;
+    }
+    __syncthreads();
+    // The rows to be joined come into the ring's memory, all of them requested at once (a loop of copies and a loop of sums: this
+    // code runs once, so what it costs is fetching it and one trip to memory).
+    float2 *ml = reinterpret_cast<float2 *>(comb);                       // [pieces][8 NT]
+    float *wgt = reinterpret_cast<float *>(ml + kMaxJoin * 8 * NT);      // [8 NT][kMaxJoin]
+    float2 *tot = reinterpret_cast<float2 *>(wgt + kMaxJoin * 8 * NT);   // [8 NT]: M, L
+    const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(smem), ml0 = (uint32_t)__cvta_generic_to_shared(ml);
+#pragma unroll 1
+    for (int x = 0; x < 2; ++x) {
+        const int c_lo = sh.split[x].c_lo, c_hi = sh.split[x].c_hi, pieces = c_hi - c_lo + 1;
+        if (c_lo < 0 || !sh.split[x].last) continue;
+        const int q_head = sh.split[x].q_head, cols = sh.split[x].heads_here * (D / 4), b = sh.split[x].b;
+        const bool grouped = pieces > kMaxJoin;
+        int c0 = grouped ? c_lo + (cta - c_lo) / kJoinGroup * kJoinGroup : c_lo, apart = 1;   // CTAs c0, c0 + apart, ...
+        int n = grouped ? min(kJoinGroup, c_hi - c0 + 1) : pieces;
+#pragma unroll 1
+        for (bool final = !grouped;;) {
+            __threadfence();
+            auto place = [&](int i) {   // the first piece of a (sequence, head) lies in its CTA's slot 1, the others in slot 0
+                const int c = c0 + i * apart;
+                return p.part + (size_t)(2 * c + (c == c_lo ? 1 : 0)) * S::kSlotFloats;
+            };
+            for (int i = tid; i < n * 4 * NT; i += kWarps * 32)   // 16 bytes: two heads' words
+                copy16(ml0 + i * 16, place(i / (4 * NT)) + 8 * NT * D + 4 * (i % (4 * NT)));
+            copy_commit();
+            const int fit = kWarps * S::kStages * S::kStage / (cols * 16);   // pieces that the ring holds at a time (10 at least)
+            for (int lo = 0; lo < n; lo += fit) {
+                const int hi = min(lo + fit, n);
+                for (int col = tid; col < cols; col += kWarps * 32)
+                    for (int i = lo; i < hi; ++i) copy16(ring0 + ((i - lo) * cols + col) * 16, place(i) + 4 * col);
+                copy_commit();
+                if (lo == 0) {
+                    copy_wait<1>();
+                    __syncthreads();
+                    for (int h = warp; h < 8 * NT; h += kWarps) {   // rows beyond the heads in use weigh what happens to be there
+                        const float2 u = lane < n ? ml[lane * 8 * NT + h] : make_float2(-INFINITY, 0.f);
+                        const float2 v = lane + 32 < n ? ml[(lane + 32) * 8 * NT + h] : make_float2(-INFINITY, 0.f);
+                        const float M = warp_max(fmaxf(u.x, v.x));
+                        const float ref = M == -INFINITY ? 0.f : M;
+                        const float wu = exp2f(u.x - ref), wv = exp2f(v.x - ref);
+                        if (lane < n) wgt[h * kMaxJoin + lane] = wu;
+                        if (lane + 32 < n) wgt[h * kMaxJoin + lane + 32] = wv;
+                        const float L = warp_sum(fmaf(wu, u.y, wv * v.y));
+                        if (lane == 0) tot[h] = make_float2(M, L);
+                    }
+                    __syncthreads();
+                }
+                copy_wait<0>();
+                for (int col = tid; col < cols; col += kWarps * 32) {   // every thread reads what it copied itself
+                    const int h = col / (D / 4);
+                    const float4 *rows = reinterpret_cast<const float4 *>(smem);
+                    float4 *slot0 = reinterpret_cast<float4 *>(place(0)) + col;
+                    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (lo > 0) sum = *slot0;   // what the pieces before these gave
+                    for (int i = lo; i < hi; ++i) {
+                        const float w = wgt[h * kMaxJoin + i];
+                        const float4 v = rows[(i - lo) * cols + col];
+                        sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
+                    }
+                    const float2 ML = tot[h];
+                    if (!final || hi < n) {
+                        *slot0 = sum;   // this thread alone read that place, and has
+                        if (hi == n && col % (D / 4) == 0) *(reinterpret_cast<float2 *>(place(0) + 8 * NT * D) + h) = ML;
+                        continue;
+                    }
+                    const float inv = ML.y == 0.f ? 0.f : 1.f / ML.y;
+                    const long long at = b * p.out_stride + (long long)q_head * D + 4 * col;
+                    if (p.type == NNC_F32) *reinterpret_cast<float4 *>(p.out + at * 4) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+                    else if (p.type == NNC_BF16)
+                        *reinterpret_cast<uint2 *>(p.out + at * 2) = make_uint2(pack_bf16x2(sum.x * inv, sum.y * inv), pack_bf16x2(sum.z * inv, sum.w * inv));
+                    else {
+                        const __half2 lo2 = __floats2half2_rn(sum.x * inv, sum.y * inv), hi2 = __floats2half2_rn(sum.z * inv, sum.w * inv);
+                        *reinterpret_cast<uint2 *>(p.out + at * 2) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo2), *reinterpret_cast<const uint32_t *>(&hi2));
+                    }
+                    if (p.lse && col % (D / 4) == 0)
+                        p.lse[(long long)b * (p.c.n_kv * p.group) + q_head + h] = ML.y == 0.f ? -INFINITY : (ML.x + log2f(ML.y)) * kLn2;
+                }
+            }
+            __syncthreads();   // what is copied next goes where these weights and rows are
+            if (final) break;
+            __threadfence();
+            __syncthreads();
+            const int groups = (pieces + kJoinGroup - 1) / kJoinGroup;
+            if (tid == 0) {
+                uint32_t *ticket = p.tickets + 2 * kPagedMaxCtas + c_lo;
+                const int last = atomicAdd(ticket, 1u) == (unsigned)(groups - 1);
+                if (last) *ticket = 0u;
+                sh.split[x].last = last;
+            }
+            __syncthreads();
+            if (!sh.split[x].last) break;
+            c0 = c_lo; apart = kJoinGroup; n = groups; final = true;
+        }
+    }
 }
 
 template <int D, int NT, int KV, int QT, int PT>
@@ -658,7 +853,7 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     cudaError_t e = ensure_dynamic_smem(kern, S::kSmem, &raised);
     if (e != cudaSuccess) return e;
     const long long most = ((long long)p.c.pages_per_seq << p.c.page_shift);
-    const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile) * p.batch * p.c.n_kv * p.chunks;   // the longest list the table allows
+    const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile + 1) * p.batch * p.c.n_kv * p.chunks;   // the longest list the table allows
     if (tiles > 0x7fffffffll) return cudaErrorInvalidValue;
     long long ctas = 2ll * lc.sm_count;
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
@@ -677,10 +872,10 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
 // 16-bit results: queries as one exact term, probabilities as two; fp32 results: as many terms as fp32 has bits for
 template <int D, int NT>
 cudaError_t launch_typed(const LaunchCtx &lc, const PagedAttnParams &p, int kv) {
-    const bool f32 = p.type == NNC_F32;
+    const bool f32 = p.type == NNC_F32, bf16_out = p.type == NNC_BF16;
     if (kv == NNC_BF16) return f32 ? launch_one<D, NT, NNC_BF16, 3, 3>(lc, p) : launch_one<D, NT, NNC_BF16, 1, 2>(lc, p);
     if (kv == NNC_F16) return f32 ? launch_one<D, NT, NNC_F16, 2, 2>(lc, p) : launch_one<D, NT, NNC_F16, 1, 2>(lc, p);
-    return f32 ? launch_one<D, NT, NNC_E4M3, 2, 2>(lc, p) : launch_one<D, NT, NNC_E4M3, 1, 2>(lc, p);
+    return f32 ? launch_one<D, NT, NNC_E4M3, 2, 2>(lc, p) : bf16_out ? launch_one<D, NT, NNC_E4M3, 1, 1>(lc, p) : launch_one<D, NT, NNC_E4M3, 1, 2>(lc, p);
 }
 
 }  // namespace

@@ -129,7 +129,7 @@ cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, i
 // write: rows go from k, v into the cache; otherwise from the cache to k, v (`type` is theirs either way)
 cudaError_t launch_kv_paged(const LaunchCtx &lc, const nnc_paged_kv &cache, bool write, void *k, void *v, int type, int n_tokens,
                             int64_t row_stride, int64_t head_stride, const int32_t *pos, const int32_t *seq);
-constexpr int kPagedMaxCtas = NNC_ATTN_PAGED_TICKET_BYTES / 4;   // one ticket word per CTA of the attention's grid
+constexpr int kPagedMaxCtas = NNC_ATTN_PAGED_TICKET_BYTES / 12;   // three ticket words per CTA of the attention's grid
 cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, void *out, float *lse,
                               int type, int batch, int n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int window,
                               void *scratch, size_t scratch_bytes);

@@ -340,8 +340,9 @@ def attend64(q, k, v, scale, window):
 def _check_attention(out, lse, q, held, lens, scale, window, kv):
     """fp32 part, with u = 2^-22 for a product-and-sum step of the tensor cores:
     scores: D / 16 steps of up to three terms each, the scalings (8 more), relative to sum |q k|; twice that in the weights
-    (numerator and sum).  Weights: 2^-16 for two bf16 terms (with 16-bit results of a bf16 cache), within u otherwise.  Sums:
-    a step per 16 positions of a warp's share, joins of warps and of CTAs, exp2 (32 more)."""
+    (numerator and sum).  Weights: 2^-16 for two bf16 terms (16-bit results of a bf16 cache); for 16-bit results of codes one
+    fp16 value (2^-11) with bf16 results and six more bits of a second one (2^-16) with fp16; within u otherwise.  Sums: a
+    step per 16 positions of a warp's share, joins of warps and of CTAs, exp2 (32 more)."""
     k, v = held
     d = q.shape[-1]
     for b, n in enumerate(lens):
@@ -352,7 +353,7 @@ def _check_attention(out, lse, q, held, lens, scale, window, kv):
         u = 2.0 ** -22
         score = u * (3 * d / 16 + 8) * reach
         sums = u * (n / 16 + 32)
-        weights = 2.0 ** -16 if kv is BF16 and out.dtype is not F32 else u
+        weights = {(BF16, BF16): 2.0 ** -16, (E4M3, BF16): 2.0 ** -11, (E4M3, F16): 2.0 ** -16}.get((kv, out.dtype), u)
         tol = torch.finfo(out.dtype).eps / 2 * want.abs() + (weights + sums + 2 * score)[..., None] * size
         tol += torch.finfo(F16).smallest_normal * 2.0 ** -11 if out.dtype is F16 else 0
         bad = (out[b].double() - want).abs() > tol
