@@ -44,7 +44,7 @@ struct PagedAttnParams {
     uint32_t *tickets;
     size_t part_floats;
     long long q_stride, out_stride;   // elements
-    int type, batch, group, chunks, window;   // chunks: groups of NT * 8 query heads per KV head
+    int batch, group, chunks, window;   // chunks: groups of NT * 8 query heads per KV head
     float scale_log2;
 };
 
@@ -148,10 +148,8 @@ struct Reach {
     // places of a (sequence, head) in the list: its tiles and one for what it costs to begin and to end
     __device__ __forceinline__ int places() const { return tiles ? tiles + 1 : 0; }
 };
-template <int TILE> __device__ __forceinline__ Reach reach_of(const PagedAttnParams &p, int b) {
-    const int most = p.c.pages_per_seq << p.c.page_shift;
-    int len = p.lens[b];
-    len = max(0, min(len, most));
+template <int TILE> __device__ __forceinline__ Reach reach_of(const PagedAttnParams &p, int len) {
+    len = max(0, min(len, p.c.pages_per_seq << p.c.page_shift));
     Reach r;
     r.end = len;
     r.start = (p.window > 0 && len > p.window) ? len - p.window : 0;
@@ -162,25 +160,37 @@ template <int TILE> __device__ __forceinline__ Reach reach_of(const PagedAttnPar
 // a tile, and its place in the list
 struct Place {
     Reach r;
-    int b, hh, tile;   // hh: KV head * chunks + chunk of its query heads
+    int b, head, chunk, tile;   // head: KV head; chunk: which 8 NT of its query heads
     int index;
 };
-template <int TILE> __device__ __forceinline__ void step(const PagedAttnParams &p, Place &at, int heads) {
+template <int TILE> __device__ __forceinline__ void step(const PagedAttnParams &p, Place &at) {
     ++at.index;
     if (++at.tile < at.r.tiles) return;
     ++at.index;
     at.tile = 0;
-    if (++at.hh < heads) return;
-    at.hh = 0;
+    if (++at.chunk < p.chunks) return;
+    at.chunk = 0;
+    if (++at.head < p.c.n_kv) return;
+    at.head = 0;
     do {
         if (++at.b >= p.batch) { at.r = Reach{0, 0, 0}; return; }   // past the list's end: nothing is taken from here
-        at.r = reach_of<TILE>(p, at.b);
+        at.r = reach_of<TILE>(p, p.lens[at.b]);
     } while (at.r.tiles == 0);
 }
 
-__device__ __forceinline__ void store_out(const PagedAttnParams &p, long long at, float v) {
-    if (p.type == NNC_F32) reinterpret_cast<float *>(p.out)[at] = v;
-    else if (p.type == NNC_BF16) reinterpret_cast<uint16_t *>(p.out)[at] = f32_to_bf16_bits(v);
+// Counts a CTA that has written its piece, after a barrier of its threads; true for the last of n, which leaves the word at
+// zero.  Release and acquire of this one thread, with the barriers around it, order the CTA's stores and loads.
+__device__ __forceinline__ bool take_ticket(uint32_t *ticket, int n) {
+    uint32_t before;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(ticket) : "memory");
+    if (before != (uint32_t)(n - 1)) return false;
+    *ticket = 0u;
+    return true;
+}
+
+template <int TYPE> __device__ __forceinline__ void store_out(const PagedAttnParams &p, long long at, float v) {
+    if constexpr (TYPE == NNC_F32) reinterpret_cast<float *>(p.out)[at] = v;
+    else if constexpr (TYPE == NNC_BF16) reinterpret_cast<uint16_t *>(p.out)[at] = f32_to_bf16_bits(v);
     else reinterpret_cast<__half *>(p.out)[at] = __float2half_rn(v);
 }
 
@@ -190,6 +200,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
     typedef Shape<D, NT, KV> S;
     constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3, kFresh = QT > 1;
     constexpr int PB = S::kPB, TILE = S::kTile, ROW = S::kRow;
+    // the queries' and the results' type goes with the number of terms (launch_typed)
+    constexpr int TYPE = QT > 1 ? NNC_F32 : BF || (CODES && PT == 1) ? NNC_BF16 : NNC_F16;
     // fp16 probabilities are scaled by 2^14, so that small ones keep their bits (the sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 14.f;
     extern __shared__ __align__(128) char smem[];
@@ -197,13 +209,16 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     const int g8 = lane >> 2, t4 = lane & 3;
-    const int heads = p.c.n_kv * p.chunks;
-
-    // ---- the list: how many tiles there are, and where this CTA's share begins ----
+    // ---- the list: how many places there are, and where this CTA's share begins ----
+    const int heads = p.c.n_kv * p.chunks, most = p.c.pages_per_seq << p.c.page_shift;
     const int per = (p.batch + kWarps * 32 - 1) / (kWarps * 32);
     const int b_lo = min(tid * per, p.batch), b_hi = min(b_lo + per, p.batch);
-    int mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += reach_of<TILE>(p, b).places();
+    int mine = 0, odd = 0;   // odd: an empty sequence, or a length that does not fit
+    for (int b = b_lo; b < b_hi; ++b) {
+        const int len = p.lens[b];
+        odd |= len <= 0 || len > most;
+        mine += reach_of<TILE>(p, len).places();
+    }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -211,48 +226,49 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         if (lane >= o) incl += x;
     }
     if (lane == 31) sh.sums[warp] = incl;
-    __syncthreads();
+    if (__syncthreads_or(odd)) {   // zeros for sequences with nothing to attend to; lengths that do not fit are reported
+        for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+            const int len = p.lens[b], n_q = p.c.n_kv * p.group;
+            if (len > most && tid == 0) paged_complain(p.c);
+            if (len > 0) continue;
+            for (int i = tid; i < n_q * D; i += kWarps * 32) store_out<TYPE>(p, b * p.out_stride + i, 0.f);
+            if (p.lse) for (int i = tid; i < n_q; i += kWarps * 32) p.lse[(long long)b * n_q + i] = -INFINITY;
+        }
+    }
     int before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sh.sums[w]; all += sh.sums[w]; }
-    const int excl = before + incl - mine;
-    const long long total = (long long)all * heads;   // places; the host bounds them by 2^31
-    const int n_ctas = (int)min((long long)gridDim.x, total);
+    const int total = all * heads;                             // places; the host bounds them by 2^30
+    const int share = (total + gridDim.x - 1) / gridDim.x;     // of every CTA but the last ones
     const int cta = blockIdx.x;
-
-    // sequences with nothing to attend to: zeros; and lengths that do not fit are reported
-    for (int b = cta; b < p.batch; b += gridDim.x) {
-        if (tid == 0 && p.lens[b] > (p.c.pages_per_seq << p.c.page_shift)) paged_complain(p.c);
-        if (reach_of<TILE>(p, b).tiles) continue;
-        const int n_q = p.c.n_kv * p.group;
-        for (int i = tid; i < n_q * D; i += kWarps * 32) store_out(p, b * p.out_stride + i, 0.f);
-        if (p.lse) for (int i = tid; i < n_q; i += kWarps * 32) p.lse[(long long)b * n_q + i] = -INFINITY;
-    }
-    if (cta >= n_ctas) return;
-    const int t0 = (int)(total * cta / n_ctas), t1 = (int)(total * (cta + 1) / n_ctas);
-
-    if (mine > 0) {
-        const long long lo = (long long)excl * heads, hi = (long long)(excl + mine) * heads;
-        if (t0 >= lo && t0 < hi) {
-            long long rest = t0 - lo;
-            int b = b_lo;
+    if ((long long)cta * share >= total) return;
+    const int t0 = cta * share, t1 = min(t0 + share, total);
+    {
+        const int lo = (before + incl - mine) * heads;
+        if (t0 >= lo && t0 - lo < mine * heads) {
+            int rest = t0 - lo, b = b_lo;
             for (; b < b_hi; ++b) {
-                const long long n = (long long)reach_of<TILE>(p, b).places() * heads;
+                const int n = reach_of<TILE>(p, p.lens[b]).places() * heads;
                 if (rest < n) break;
                 rest -= n;
             }
             sh.first_b = b;
-            sh.first_rest = (int)rest;
+            sh.first_rest = rest;
         }
     }
+    if (tid < 2) sh.split[tid].c_lo = -1;
     __syncthreads();
     Place ahead;   // where the copies are
     ahead.b = sh.first_b;
-    ahead.r = reach_of<TILE>(p, ahead.b);
-    ahead.hh = sh.first_rest / ahead.r.places();
-    ahead.tile = sh.first_rest - ahead.hh * ahead.r.places();
+    ahead.r = reach_of<TILE>(p, p.lens[ahead.b]);
+    {
+        const int at = sh.first_rest / ahead.r.places();
+        ahead.tile = sh.first_rest - at * ahead.r.places();
+        ahead.head = at / p.chunks;
+        ahead.chunk = at - ahead.head * p.chunks;
+    }
     ahead.index = t0;
-    if (ahead.tile == ahead.r.tiles) { --ahead.index; --ahead.tile; step<TILE>(p, ahead, heads); }   // the place after its tiles
+    if (ahead.tile == ahead.r.tiles) { --ahead.index; --ahead.tile; step<TILE>(p, ahead); }   // the place after its tiles
     if (ahead.index >= t1) return;
     Place now = ahead;   // where the products are
 
@@ -273,7 +289,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
     const int r0 = lane / kPieces, c0 = lane % kPieces;   // this lane's row and piece in the first step of 16 rows
     auto request = [&](int stage) {
         const int p0 = (ahead.r.start & ~15) + ahead.tile * TILE + warp * PB;
-        const int head = ahead.hh / p.chunks;
         const uint32_t base = ring + stage * S::kStage;
         present &= ~(((1u << S::kSub) - 1u) << (stage * S::kSub));
 #pragma unroll
@@ -281,7 +296,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
             const int pb = p0 + 16 * u;
             if (pb >= ahead.r.end) break;
             const bool there = (unsigned)pages[u] < (unsigned)p.c.n_pages;
-            const long long row = there ? paged_row(p.c, pages[u], head, pb & ((1 << p.c.page_shift) - 1)) : 0;
+            const long long row = there ? paged_row(p.c, pages[u], ahead.head, pb & ((1 << p.c.page_shift) - 1)) : 0;
             const char *ks = p.c.k + row * ROW + lane * 16, *vs = p.c.v + row * ROW + lane * 16;   // 16 rows are one run of bytes
             if (there && pb >= ahead.r.start && pb + 16 <= ahead.r.end) {
 #pragma unroll
@@ -317,57 +332,48 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
 
     // Queries of the (sequence, head) at `now`: lane (g8, t4) holds head g8's elements of contraction columns 2 t4, 2 t4 + 1, 2 t4 + 8,
     // 2 t4 + 9 of every step of 16; with codes, a key's four neighbouring codes 4 t4 .. 4 t4 + 3 stand in those columns.
-    // All of them are requested before any is used.
-    uint32_t raw[NT][D / 16][4];
+    // They are all requested before any is used, and wait as they are in the fragments' registers.
     auto load_queries = [&]() {
-        const int kv_head = now.hh / p.chunks, chunk = now.hh - kv_head * p.chunks;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int g = chunk * (8 * NT) + nt * 8 + g8;
-            const long long at = now.b * p.q_stride + (long long)(kv_head * p.group + (g < p.group ? g : 0)) * D + (CODES ? 4 : 2) * t4;
+            const int g = now.chunk * (8 * NT) + nt * 8 + g8;
+            const long long at = now.b * p.q_stride + (long long)(now.head * p.group + (g < p.group ? g : 0)) * D + (CODES ? 4 : 2) * t4;
             constexpr int kApart = CODES ? 2 : 8;
-            if (p.type == NNC_F32) {
-                const float *src = reinterpret_cast<const float *>(p.q) + at;
 #pragma unroll
-                for (int s = 0; s < D / 16; ++s) {
-                    const uint2 a = *reinterpret_cast<const uint2 *>(src + 16 * s), b = *reinterpret_cast<const uint2 *>(src + 16 * s + kApart);
-                    raw[nt][s][0] = a.x; raw[nt][s][1] = a.y; raw[nt][s][2] = b.x; raw[nt][s][3] = b.y;
-                }
-            } else {
-                const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q) + at;
-#pragma unroll
-                for (int s = 0; s < D / 16; ++s) {
-                    raw[nt][s][0] = *reinterpret_cast<const uint32_t *>(src + 16 * s);
-                    raw[nt][s][1] = *reinterpret_cast<const uint32_t *>(src + 16 * s + kApart);
+            for (int s = 0; s < D / 16; ++s) {
+                if constexpr (TYPE == NNC_F32) {
+                    const float *src = reinterpret_cast<const float *>(p.q) + at + 16 * s;
+                    const uint2 a = *reinterpret_cast<const uint2 *>(src), b = *reinterpret_cast<const uint2 *>(src + kApart);
+                    qf[nt][0][s][0] = a.x; qf[nt][0][s][1] = a.y; qf[nt][QT - 1][s][0] = b.x; qf[nt][QT - 1][s][1] = b.y;
+                } else {
+                    const uint16_t *src = reinterpret_cast<const uint16_t *>(p.q) + at + 16 * s;
+                    qf[nt][0][s][0] = *reinterpret_cast<const uint32_t *>(src);
+                    qf[nt][0][s][1] = *reinterpret_cast<const uint32_t *>(src + kApart);
                 }
             }
         }
     };
     auto begin_piece = [&]() {
-        const int chunk = now.hh % p.chunks;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const bool there = chunk * (8 * NT) + nt * 8 + g8 < p.group;
+            const bool there = now.chunk * (8 * NT) + nt * 8 + g8 < p.group;
             float f[D / 16][4];
-            if (p.type == NNC_F32) {
 #pragma unroll
-                for (int s = 0; s < D / 16; ++s)
+            for (int s = 0; s < D / 16; ++s)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) f[s][e] = __uint_as_float(raw[nt][s][e]);
-            } else if (p.type == NNC_BF16) {
-#pragma unroll
-                for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) { f[s][2 * e] = bf16_lo(raw[nt][s][e]); f[s][2 * e + 1] = bf16_hi(raw[nt][s][e]); }
-            } else {
-#pragma unroll
-                for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const __half2 h = *reinterpret_cast<const __half2 *>(&raw[nt][s][e]);
-                        f[s][2 * e] = __low2float(h); f[s][2 * e + 1] = __high2float(h);
+                for (int e = 0; e < 2; ++e) {
+                    if constexpr (TYPE == NNC_F32) {
+                        f[s][e] = __uint_as_float(qf[nt][0][s][e]);
+                        f[s][2 + e] = __uint_as_float(qf[nt][QT - 1][s][e]);
+                    } else if constexpr (TYPE == NNC_BF16) {
+                        f[s][2 * e] = bf16_lo(qf[nt][0][s][e]);
+                        f[s][2 * e + 1] = bf16_hi(qf[nt][0][s][e]);
+                    } else {
+                        const __half2 h = *reinterpret_cast<const __half2 *>(&qf[nt][0][s][e]);
+                        f[s][2 * e] = __low2float(h);
+                        f[s][2 * e + 1] = __high2float(h);
                     }
-            }
+                }
             float top = 0.f;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s)
@@ -408,26 +414,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
 
     // asks L2 for the queries of the (sequence, head) that the copies have reached
     auto prefetch_queries = [&]() {
-        const int kv_head = ahead.hh / p.chunks, chunk = ahead.hh - kv_head * p.chunks;
-        const int size = p.type == NNC_F32 ? 4 : 2, at = (warp * 32 + lane) * 128;   // a line each
-        const int q_head = kv_head * p.group + chunk * (8 * NT), heads_here = min(8 * NT, p.group - chunk * (8 * NT));
+        constexpr int size = TYPE == NNC_F32 ? 4 : 2;
+        const int at = (warp * 32 + lane) * 128;   // a line each
+        const int q_head = ahead.head * p.group + ahead.chunk * (8 * NT), heads_here = min(8 * NT, p.group - ahead.chunk * (8 * NT));
         if (at < heads_here * D * size)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(p.q + (ahead.b * p.q_stride + (long long)q_head * D) * size + at));
     };
-
-    if (tid < 2) sh.split[tid].c_lo = -1;
-    find_pages();
-    load_queries();   // before the rows: behind them in the memory system they would come last
-#pragma unroll
-    for (int st = 0; st < S::kStages - 1; ++st) {
-        if (ahead.index < t1) {
-            request(st);
-            step<TILE>(p, ahead, heads);
-            if (ahead.index < t1) find_pages();
-        }
-        copy_commit();
-    }
-    begin_piece();
 
     // lane's row and piece in the four 8x8 matrices of an ldmatrix: K (rows = positions) and V (transposed)
     const int lr = lane & 7, lm = lane >> 3;
@@ -621,8 +613,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         const int item_lo = now.index - now.tile, item_hi = item_lo + now.r.tiles;   // places of this (sequence, head)'s tiles
         const int first = piece_first;
         const bool whole = first == item_lo && now.index + 1 == item_hi;
-        const int kv_head = now.hh / p.chunks, chunk = now.hh - kv_head * p.chunks;
-        const int q_head = kv_head * p.group + chunk * (8 * NT), heads_here = min(8 * NT, p.group - chunk * (8 * NT));
+        const int q_head = now.head * p.group + now.chunk * (8 * NT), heads_here = min(8 * NT, p.group - now.chunk * (8 * NT));
         const long long out_at = now.b * p.out_stride + (long long)q_head * D, lse_at = (long long)now.b * (p.c.n_kv * p.group) + q_head;
         // partial results: slot 0 of a CTA for a piece that continues an earlier CTA's, slot 1 for one that starts here
         float *slot = p.part + (size_t)(2 * cta + (first == item_lo ? 1 : 0)) * S::kSlotFloats;
@@ -682,8 +673,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
                     const int i = warp * S::kOwn + j;
                     const int d0 = CODES ? 16 * i + 2 * g8 : 16 * i + g8, d1 = CODES ? d0 + 1 : d0 + 8;
                     if (whole) {
-                        store_out(p, out_at + h * D + d0, sum[j][e] * inv);
-                        store_out(p, out_at + h * D + d1, sum[j][2 + e] * inv);
+                        store_out<TYPE>(p, out_at + h * D + d0, sum[j][e] * inv);
+                        store_out<TYPE>(p, out_at + h * D + d1, sum[j][2 + e] * inv);
                     } else {
                         slot[h * D + d0] = sum[j][e];
                         slot[h * D + d1] = sum[j][2 + e];
@@ -698,44 +689,48 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         }
         if (!whole && tid == 0) {
             auto &s = sh.split[first == item_lo ? 1 : 0];
-            s.c_lo = (int)(((item_lo + 1ll) * n_ctas - 1) / total);      // the CTAs that have a piece of it
-            s.c_hi = (int)(((long long)item_hi * n_ctas - 1) / total);
+            s.c_lo = item_lo / share;          // the CTAs that have a piece of it
+            s.c_hi = (item_hi - 1) / share;
             s.q_head = q_head;
             s.heads_here = heads_here;
             s.b = now.b;
         }
     };
 
-    for (int stage = 0; now.index < t1;) {
-        copy_wait<S::kStages - 2>();
-        __syncwarp();
-        const int refill = stage == 0 ? S::kStages - 1 : stage - 1;   // the stage that the step before this one used
-        if (ahead.index < t1) {
-            request(refill);
-            step<TILE>(p, ahead, heads);
+    // One loop for filling the ring and for the steady state, so that its code exists once: a launch fetches every instruction
+    // that it runs from memory.
+    find_pages();
+    bool begins = true;
+    for (int stage = 0, fill = 0, requests = S::kStages; now.index < t1; requests = 1) {
+        if (begins) load_queries();   // before the rows: behind them in the memory system they would come last
+#pragma unroll 1
+        for (; requests > 0; --requests) {   // the stage that the step before this one used, or at first all of them
             if (ahead.index < t1) {
-                find_pages();
-                if (ahead.tile == 0) prefetch_queries();
+                request(fill);
+                step<TILE>(p, ahead);
+                if (ahead.index < t1) {
+                    find_pages();
+                    if (ahead.tile == 0) prefetch_queries();
+                }
             }
+            copy_commit();
+            fill = fill + 1 == S::kStages ? 0 : fill + 1;
         }
-        copy_commit();
+        if (begins) begin_piece();
+        copy_wait<S::kStages - 1>();
+        __syncwarp();
         products(stage);
         __syncwarp();
-        const bool ends = now.tile + 1 == now.r.tiles || now.index + 1 == t1;
-        if (ends) end_piece();
-        step<TILE>(p, now, heads);
-        if (ends && now.index < t1) {
-            piece_first = now.index;
-            load_queries();
-            begin_piece();
-        }
+        begins = now.tile + 1 == now.r.tiles;
+        if (begins || now.index + 1 == t1) end_piece();
+        step<TILE>(p, now);
+        if (begins) piece_first = now.index;
         stage = stage + 1 == S::kStages ? 0 : stage + 1;
     }
     copy_wait<0>();
 
     // ---- (sequence, head)s that several CTAs share: whoever finishes last joins the pieces, in order.  This waits until the
     //      CTA's own list is done, so that its copies never stand still for another's results ----
-    __threadfence();
     __syncthreads();
     if (sh.split[0].c_lo < 0 && sh.split[1].c_lo < 0) return;
     if (tid < 2 && sh.split[tid].c_lo >= 0) {
@@ -746,8 +741,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         // tickets: [0, max) for an item's first (or only) group, [max, 2 max) for its later ones (their first CTA may start another
         // item's first group), [2 max, 3 max) for the groups' results
         uint32_t *ticket = p.tickets + (group ? kPagedMaxCtas : 0) + g_lo;
-        s.last = atomicAdd(ticket, 1u) == (unsigned)(expected - 1);
-        if (s.last) *ticket = 0u;
+        s.last = take_ticket(ticket, expected);
     }
     __syncthreads();
     // The rows to be joined come into the ring's memory, all of them requested at once (a loop of copies and a loop of sums: this
@@ -766,7 +760,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
         int n = grouped ? min(kJoinGroup, c_hi - c0 + 1) : pieces;
 #pragma unroll 1
         for (bool final = !grouped;;) {
-            __threadfence();
             auto place = [&](int i) {   // the first piece of a (sequence, head) lies in its CTA's slot 1, the others in slot 0
                 const int c = c0 + i * apart;
                 return p.part + (size_t)(2 * c + (c == c_lo ? 1 : 0)) * S::kSlotFloats;
@@ -803,6 +796,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
                     float4 *slot0 = reinterpret_cast<float4 *>(place(0)) + col;
                     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (lo > 0) sum = *slot0;   // what the pieces before these gave
+#pragma unroll 4
                     for (int i = lo; i < hi; ++i) {
                         const float w = wgt[h * kMaxJoin + i];
                         const float4 v = rows[(i - lo) * cols + col];
@@ -816,8 +810,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
                     }
                     const float inv = ML.y == 0.f ? 0.f : 1.f / ML.y;
                     const long long at = b * p.out_stride + (long long)q_head * D + 4 * col;
-                    if (p.type == NNC_F32) *reinterpret_cast<float4 *>(p.out + at * 4) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-                    else if (p.type == NNC_BF16)
+                    if constexpr (TYPE == NNC_F32) *reinterpret_cast<float4 *>(p.out + at * 4) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+                    else if constexpr (TYPE == NNC_BF16)
                         *reinterpret_cast<uint2 *>(p.out + at * 2) = make_uint2(pack_bf16x2(sum.x * inv, sum.y * inv), pack_bf16x2(sum.z * inv, sum.w * inv));
                     else {
                         const __half2 lo2 = __floats2half2_rn(sum.x * inv, sum.y * inv), hi2 = __floats2half2_rn(sum.z * inv, sum.w * inv);
@@ -829,15 +823,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
             }
             __syncthreads();   // what is copied next goes where these weights and rows are
             if (final) break;
-            __threadfence();
-            __syncthreads();
             const int groups = (pieces + kJoinGroup - 1) / kJoinGroup;
-            if (tid == 0) {
-                uint32_t *ticket = p.tickets + 2 * kPagedMaxCtas + c_lo;
-                const int last = atomicAdd(ticket, 1u) == (unsigned)(groups - 1);
-                if (last) *ticket = 0u;
-                sh.split[x].last = last;
-            }
+            if (tid == 0) sh.split[x].last = take_ticket(p.tickets + 2 * kPagedMaxCtas + c_lo, groups);
             __syncthreads();
             if (!sh.split[x].last) break;
             c0 = c_lo; apart = kJoinGroup; n = groups; final = true;
@@ -854,7 +841,7 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     if (e != cudaSuccess) return e;
     const long long most = ((long long)p.c.pages_per_seq << p.c.page_shift);
     const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile + 1) * p.batch * p.c.n_kv * p.chunks;   // the longest list the table allows
-    if (tiles > 0x7fffffffll) return cudaErrorInvalidValue;
+    if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
     long long ctas = 2ll * lc.sm_count;
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
     const long long fit = (long long)(p.part_floats / (2 * S::kSlotFloats));
@@ -871,8 +858,8 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
 
 // 16-bit results: queries as one exact term, probabilities as two; fp32 results: as many terms as fp32 has bits for
 template <int D, int NT>
-cudaError_t launch_typed(const LaunchCtx &lc, const PagedAttnParams &p, int kv) {
-    const bool f32 = p.type == NNC_F32, bf16_out = p.type == NNC_BF16;
+cudaError_t launch_typed(const LaunchCtx &lc, const PagedAttnParams &p, int kv, int type) {
+    const bool f32 = type == NNC_F32, bf16_out = type == NNC_BF16;
     if (kv == NNC_BF16) return f32 ? launch_one<D, NT, NNC_BF16, 3, 3>(lc, p) : launch_one<D, NT, NNC_BF16, 1, 2>(lc, p);
     if (kv == NNC_F16) return f32 ? launch_one<D, NT, NNC_F16, 2, 2>(lc, p) : launch_one<D, NT, NNC_F16, 1, 2>(lc, p);
     return f32 ? launch_one<D, NT, NNC_E4M3, 2, 2>(lc, p) : bf16_out ? launch_one<D, NT, NNC_E4M3, 1, 1>(lc, p) : launch_one<D, NT, NNC_E4M3, 1, 2>(lc, p);
@@ -890,13 +877,13 @@ cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_page
     p.part = (float *)((char *)scratch + NNC_ATTN_PAGED_TICKET_BYTES);
     p.part_floats = (scratch_bytes - NNC_ATTN_PAGED_TICKET_BYTES) / 4;
     p.q_stride = q_stride; p.out_stride = out_stride;
-    p.type = type; p.batch = batch; p.window = window;
+    p.batch = batch; p.window = window;
     p.group = n_q_heads / cache.n_kv_heads;
     p.scale_log2 = scale * 1.4426950408889634f;
     const bool two = p.group > 8;   // one 8-column operand, or two, that share every key and value fragment
     p.chunks = two ? (p.group + 15) / 16 : 1;
-    if (cache.head_dim == 64) return two ? launch_typed<64, 2>(lc, p, cache.type) : launch_typed<64, 1>(lc, p, cache.type);
-    return two ? launch_typed<128, 2>(lc, p, cache.type) : launch_typed<128, 1>(lc, p, cache.type);
+    if (cache.head_dim == 64) return two ? launch_typed<64, 2>(lc, p, cache.type, type) : launch_typed<64, 1>(lc, p, cache.type, type);
+    return two ? launch_typed<128, 2>(lc, p, cache.type, type) : launch_typed<128, 1>(lc, p, cache.type, type);
 }
 
 }  // namespace nnc
