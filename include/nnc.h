@@ -380,7 +380,7 @@ int nnc_op_kv_read_paged(const nnc_paged_kv *cache, void *k, void *v, int32_t ty
  * graphs included).  Results do not depend on scheduling: partial results are joined in a fixed order.  q, out and
  * their strides are multiples of 16 bytes. */
 #define NNC_ATTN_PAGED_SCRATCH_BYTES (16u << 20)
-#define NNC_ATTN_PAGED_TICKET_BYTES 4096
+#define NNC_ATTN_PAGED_TICKET_BYTES 8192
 int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, void *out, float *lse, int32_t type,
                              int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
                              void *scratch, size_t scratch_bytes, void *cuda_stream);

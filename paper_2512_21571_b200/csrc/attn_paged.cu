@@ -32,7 +32,7 @@ constexpr int kWarps = 4;
 constexpr float kLn2 = 0.69314718055994530942f;
 // partial results that one CTA joins: up to kMaxJoin at once, in groups of kJoinGroup first where there are more (one SM reads
 // them at some 100 GB/s, so a long list is cheaper in two rounds)
-constexpr int kMaxJoin = 48, kJoinGroup = 24;
+constexpr int kMaxJoin = 64, kJoinGroup = 24;
 
 struct PagedAttnParams {
     PagedView c;
@@ -48,8 +48,9 @@ struct PagedAttnParams {
     float scale_log2;
 };
 
-template <int D, int NT, int KV>
+template <int D, int NT, int KV, int QT>
 struct Shape {
+    static constexpr int kCtas = NT == 1 && QT == 1 ? 3 : 2;   // resident per SM
     static constexpr int kBytes = KV == NNC_E4M3 ? 1 : 2;
     static constexpr int kRow = D * kBytes;                  // bytes of a row
     static constexpr int kPB = kRow == 256 ? 16 : 32;        // positions of a warp's block
@@ -57,10 +58,12 @@ struct Shape {
     static constexpr int kTile = kWarps * kPB;
     static constexpr int kData = 2 * kPB * kRow;             // K rows, then V rows
     static constexpr int kStage = kData + (KV == NNC_E4M3 ? 2 * kPB : 0);   // then K scales, V scales
-    static constexpr int kStages = kData == 8192 ? 3 : 5;
+    static constexpr int kStages = kCtas == 3 ? (kData == 8192 ? 2 : 4) : kData == 8192 ? 3 : 5;
     static constexpr int kTilesD = D / 16;                   // 16-row tiles of O^T
     static constexpr int kOwn = kTilesD / kWarps;            // tiles that a warp merges
-    static constexpr int kHand = kWarps * 3 * kOwn * 4 * 32 * 4;   // bytes: the pieces that warps hand to one another,
+    static constexpr int kRounds = kCtas == 3 ? kOwn : 1;    // warps hand their tiles to one another in so many rounds,
+    static constexpr int kOnce = kOwn / kRounds;             // so many tiles a warp at once,
+    static constexpr int kHand = kWarps * 3 * kOnce * 4 * 32 * 4;   // in so many bytes,
     static constexpr int kJoin = 8 * NT * kMaxJoin * 12 + 8 * NT * 8;   // or (m, l), weights and sums where results are joined
     static constexpr int kComb = kHand > kJoin ? kHand : kJoin;
     static constexpr int kSmem = kWarps * kStages * kStage + kComb;
@@ -196,8 +199,8 @@ template <int TYPE> __device__ __forceinline__ void store_out(const PagedAttnPar
 
 // QT, PT: terms of the queries and of the probabilities
 template <int D, int NT, int KV, int QT, int PT>
-__global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedAttnParams p) {
-    typedef Shape<D, NT, KV> S;
+__global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn_paged_kernel(const PagedAttnParams p) {
+    typedef Shape<D, NT, KV, QT> S;
     constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3, kFresh = QT > 1;
     constexpr int PB = S::kPB, TILE = S::kTile, ROW = S::kRow;
     // the queries' and the results' type goes with the number of terms (launch_typed)
@@ -607,7 +610,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
     };
 
     // ---- results.  A warp's fragments of O^T tile i: rows d0 (and d1) of two heads ----
-    float (*comb)[3][S::kOwn][32][4] = reinterpret_cast<float (*)[3][S::kOwn][32][4]>(smem + kWarps * S::kStages * S::kStage);
+    float (*comb)[3][S::kOnce][32][4] = reinterpret_cast<float (*)[3][S::kOnce][32][4]>(smem + kWarps * S::kStages * S::kStage);
 
     auto end_piece = [&]() {
         const int item_lo = now.index - now.tile, item_hi = item_lo + now.r.tiles;   // places of this (sequence, head)'s tiles
@@ -628,64 +631,70 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 if (g8 == 0) { sh.ml[warp][2 * t4 + e][0] = m_run[nt][e] == -INFINITY ? -INFINITY : m_run[nt][e] - kLift; sh.ml[warp][2 * t4 + e][1] = l; }
             }
-            float own[S::kOwn][4];
-#pragma unroll
-            for (int i = 0; i < S::kTilesD; ++i) {
-                const int to = i / S::kOwn, j = i % S::kOwn;
-                const float4 v = make_float4(o[nt][i][0], o[nt][i][1], o[nt][i][2], o[nt][i][3]);
-                if (to == warp) { own[j][0] = v.x; own[j][1] = v.y; own[j][2] = v.z; own[j][3] = v.w; }
-                else *reinterpret_cast<float4 *>(comb[to][warp < to ? warp : warp - 1][j][lane]) = v;
-            }
-            __syncthreads();
             float M[2], L[2], wgt[kWarps][2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                M[e] = -INFINITY;
+            for (int round = 0; round < S::kRounds; ++round) {
+                float own[S::kOnce][4];
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) M[e] = fmaxf(M[e], sh.ml[w][2 * t4 + e][0]);
-                const float ref = M[e] == -INFINITY ? 0.f : M[e];
-                L[e] = 0.f;
+                for (int to = 0; to < kWarps; ++to)
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    wgt[w][e] = exp2f(sh.ml[w][2 * t4 + e][0] - ref);
-                    L[e] = fmaf(wgt[w][e], sh.ml[w][2 * t4 + e][1], L[e]);
-                }
-            }
-            float sum[S::kOwn][4];
+                    for (int j = 0; j < S::kOnce; ++j) {
+                        const float (&v)[4] = o[nt][to * S::kOwn + round * S::kOnce + j];
+                        if (to == warp) { own[j][0] = v[0]; own[j][1] = v[1]; own[j][2] = v[2]; own[j][3] = v[3]; }
+                        else *reinterpret_cast<float4 *>(comb[to][warp < to ? warp : warp - 1][j][lane]) = make_float4(v[0], v[1], v[2], v[3]);
+                    }
+                __syncthreads();
+                if (round == 0) {
 #pragma unroll
-            for (int j = 0; j < S::kOwn; ++j) sum[j][0] = sum[j][1] = sum[j][2] = sum[j][3] = 0.f;
+                    for (int e = 0; e < 2; ++e) {
+                        M[e] = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w)
+                        for (int w = 0; w < kWarps; ++w) M[e] = fmaxf(M[e], sh.ml[w][2 * t4 + e][0]);
+                        const float ref = M[e] == -INFINITY ? 0.f : M[e];
+                        L[e] = 0.f;
 #pragma unroll
-                for (int j = 0; j < S::kOwn; ++j) {
-                    float4 v = make_float4(own[j][0], own[j][1], own[j][2], own[j][3]);
-                    if (w != warp) v = *reinterpret_cast<const float4 *>(comb[warp][w < warp ? w : w - 1][j][lane]);
-                    sum[j][0] = fmaf(wgt[w][0], v.x, sum[j][0]); sum[j][1] = fmaf(wgt[w][1], v.y, sum[j][1]);
-                    sum[j][2] = fmaf(wgt[w][0], v.z, sum[j][2]); sum[j][3] = fmaf(wgt[w][1], v.w, sum[j][3]);
-                }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int h = nt * 8 + 2 * t4 + e;
-                if (h >= heads_here) continue;
-                const float inv = L[e] == 0.f ? 0.f : 1.f / L[e];
-#pragma unroll
-                for (int j = 0; j < S::kOwn; ++j) {
-                    const int i = warp * S::kOwn + j;
-                    const int d0 = CODES ? 16 * i + 2 * g8 : 16 * i + g8, d1 = CODES ? d0 + 1 : d0 + 8;
-                    if (whole) {
-                        store_out<TYPE>(p, out_at + h * D + d0, sum[j][e] * inv);
-                        store_out<TYPE>(p, out_at + h * D + d1, sum[j][2 + e] * inv);
-                    } else {
-                        slot[h * D + d0] = sum[j][e];
-                        slot[h * D + d1] = sum[j][2 + e];
+                        for (int w = 0; w < kWarps; ++w) {
+                            wgt[w][e] = exp2f(sh.ml[w][2 * t4 + e][0] - ref);
+                            L[e] = fmaf(wgt[w][e], sh.ml[w][2 * t4 + e][1], L[e]);
+                        }
                     }
                 }
-                if (warp == 0 && g8 == 0) {
-                    if (!whole) *(reinterpret_cast<float2 *>(slot + 8 * NT * D) + h) = make_float2(M[e], L[e]);
-                    else if (p.lse) p.lse[lse_at + h] = L[e] == 0.f ? -INFINITY : (M[e] + log2f(L[e])) * kLn2;
+                float sum[S::kOnce][4];
+#pragma unroll
+                for (int j = 0; j < S::kOnce; ++j) sum[j][0] = sum[j][1] = sum[j][2] = sum[j][3] = 0.f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w)
+#pragma unroll
+                    for (int j = 0; j < S::kOnce; ++j) {
+                        float4 v = make_float4(own[j][0], own[j][1], own[j][2], own[j][3]);
+                        if (w != warp) v = *reinterpret_cast<const float4 *>(comb[warp][w < warp ? w : w - 1][j][lane]);
+                        sum[j][0] = fmaf(wgt[w][0], v.x, sum[j][0]); sum[j][1] = fmaf(wgt[w][1], v.y, sum[j][1]);
+                        sum[j][2] = fmaf(wgt[w][0], v.z, sum[j][2]); sum[j][3] = fmaf(wgt[w][1], v.w, sum[j][3]);
+                    }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int h = nt * 8 + 2 * t4 + e;
+                    if (h >= heads_here) continue;
+                    const float inv = L[e] == 0.f ? 0.f : 1.f / L[e];
+#pragma unroll
+                    for (int j = 0; j < S::kOnce; ++j) {
+                        const int i = warp * S::kOwn + round * S::kOnce + j;
+                        const int d0 = CODES ? 16 * i + 2 * g8 : 16 * i + g8, d1 = CODES ? d0 + 1 : d0 + 8;
+                        if (whole) {
+                            store_out<TYPE>(p, out_at + h * D + d0, sum[j][e] * inv);
+                            store_out<TYPE>(p, out_at + h * D + d1, sum[j][2 + e] * inv);
+                        } else {
+                            slot[h * D + d0] = sum[j][e];
+                            slot[h * D + d1] = sum[j][2 + e];
+                        }
+                    }
+                    if (round == 0 && warp == 0 && g8 == 0) {
+                        if (!whole) *(reinterpret_cast<float2 *>(slot + 8 * NT * D) + h) = make_float2(M[e], L[e]);
+                        else if (p.lse) p.lse[lse_at + h] = L[e] == 0.f ? -INFINITY : (M[e] + log2f(L[e])) * kLn2;
+                    }
                 }
+                __syncthreads();
             }
-            __syncthreads();
         }
         if (!whole && tid == 0) {
             auto &s = sh.split[first == item_lo ? 1 : 0];
@@ -834,7 +843,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_paged_kernel(const PagedA
 
 template <int D, int NT, int KV, int QT, int PT>
 cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
-    typedef Shape<D, NT, KV> S;
+    typedef Shape<D, NT, KV, QT> S;
     static unsigned long long raised = 0;
     auto kern = attn_paged_kernel<D, NT, KV, QT, PT>;
     cudaError_t e = ensure_dynamic_smem(kern, S::kSmem, &raised);
@@ -842,7 +851,7 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     const long long most = ((long long)p.c.pages_per_seq << p.c.page_shift);
     const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile + 1) * p.batch * p.c.n_kv * p.chunks;   // the longest list the table allows
     if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
-    long long ctas = 2ll * lc.sm_count;
+    long long ctas = (long long)S::kCtas * lc.sm_count;
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
     const long long fit = (long long)(p.part_floats / (2 * S::kSlotFloats));
     if (ctas > fit) ctas = fit;

@@ -382,7 +382,7 @@ def test_attention(nnc, scratch, kv, dtype, heads, group, d, page, window):
     q = _randn(_gen(d + group), len(lens), heads * group, d, dtype=dtype)
     out, lse = nnc.op_attn_decode_paged(q, cache, _ints(lens), window=window, scratch=scratch, want_lse=True)
     _check_attention(out, lse, q, held, lens, d ** -0.5, window, kv)
-    assert nnc.op_status() == 0 and not scratch[:4096].any()
+    assert nnc.op_status() == 0 and not scratch[:8192].any()
     again, lse2 = nnc.op_attn_decode_paged(q, cache, _ints(lens), window=window, scratch=scratch, want_lse=True)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
@@ -472,7 +472,7 @@ def test_lengths_and_pages_out_of_range_are_cut_and_reported(nnc, scratch):
     cache.page_table[0] = -1                                          # none left: a row of zeros
     out, lse = nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch, want_lse=True)
     assert nnc.op_status() == 0x100 and (out[0] == 0).all() and (lse[0] == -math.inf).all()
-    assert nnc.op_status() == 0 and not scratch[:4096].any()
+    assert nnc.op_status() == 0 and not scratch[:8192].any()
 
 
 def test_attention_agrees_with_the_contiguous_cache_kernel(nnc, scratch):
