@@ -769,18 +769,29 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         int n = grouped ? min(kJoinGroup, c_hi - c0 + 1) : pieces;
 #pragma unroll 1
         for (bool final = !grouped;;) {
-            auto place = [&](int i) {   // the first piece of a (sequence, head) lies in its CTA's slot 1, the others in slot 0
-                const int c = c0 + i * apart;
-                return p.part + (size_t)(2 * c + (c == c_lo ? 1 : 0)) * S::kSlotFloats;
-            };
-            for (int i = tid; i < n * 4 * NT; i += kWarps * 32)   // 16 bytes: two heads' words
-                copy16(ml0 + i * 16, place(i / (4 * NT)) + 8 * NT * D + 4 * (i % (4 * NT)));
+            // the first piece of a (sequence, head) lies in its CTA's slot 1, the others in slot 0
+            float *const slot_a = p.part + (size_t)(2 * c0 + (c0 == c_lo ? 1 : 0)) * S::kSlotFloats;
+            const float *const slot_b = p.part + (size_t)(2 * c0) * S::kSlotFloats;   // the i-th from there, i > 0
+            const size_t step = (size_t)(2 * apart) * S::kSlotFloats;
+            for (int i = tid; i < n * 4 * NT; i += kWarps * 32) {   // 16 bytes: two heads' words
+                const int from = i / (4 * NT);
+                copy16(ml0 + i * 16, (from ? slot_b + from * step : slot_a) + 8 * NT * D + 4 * (i % (4 * NT)));
+            }
             copy_commit();
             const int fit = kWarps * S::kStages * S::kStage / (cols * 16);   // pieces that the ring holds at a time (10 at least)
             for (int lo = 0; lo < n; lo += fit) {
                 const int hi = min(lo + fit, n);
-                for (int col = tid; col < cols; col += kWarps * 32)
-                    for (int i = lo; i < hi; ++i) copy16(ring0 + ((i - lo) * cols + col) * 16, place(i) + 4 * col);
+                for (int col = tid; col < cols; col += kWarps * 32) {
+                    uint32_t dst = ring0 + col * 16;
+                    const float *src = (lo ? slot_b + lo * step : slot_a) + 4 * col, *next = slot_b + (lo + 1) * step + 4 * col;
+#pragma unroll 4
+                    for (int i = lo; i < hi; ++i) {
+                        copy16(dst, src);
+                        dst += cols * 16;
+                        src = next;
+                        next += step;
+                    }
+                }
                 copy_commit();
                 if (lo == 0) {
                     copy_wait<1>();
@@ -802,7 +813,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                 for (int col = tid; col < cols; col += kWarps * 32) {   // every thread reads what it copied itself
                     const int h = col / (D / 4);
                     const float4 *rows = reinterpret_cast<const float4 *>(smem);
-                    float4 *slot0 = reinterpret_cast<float4 *>(place(0)) + col;
+                    float4 *slot0 = reinterpret_cast<float4 *>(slot_a) + col;
                     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (lo > 0) sum = *slot0;   // what the pieces before these gave
 #pragma unroll 4
@@ -814,7 +825,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                     const float2 ML = tot[h];
                     if (!final || hi < n) {
                         *slot0 = sum;   // this thread alone read that place, and has
-                        if (hi == n && col % (D / 4) == 0) *(reinterpret_cast<float2 *>(place(0) + 8 * NT * D) + h) = ML;
+                        if (hi == n && col % (D / 4) == 0) *(reinterpret_cast<float2 *>(slot_a + 8 * NT * D) + h) = ML;
                         continue;
                     }
                     const float inv = ML.y == 0.f ? 0.f : 1.f / ML.y;

@@ -5,9 +5,8 @@
 // KV head): eight elements each, so a 16-bit row moves as 16-byte vectors and a row of codes as 8-byte ones, and a row's
 // largest magnitude is found by shuffles among its lanes, with the row read once.  The key row's and the value row's loads
 // are in flight together.
-#include <cuda_fp16.h>
-
 #include "paged.cuh"
+#include "vec8.cuh"
 
 namespace nnc {
 
@@ -22,55 +21,6 @@ struct RowsParams {
 };
 
 constexpr int kScaleMax = 60;   // a row's exponent lies in [-60, 60]
-
-template <int TYPE> struct Vec8 { uint4 q[TYPE == NNC_F32 ? 2 : 1]; };   // eight elements of a 16-bit type or of fp32
-
-template <int TYPE> __device__ __forceinline__ Vec8<TYPE> load8(const char *p) {
-    Vec8<TYPE> r;
-    r.q[0] = reinterpret_cast<const uint4 *>(p)[0];
-    if constexpr (TYPE == NNC_F32) r.q[1] = reinterpret_cast<const uint4 *>(p)[1];
-    return r;
-}
-template <int TYPE> __device__ __forceinline__ void store8(char *p, const Vec8<TYPE> &r) {
-    reinterpret_cast<uint4 *>(p)[0] = r.q[0];
-    if constexpr (TYPE == NNC_F32) reinterpret_cast<uint4 *>(p)[1] = r.q[1];
-}
-
-template <int TYPE> __device__ __forceinline__ void unpack8(const Vec8<TYPE> &r, float (&f)[8]) {
-    if constexpr (TYPE == NNC_F32) {
-        const uint32_t w[8] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w, r.q[1].x, r.q[1].y, r.q[1].z, r.q[1].w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
-    } else {
-        const uint32_t w[4] = {r.q[0].x, r.q[0].y, r.q[0].z, r.q[0].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (TYPE == NNC_BF16) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
-            else {
-                f[2 * i] = __half2float(__ushort_as_half((uint16_t)w[i]));
-                f[2 * i + 1] = __half2float(__ushort_as_half((uint16_t)(w[i] >> 16)));
-            }
-        }
-    }
-}
-template <int TYPE> __device__ __forceinline__ Vec8<TYPE> pack8(const float (&f)[8]) {
-    Vec8<TYPE> r;
-    if constexpr (TYPE == NNC_F32) {
-        r.q[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-        r.q[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (TYPE == NNC_BF16) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
-            else
-                w[i] = (uint32_t)__half_as_ushort(__float2half_rn(f[2 * i])) |
-                       (uint32_t)__half_as_ushort(__float2half_rn(f[2 * i + 1])) << 16;
-        }
-        r.q[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    return r;
-}
 
 // Eight values of a row whose `lanes` lanes hold the rest: the row's exponent (biased by 127) and these values' codes.
 template <int LANES> __device__ __forceinline__ uint2 quantise8(const float (&f)[8], uint32_t &byte) {
@@ -108,98 +58,139 @@ __device__ __forceinline__ void dequantise8(const uint2 codes, uint32_t byte, fl
     }
 }
 
-// D: head_dim; KV: the cache's type; TYPE: the type of the rows outside
-template <int D, int KV, int TYPE, bool WRITE>
+// D: head_dim; KV: the cache's type; TYPE: the type of the rows outside; R: rows a thread takes part in, whose loads are in
+// flight together
+template <int D, int KV, int TYPE, bool WRITE, int R>
 __global__ void __launch_bounds__(256) kv_rows_kernel(const RowsParams p) {
-    constexpr int kLanes = D / 8, kRowsPerCta = 256 / kLanes;
-    const int lane = threadIdx.x % kLanes;
-    const long long row = (long long)blockIdx.x * kRowsPerCta + threadIdx.x / kLanes;
-    const long long t_all = row / p.c.n_kv;
-    const int h = (int)(row - t_all * p.c.n_kv);
-    const bool in = t_all < p.n_tokens;
-    const int t = in ? (int)t_all : 0;
-    const int s = p.seq ? p.seq[t] : t, n = p.pos[t];
+    constexpr int kLanes = D / 8, kRows = 256 / kLanes;   // rows a CTA takes at once
     constexpr int kOutside = TYPE == NNC_F32 ? 32 : 16;   // bytes of a lane's eight elements outside the cache
-    const long long off = t * p.row_stride + h * p.head_stride + lane * kOutside;
-    Vec8<TYPE> k, v;
-    if constexpr (WRITE) { k = load8<TYPE>(p.k + off); v = load8<TYPE>(p.v + off); }
-    // the address: padding is left out, what lies outside is left out and reported
-    bool live = in && s >= 0 && n >= 0;
-    long long at = 0;
-    if (live) {
-        const int column = n >> p.c.page_shift;
-        int page = -1;
-        if (s < p.c.n_seqs && column < p.c.pages_per_seq) page = p.c.table[(long long)s * p.c.pages_per_seq + column];
-        if (page < 0 || page >= p.c.n_pages) {
-            live = false;
-            if (lane == 0 && h == 0) paged_complain(p.c);
-        } else {
-            at = paged_row(p.c, page, h, n & ((1 << p.c.page_shift) - 1));
+    const int lane = threadIdx.x % kLanes;
+    const unsigned rows = (unsigned)p.n_tokens * (unsigned)p.c.n_kv;
+    const unsigned row0 = blockIdx.x * (unsigned)(kRows * R) + threadIdx.x / kLanes;
+    int s[R], n[R], h[R], page[R];
+    bool live[R];
+    long long off[R], at[R];
+    Vec8<TYPE> k[R], v[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const unsigned row = row0 + i * kRows;
+        live[i] = row < rows;
+        const unsigned t = live[i] ? row / (unsigned)p.c.n_kv : 0u;
+        h[i] = live[i] ? (int)(row - t * p.c.n_kv) : 0;
+        s[i] = p.seq ? p.seq[t] : (int)t;
+        n[i] = p.pos[t];
+        off[i] = t * p.row_stride + h[i] * p.head_stride + lane * kOutside;
+        if constexpr (WRITE) { k[i] = load8<TYPE>(p.k + off[i]); v[i] = load8<TYPE>(p.v + off[i]); }
+    }
+    // the addresses: padding is left out, what lies outside is left out and reported
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        live[i] = live[i] && s[i] >= 0 && n[i] >= 0;
+        const int column = n[i] >> p.c.page_shift;
+        page[i] = -1;
+        if (live[i] && s[i] < p.c.n_seqs && column < p.c.pages_per_seq) page[i] = p.c.table[(long long)s[i] * p.c.pages_per_seq + column];
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (live[i] && (unsigned)page[i] >= (unsigned)p.c.n_pages) {
+            live[i] = false;
+            if (lane == 0 && h[i] == 0) paged_complain(p.c);
         }
+        at[i] = live[i] ? paged_row(p.c, page[i], h[i], n[i] & ((1 << p.c.page_shift) - 1)) : 0;
     }
     if constexpr (WRITE) {
-        if constexpr (KV == TYPE) {
-            if (!live) return;
-            const long long b = at * (2 * D) + lane * 16;
-            store8<TYPE>(p.c.k + b, k);
-            store8<TYPE>(p.c.v + b, v);
-        } else {
-            float fk[8], fv[8];
-            unpack8<TYPE>(k, fk);
-            unpack8<TYPE>(v, fv);
-            if constexpr (KV == NNC_E4M3) {
-                uint32_t ke, ve;   // every lane of the warp takes part in the shuffles, whether its row is live or not
-                const uint2 kc = quantise8<kLanes>(fk, ke), vc = quantise8<kLanes>(fv, ve);
-                if (!live) return;
-                *reinterpret_cast<uint2 *>(p.c.k + at * D + lane * 8) = kc;
-                *reinterpret_cast<uint2 *>(p.c.v + at * D + lane * 8) = vc;
-                if (lane == 0) { p.c.k_scale[at] = (uint8_t)ke; p.c.v_scale[at] = (uint8_t)ve; }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const long long b = at[i] * (2 * D) + lane * 16;
+            if constexpr (KV == TYPE) {
+                if (!live[i]) continue;
+                store8<TYPE>(p.c.k + b, k[i]);
+                store8<TYPE>(p.c.v + b, v[i]);
             } else {
-                if (!live) return;
-                const long long b = at * (2 * D) + lane * 16;
-                store8<KV>(p.c.k + b, pack8<KV>(fk));
-                store8<KV>(p.c.v + b, pack8<KV>(fv));
+                float fk[8], fv[8];
+                unpack8<TYPE>(k[i], fk);
+                unpack8<TYPE>(v[i], fv);
+                if constexpr (KV == NNC_E4M3) {
+                    uint32_t ke, ve;   // every lane of the warp takes part in the shuffles, whether its row is live or not
+                    const uint2 kc = quantise8<kLanes>(fk, ke), vc = quantise8<kLanes>(fv, ve);
+                    if (!live[i]) continue;
+                    *reinterpret_cast<uint2 *>(p.c.k + at[i] * D + lane * 8) = kc;
+                    *reinterpret_cast<uint2 *>(p.c.v + at[i] * D + lane * 8) = vc;
+                    if (lane == 0) { p.c.k_scale[at[i]] = (uint8_t)ke; p.c.v_scale[at[i]] = (uint8_t)ve; }
+                } else {
+                    if (!live[i]) continue;
+                    store8<KV>(p.c.k + b, pack8<KV>(fk));
+                    store8<KV>(p.c.v + b, pack8<KV>(fv));
+                }
             }
         }
     } else {
-        if (!live) return;
-        if constexpr (KV == TYPE) {
-            const long long b = at * (2 * D) + lane * 16;
-            k = load8<TYPE>(p.c.k + b);
-            v = load8<TYPE>(p.c.v + b);
-        } else {
-            float fk[8], fv[8];
-            if constexpr (KV == NNC_E4M3) {
-                const uint2 kc = *reinterpret_cast<const uint2 *>(p.c.k + at * D + lane * 8);
-                const uint2 vc = *reinterpret_cast<const uint2 *>(p.c.v + at * D + lane * 8);
-                dequantise8(kc, p.c.k_scale[at], fk);
-                dequantise8(vc, p.c.v_scale[at], fv);
-            } else {
-                const long long b = at * (2 * D) + lane * 16;
-                unpack8<KV>(load8<KV>(p.c.k + b), fk);
-                unpack8<KV>(load8<KV>(p.c.v + b), fv);
+        // a row that is not there is read from the pool's first one and not stored
+        if constexpr (KV == NNC_E4M3) {
+            uint2 kc[R], vc[R];
+            uint32_t ke[R], ve[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                kc[i] = *reinterpret_cast<const uint2 *>(p.c.k + at[i] * D + lane * 8);
+                vc[i] = *reinterpret_cast<const uint2 *>(p.c.v + at[i] * D + lane * 8);
+                ke[i] = p.c.k_scale[at[i]];
+                ve[i] = p.c.v_scale[at[i]];
             }
-            k = pack8<TYPE>(fk);
-            v = pack8<TYPE>(fv);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float fk[8], fv[8];
+                dequantise8(kc[i], ke[i], fk);
+                dequantise8(vc[i], ve[i], fv);
+                k[i] = pack8<TYPE>(fk);
+                v[i] = pack8<TYPE>(fv);
+            }
+        } else {
+            Vec8<KV> ck[R], cv[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const long long b = at[i] * (2 * D) + lane * 16;
+                ck[i] = load8<KV>(p.c.k + b);
+                cv[i] = load8<KV>(p.c.v + b);
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if constexpr (KV == TYPE) { k[i] = ck[i]; v[i] = cv[i]; }
+                else {
+                    float fk[8], fv[8];
+                    unpack8<KV>(ck[i], fk);
+                    unpack8<KV>(cv[i], fv);
+                    k[i] = pack8<TYPE>(fk);
+                    v[i] = pack8<TYPE>(fv);
+                }
+            }
         }
-        store8<TYPE>(p.k + off, k);
-        store8<TYPE>(p.v + off, v);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (!live[i]) continue;
+            store8<TYPE>(p.k + off[i], k[i]);
+            store8<TYPE>(p.v + off[i], v[i]);
+        }
     }
+}
+
+template <int D, int KV, int TYPE, bool WRITE>
+cudaError_t launch_sized(const LaunchCtx &lc, const RowsParams &p) {
+    constexpr int kRows = 256 / (D / 8);
+    const long long rows = (long long)p.n_tokens * p.c.n_kv;
+    const long long once = (rows + kRows - 1) / kRows;
+    // four rows a thread where that still leaves every SM several CTAs; otherwise one, for the shortest way through
+    if (once >= 16ll * lc.sm_count)
+        return launch(lc, kv_rows_kernel<D, KV, TYPE, WRITE, 4>, dim3((unsigned)((once + 3) / 4)), dim3(256), p);
+    return launch(lc, kv_rows_kernel<D, KV, TYPE, WRITE, 1>, dim3((unsigned)once), dim3(256), p);
 }
 
 template <int D, int KV>
 cudaError_t launch_rows(const LaunchCtx &lc, const RowsParams &p, bool write, int type) {
-    const long long rows = (long long)p.n_tokens * p.c.n_kv;
-    constexpr int kRowsPerCta = 256 / (D / 8);
-    const dim3 grid((unsigned)((rows + kRowsPerCta - 1) / kRowsPerCta)), block(256);
-#define NNC_ROWS_CASE(TT) \
-    return write ? launch(lc, kv_rows_kernel<D, KV, TT, true>, grid, block, p) : launch(lc, kv_rows_kernel<D, KV, TT, false>, grid, block, p)
     switch (type) {
-        case NNC_F32: NNC_ROWS_CASE(NNC_F32);
-        case NNC_BF16: NNC_ROWS_CASE(NNC_BF16);
-        default: NNC_ROWS_CASE(NNC_F16);
+        case NNC_F32: return write ? launch_sized<D, KV, NNC_F32, true>(lc, p) : launch_sized<D, KV, NNC_F32, false>(lc, p);
+        case NNC_BF16: return write ? launch_sized<D, KV, NNC_BF16, true>(lc, p) : launch_sized<D, KV, NNC_BF16, false>(lc, p);
+        default: return write ? launch_sized<D, KV, NNC_F16, true>(lc, p) : launch_sized<D, KV, NNC_F16, false>(lc, p);
     }
-#undef NNC_ROWS_CASE
 }
 
 }  // namespace

@@ -998,7 +998,7 @@ static int kv_rows_paged(const nnc_paged_kv *cache, bool write, void *k, void *v
     const int64_t el = type == NNC_F32 ? 4 : 2;
     if ((((uintptr_t)k | (uintptr_t)v) & 15) || (row_stride * el) % 16 || (head_stride * el) % 16) return NNC_ERR_INVALID_ARG;
     if (((uintptr_t)pos | (uintptr_t)seq) & 3) return NNC_ERR_INVALID_ARG;
-    if ((int64_t)n_tokens * cache->n_kv_heads > (int64_t)1 << 33) return NNC_ERR_CAPACITY;   // blocks of one launch
+    if ((int64_t)n_tokens * cache->n_kv_heads > 0x7fffffff) return NNC_ERR_CAPACITY;   // rows are counted in 32 bits
     LaunchCtx lc;
     if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
     return launch_kv_paged(lc, *cache, write, k, v, type, n_tokens, row_stride, head_stride, pos, seq) == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;

@@ -1,14 +1,11 @@
 // Rotary positions on rows of heads: y = R(position * freq) x on the first rotary_dim elements of every head.
 //
 // Bound by reading x and writing y.  The angles depend on the token and the pair only, so a CTA works out the cosines and
-// sines of its tokens once, in shared memory, and all heads use them; a thread owns eight pairs of one head (two 16-byte
-// loads and stores of 16-bit values) that it requests before the angles are known.  The angle is position * freq in 64 bits,
-// reduced to an eighth of a turn before it is rounded to fp32: what is left then is off by at most 2^-28 turns, however far
-// the position.
-#include <cuda_fp16.h>
-
-#include "common.cuh"
-#include "nnc_internal.h"
+// sines of its tokens once, in shared memory, and all heads use them.  A thread owns eight pairs of one head (two 16-byte
+// loads and stores of 16-bit values) in several tokens, whose loads are on their way while the angles are worked out.  The
+// angle is position * freq in 64 bits, reduced to an eighth of a turn before it is rounded to fp32: what is left then is off by
+// at most 2^-28 turns, however far the position.
+#include "vec8.cuh"
 
 namespace nnc {
 
@@ -20,24 +17,31 @@ struct RopeParams {
     const int32_t *pos;
     const double *freq;
     long long x_row, x_head, y_row, y_head;   // elements
-    int n_tokens, n_heads, head_dim, rot, tokens_per_cta, units;   // units: work items per head
+    int n_tokens, n_heads, rot, tokens_per_cta, units;   // units: work items per head
+    int abreast;                                         // vector form: tokens that a CTA's threads take at once
     float amplitude;
-    bool inverse, copy_rest;
+    bool inverse;
 };
 
-template <int TYPE> struct Elem { typedef uint16_t raw; };
-template <> struct Elem<NNC_F32> { typedef float raw; };
+// tokens whose loads a thread has in flight when there are many
+template <int TYPE> constexpr int kMany = TYPE == NNC_F32 ? 2 : 3;
 
-template <int TYPE> __device__ __forceinline__ float to_f32(typename Elem<TYPE>::raw r) {
-    if constexpr (TYPE == NNC_F32) return r;
-    else if constexpr (TYPE == NNC_BF16) return bf16_bits_to_f32(r);
-    else return __half2float(__ushort_as_half(r));
-}
-template <int TYPE> __device__ __forceinline__ typename Elem<TYPE>::raw from_f32(float f) {
-    if constexpr (TYPE == NNC_F32) return f;
-    else if constexpr (TYPE == NNC_BF16) return f32_to_bf16_bits(f);
-    else return __half_as_ushort(__float2half_rn(f));
-}
+template <int TYPE> struct Scalar {
+    typedef uint16_t raw;
+    static __device__ __forceinline__ float get(raw r) {
+        if constexpr (TYPE == NNC_BF16) return bf16_bits_to_f32(r);
+        else return __half2float(__ushort_as_half(r));
+    }
+    static __device__ __forceinline__ raw put(float f) {
+        if constexpr (TYPE == NNC_BF16) return f32_to_bf16_bits(f);
+        else return __half_as_ushort(__float2half_rn(f));
+    }
+};
+template <> struct Scalar<NNC_F32> {
+    typedef float raw;
+    static __device__ __forceinline__ float get(float f) { return f; }
+    static __device__ __forceinline__ float put(float f) { return f; }
+};
 
 // cosine and sine of pos * freq, times the amplitude
 __device__ __forceinline__ float2 turn_of(int pos, double freq, float amplitude, bool inverse) {
@@ -53,66 +57,116 @@ __device__ __forceinline__ float2 turn_of(int pos, double freq, float amplitude,
     return make_float2(c * amplitude, s * amplitude);
 }
 
-template <int TYPE>
-struct alignas(16) Eight { typename Elem<TYPE>::raw e[8]; };
-
-// VEC: a unit is eight pairs, moved as 16-byte vectors (or eight elements that only pass through); otherwise it is one pair
-// (or one element), for sizes and strides that do not allow vectors.
-template <int TYPE, bool VEC, bool INTERLEAVED>
+// Vector form: a unit is eight pairs (or, past the rotated part, eight elements that only pass through).  Thread: one unit of
+// one head (more, if a token has more units than the CTA has threads), in M tokens.
+template <int TYPE, bool INTERLEAVED, int M>
 __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
-    typedef typename Elem<TYPE>::raw raw;
-    extern __shared__ float2 turn[];   // [tokens_per_cta][rot / 2]
-    const int half = p.rot / 2;
-    const int t0 = blockIdx.x * p.tokens_per_cta;
-    const int tokens = min(p.tokens_per_cta, p.n_tokens - t0);
-    const int rot_units = VEC ? half / 8 : half;
-    const int per_token = p.n_heads * p.units, items = tokens * per_token;
-    for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
-        const int t = i / half;
-        turn[i] = turn_of(p.pos[t0 + t], p.freq[i - t * half], p.amplitude, p.inverse);
+    constexpr int el = TYPE == NNC_F32 ? 4 : 2;
+    extern __shared__ float4 turn[];   // [tokens_per_cta][4][rot / 16]: two pairs each; lanes of one head read side by side
+    const int half = p.rot / 2, rot_units = half / 8;
+    const int t0 = blockIdx.x * p.tokens_per_cta, tokens = min(p.tokens_per_cta, p.n_tokens - t0);
+    const int per_token = p.n_heads * p.units;
+    const int first = threadIdx.x / per_token;                       // the thread's first token; past it, every abreast-th
+    const int each = p.abreast > 1 ? per_token : (int)blockDim.x;    // units that the CTA's threads cover of a token
+    Vec8<TYPE> a[M], b[M];
+    long long x_at = 0, y_at = 0;
+    int u = 0, at_a = 0, at_b = 0;
+    auto load = [&](int r) {
+        const int h = r / p.units;
+        u = r - h * p.units;
+        if (u >= rot_units) at_a = at_b = p.rot + 8 * (u - rot_units);
+        else if (INTERLEAVED) { at_a = 16 * u; at_b = at_a + 8; }
+        else { at_a = 8 * u; at_b = half + 8 * u; }
+        x_at = (long long)(t0 + first) * p.x_row + h * p.x_head;
+        y_at = (long long)(t0 + first) * p.y_row + h * p.y_head;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            if (first + m * p.abreast >= tokens) break;
+            const char *x = p.x + (x_at + (long long)(m * p.abreast) * p.x_row) * el;
+            a[m] = load8<TYPE>(x + at_a * el);
+            if (u < rot_units) b[m] = load8<TYPE>(x + at_b * el);
+        }
+    };
+    int r = threadIdx.x - first * per_token;
+    const bool in = first < p.abreast && r < per_token;   // (a token wider than the CTA: first is 0)
+    if (in) load(r);
+    for (int k = threadIdx.x; k < tokens * half; k += blockDim.x) {
+        const int t = k / half, i = k - t * half;
+        reinterpret_cast<float2 *>(turn)[((t * 4 + (i & 7) / 2) * rot_units + i / 8) * 2 + (i & 1)] =
+            turn_of(p.pos[t0 + t], p.freq[i], p.amplitude, p.inverse);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < items; i += blockDim.x) {
-        const int t = i / per_token, r = i - t * per_token, h = r / p.units, u = r - h * p.units;
-        const raw *x = reinterpret_cast<const raw *>(p.x) + (t0 + t) * p.x_row + h * p.x_head;
-        raw *y = reinterpret_cast<raw *>(p.y) + (t0 + t) * p.y_row + h * p.y_head;
-        if (u >= rot_units) {   // elements past the rotated part
-            if constexpr (VEC) {
-                const int at = p.rot + 8 * (u - rot_units);
-                *reinterpret_cast<Eight<TYPE> *>(y + at) = *reinterpret_cast<const Eight<TYPE> *>(x + at);
-            } else {
-                const int at = p.rot + (u - rot_units);
-                y[at] = x[at];
+    if (!in) return;
+    for (;;) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int t = first + m * p.abreast;
+            if (t >= tokens) break;
+            char *y = p.y + (y_at + (long long)(m * p.abreast) * p.y_row) * el;
+            if (u < rot_units) {
+                float fa[8], fb[8];
+                unpack8<TYPE>(a[m], fa);
+                unpack8<TYPE>(b[m], fb);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 cs = turn[(t * 4 + q) * rot_units + u];   // pairs 2q and 2q + 1
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int j = 2 * q + e;
+                        float &xa = INTERLEAVED ? (j < 4 ? fa[2 * j & 7] : fb[2 * j & 7]) : fa[j];
+                        float &xb = INTERLEAVED ? (j < 4 ? fa[(2 * j & 7) + 1] : fb[(2 * j & 7) + 1]) : fb[j];
+                        const float c = e ? cs.z : cs.x, s = e ? cs.w : cs.y, va = xa, vb = xb;
+                        xa = va * c - vb * s;
+                        xb = vb * c + va * s;
+                    }
+                }
+                a[m] = pack8<TYPE>(fa);
+                store8<TYPE>(y + at_b * el, pack8<TYPE>(fb));
             }
+            store8<TYPE>(y + at_a * el, a[m]);
+        }
+        r += each;
+        if (r >= per_token) break;
+        load(r);
+    }
+}
+
+// Element by element, for sizes and strides that do not allow vectors: a unit is one pair, or one element that passes through.
+template <int TYPE, bool INTERLEAVED>
+__global__ void __launch_bounds__(512) rope_plain_kernel(const RopeParams p) {
+    typedef Scalar<TYPE> E;
+    extern __shared__ float4 turn4[];
+    float2 *turn = reinterpret_cast<float2 *>(turn4);   // [tokens_per_cta][rot / 2]
+    const int half = p.rot / 2;
+    const int t0 = blockIdx.x * p.tokens_per_cta, tokens = min(p.tokens_per_cta, p.n_tokens - t0);
+    const int per_token = p.n_heads * p.units;
+    for (int k = threadIdx.x; k < tokens * half; k += blockDim.x) {
+        const int t = k / half;
+        turn[k] = turn_of(p.pos[t0 + t], p.freq[k - t * half], p.amplitude, p.inverse);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < tokens * per_token; i += blockDim.x) {
+        const int t = i / per_token, r = i - t * per_token, h = r / p.units, u = r - h * p.units;
+        const typename E::raw *x = reinterpret_cast<const typename E::raw *>(p.x) + (long long)(t0 + t) * p.x_row + h * p.x_head;
+        typename E::raw *y = reinterpret_cast<typename E::raw *>(p.y) + (long long)(t0 + t) * p.y_row + h * p.y_head;
+        if (u >= half) {
+            y[p.rot + u - half] = x[p.rot + u - half];
             continue;
         }
-        const float2 *cs = turn + t * half + (VEC ? 8 * u : u);
-        if constexpr (VEC) {
-            const int a0 = INTERLEAVED ? 16 * u : 8 * u, b0 = INTERLEAVED ? 16 * u + 8 : half + 8 * u;
-            Eight<TYPE> a = *reinterpret_cast<const Eight<TYPE> *>(x + a0), b = *reinterpret_cast<const Eight<TYPE> *>(x + b0);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                raw &ea = INTERLEAVED ? (j < 4 ? a.e[2 * j & 7] : b.e[2 * j & 7]) : a.e[j];
-                raw &eb = INTERLEAVED ? (j < 4 ? a.e[(2 * j & 7) + 1] : b.e[(2 * j & 7) + 1]) : b.e[j];
-                const float xa = to_f32<TYPE>(ea), xb = to_f32<TYPE>(eb);
-                ea = from_f32<TYPE>(xa * cs[j].x - xb * cs[j].y);
-                eb = from_f32<TYPE>(xb * cs[j].x + xa * cs[j].y);
-            }
-            *reinterpret_cast<Eight<TYPE> *>(y + a0) = a;
-            *reinterpret_cast<Eight<TYPE> *>(y + b0) = b;
-        } else {
-            const int ia = INTERLEAVED ? 2 * u : u, ib = INTERLEAVED ? 2 * u + 1 : half + u;
-            const float xa = to_f32<TYPE>(x[ia]), xb = to_f32<TYPE>(x[ib]);
-            y[ia] = from_f32<TYPE>(xa * cs->x - xb * cs->y);
-            y[ib] = from_f32<TYPE>(xb * cs->x + xa * cs->y);
-        }
+        const int ia = INTERLEAVED ? 2 * u : u, ib = INTERLEAVED ? 2 * u + 1 : half + u;
+        const float2 cs = turn[t * half + u];
+        const float xa = E::get(x[ia]), xb = E::get(x[ib]);
+        y[ia] = E::put(xa * cs.x - xb * cs.y);
+        y[ib] = E::put(xb * cs.x + xa * cs.y);
     }
 }
 
 template <int TYPE>
-cudaError_t launch_typed(const LaunchCtx &lc, const RopeParams &p, bool vec, bool interleaved, dim3 grid, dim3 block, int smem) {
-    auto kern = vec ? (interleaved ? rope_kernel<TYPE, true, true> : rope_kernel<TYPE, true, false>)
-                    : (interleaved ? rope_kernel<TYPE, false, true> : rope_kernel<TYPE, false, false>);
+cudaError_t launch_typed(const LaunchCtx &lc, const RopeParams &p, bool vec, bool many, bool interleaved, dim3 grid, dim3 block, int smem) {
+    constexpr int M = kMany<TYPE>;
+    auto kern = !vec ? (interleaved ? rope_plain_kernel<TYPE, true> : rope_plain_kernel<TYPE, false>)
+              : many ? (interleaved ? rope_kernel<TYPE, true, M> : rope_kernel<TYPE, false, M>)
+                     : (interleaved ? rope_kernel<TYPE, true, 1> : rope_kernel<TYPE, false, 1>);
     if (lc.launches) ++*lc.launches;
     kern<<<grid, block, smem, lc.stream>>>(p);
     return cudaGetLastError();
@@ -127,28 +181,33 @@ cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, i
     RopeParams p;
     p.x = (const char *)x; p.y = (char *)y; p.pos = positions; p.freq = freq;
     p.x_row = x_row; p.x_head = x_head; p.y_row = y_row; p.y_head = y_head;
-    p.n_tokens = n_tokens; p.n_heads = n_heads; p.head_dim = head_dim; p.rot = rotary_dim;
+    p.n_tokens = n_tokens; p.n_heads = n_heads; p.rot = rotary_dim;
     p.amplitude = amplitude; p.inverse = inverse;
-    p.copy_rest = x != y && rotary_dim < head_dim;
-    // vectors need whole groups of eight pairs, whole 16-byte pieces of what passes through, and 16-byte rows and heads
+    const bool copy_rest = x != y && rotary_dim < head_dim;
+    // vectors need whole groups of eight pairs, whole pieces of eight of what passes through, and 16-byte rows and heads
     bool vec = half % 8 == 0 && head_dim % 8 == 0 && !(((uintptr_t)x | (uintptr_t)y) & 15);
     for (int64_t s : {x_row, x_head, y_row, y_head}) vec = vec && (s * el) % 16 == 0;
     p.units = vec ? half / 8 : half;
-    if (p.copy_rest) p.units += vec ? (head_dim - rotary_dim) / 8 : head_dim - rotary_dim;
+    if (copy_rest) p.units += vec ? (head_dim - rotary_dim) / 8 : head_dim - rotary_dim;
     const long long per_token = (long long)n_heads * p.units;
-    // one token a CTA where a token fills one, as many as give 256 items otherwise (the angles' table: 16 KB at most)
-    long long tokens = per_token >= 256 ? 1 : 256 / per_token;
-    if (tokens * half > 2048) tokens = half >= 2048 ? 1 : 2048 / half;
-    if (tokens > n_tokens) tokens = n_tokens;
-    p.tokens_per_cta = (int)tokens;
-    long long threads = (tokens * per_token + 31) / 32 * 32;
+    // A CTA's threads take one token abreast where that gives them 128 units or more, and else as many as give 256.  With enough
+    // tokens for several CTAs per SM a thread has kMany of them in flight; otherwise one, for the shortest way through.
+    const int m = type == NNC_F32 ? kMany<NNC_F32> : kMany<NNC_BF16>;
+    long long abreast = per_token >= 128 ? 1 : 256 / per_token;
+    if (abreast * m * half > 4096) abreast = 4096 / (m * half) > 1 ? 4096 / (m * half) : 1;   // 32 KB of angles at most
+    long long threads = abreast * per_token;
     if (threads > 512) threads = 512;
-    const dim3 grid((unsigned)((n_tokens + tokens - 1) / tokens)), block((unsigned)threads);
+    p.abreast = (int)abreast;
+    const bool many = vec && n_tokens >= 4ll * abreast * m * lc.sm_count;
+    long long tokens = abreast * (many ? m : 1);
+    if (!vec) tokens = 1;
+    p.tokens_per_cta = (int)tokens;
+    const dim3 grid((unsigned)((n_tokens + tokens - 1) / tokens)), block((unsigned)((threads + 31) / 32 * 32));
     const int smem = (int)(tokens * half * sizeof(float2));
     switch (type) {
-        case NNC_F32: return launch_typed<NNC_F32>(lc, p, vec, interleaved, grid, block, smem);
-        case NNC_BF16: return launch_typed<NNC_BF16>(lc, p, vec, interleaved, grid, block, smem);
-        default: return launch_typed<NNC_F16>(lc, p, vec, interleaved, grid, block, smem);
+        case NNC_F32: return launch_typed<NNC_F32>(lc, p, vec, many, interleaved, grid, block, smem);
+        case NNC_BF16: return launch_typed<NNC_BF16>(lc, p, vec, many, interleaved, grid, block, smem);
+        default: return launch_typed<NNC_F16>(lc, p, vec, many, interleaved, grid, block, smem);
     }
 }
 
