@@ -428,30 +428,24 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4
 ATTN_PAGED_SCRATCH_BYTES = 16 << 20
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _same_device(device: torch.device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on {device} and {t.device} in one call")
-
-
-def _launch(fn, what: str, device: torch.device, *args):
+def _launch(fn, device: int, *args):
     """The C call on the tensors' own device and that device's current stream, whichever device is current."""
-    if device.index == torch._C._cuda_getDevice():
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if device == _current_device():
+        rc = fn(*args, _current_stream(device))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+            rc = fn(*args, _current_stream(device))
     if rc:
-        raise NncError(rc, what)
+        raise NncError(rc, fn.__name__)
 
 
 def _disjoint(t: torch.Tensor) -> bool:
     """No two elements of t share memory (as far as sorted strides show it)."""
+    if t.is_contiguous():
+        return True
     span = 1
     for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
         if stride < span:
@@ -460,19 +454,34 @@ def _disjoint(t: torch.Tensor) -> bool:
     return True
 
 
-def _rows(t: torch.Tensor, what: str):
-    _need(t.is_cuda and t.dim() == 3 and t.stride(2) == 1, f"{what}: a CUDA tensor [tokens][heads][head_dim] with contiguous heads")
+def _rows(t: torch.Tensor, device: int, what: str):
+    """The type number and the strides between rows and heads of t, [tokens][heads][head_dim] with contiguous heads."""
+    kind = _TYPES.get(t.dtype, 3)
+    if kind == 3 or t.dim() != 3 or t.get_device() != device:
+        raise ValueError(f"{what}: [tokens][heads][head_dim] of float32, bfloat16 or float16 on one CUDA device with the other tensors of the call")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{what}: elements of a head next to each other")
+    return kind, row, head
 
 
-def _index(t: torch.Tensor, n: int, what: str) -> int:
-    _need(t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), f"{what}: {n} contiguous int32 numbers")
+def _index(t: torch.Tensor, n: int, device: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: {n} contiguous int32 numbers on the call's CUDA device")
     return t.data_ptr()
+
+
+def _device(t: torch.Tensor, what: str) -> int:
+    if not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor")
+    return t.get_device()
 
 
 def rope_frequencies(rotary_dim: int, theta: float = 1e6, scaling: str = "plain", factor: float = 1.0, original: float = 0.0,
                      slow: float = 1.0, fast: float = 32.0, device="cuda"):
     """nnc_rope_frequencies: (float64 [rotary_dim / 2] on `device`, amplitude)."""
-    _need(scaling in ROPE_SCALINGS, f"scaling: one of {', '.join(ROPE_SCALINGS)}")
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: one of {', '.join(ROPE_SCALINGS)}")
     freq = torch.empty(max(0, rotary_dim) // 2, dtype=torch.float64)
     amplitude = C.c_float(1.0)
     _ok(lib.nnc_rope_frequencies(rotary_dim, theta, ROPE_SCALINGS[scaling], factor, original, slow, fast, freq.data_ptr(),
@@ -484,20 +493,20 @@ def op_rope(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interl
             inverse: bool = False, out: Optional[torch.Tensor] = None):
     """nnc_op_rope: x [tokens][heads][head_dim] (any strides between rows and heads) turned by int32 `positions`; the first
     2 * len(freq) elements of each head turn.  out: None, x itself, or a tensor of x's shape and type that x does not overlap."""
-    _rows(x, "x")
-    _need(x.dtype in _TYPES and x.dtype is not torch.float8_e4m3fn, "x: float32, bfloat16 or float16")
-    _need(freq.dtype is torch.float64 and freq.dim() == 1 and freq.is_contiguous(), "freq: contiguous float64 numbers")
+    device = _device(x, "x")
+    kind, row, head = _rows(x, device, "x")
     tokens, heads, d = x.shape
     if out is None:
-        out = torch.empty((tokens, heads, d), dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x) if x.is_contiguous() else torch.empty((tokens, heads, d), dtype=x.dtype, device=x.device)
+        out_row, out_head = heads * d, d
     else:
-        _rows(out, "out")
-        _need(out.shape == x.shape and out.dtype == x.dtype and _disjoint(out), "out: x's shape and type, no rows that overlap")
-    _same_device(x.device, positions, freq, out)
-    xs, ys = x.stride(), out.stride()
-    _launch(lib.nnc_op_rope, "nnc_op_rope", x.device, x.data_ptr(), out.data_ptr(), _TYPES[x.dtype], tokens, heads, d, xs[0], xs[1],
-            ys[0], ys[1], _index(positions, tokens, "positions"), freq.data_ptr(), 2 * freq.shape[0], interleaved, inverse,
-            amplitude)
+        out_kind, out_row, out_head = _rows(out, device, "out")
+        if out.shape != x.shape or out_kind != kind or not _disjoint(out):
+            raise ValueError("out: x's shape and type, no rows that overlap")
+    if freq.dtype is not torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != device:
+        raise ValueError("freq: contiguous float64 numbers on the call's CUDA device")
+    _launch(lib.nnc_op_rope, device, x.data_ptr(), out.data_ptr(), kind, tokens, heads, d, row, head, out_row, out_head,
+            _index(positions, tokens, device, "positions"), freq.data_ptr(), 2 * freq.shape[0], interleaved, inverse, amplitude)
     return out
 
 
@@ -510,17 +519,23 @@ class PagedKV:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                  v_scale: Optional[torch.Tensor] = None):
-        _need(k.is_cuda and k.dim() == 4 and k.dtype in (torch.bfloat16, torch.float16, torch.float8_e4m3fn) and k.is_contiguous(),
-              "k: a contiguous CUDA tensor [n_pages][n_kv_heads][page_size][head_dim] of bfloat16, float16 or float8_e4m3fn")
-        _need(v.shape == k.shape and v.dtype is k.dtype and v.is_contiguous(), "v: k's shape and type, contiguous")
-        _need(page_table.dtype is torch.int32 and page_table.dim() == 2 and page_table.is_contiguous(), "page_table: contiguous int32 [n_seqs][pages_per_seq]")
+        device = _device(k, "k")
+        if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16, torch.float8_e4m3fn) or not k.is_contiguous():
+            raise ValueError("k: a contiguous tensor [n_pages][n_kv_heads][page_size][head_dim] of bfloat16, float16 or float8_e4m3fn")
+        if v.shape != k.shape or v.dtype is not k.dtype or not v.is_contiguous():
+            raise ValueError("v: k's shape and type, contiguous")
+        if page_table.dtype is not torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
+            raise ValueError("page_table: contiguous int32 [n_seqs][pages_per_seq]")
         codes = k.dtype is torch.float8_e4m3fn
         for s in (k_scale, v_scale):
-            _need((s is not None) == codes, "k_scale and v_scale belong to float8_e4m3fn caches, and to no other")
-            _need(s is None or (s.dtype is torch.uint8 and s.shape == k.shape[:3] and s.is_contiguous()), "scales: contiguous uint8 [n_pages][n_kv_heads][page_size]")
-        _same_device(k.device, v, page_table, k_scale, v_scale)
+            if (s is not None) != codes:
+                raise ValueError("k_scale and v_scale belong to float8_e4m3fn caches, and to no other")
+            if codes and (s.dtype is not torch.uint8 or s.shape != k.shape[:3] or not s.is_contiguous()):
+                raise ValueError("scales: contiguous uint8 [n_pages][n_kv_heads][page_size]")
+        if any(t is not None and t.get_device() != device for t in (v, page_table, k_scale, v_scale)):
+            raise ValueError("tensors of one cache on several devices")
         self.k, self.v, self.page_table, self.k_scale, self.v_scale = k, v, page_table, k_scale, v_scale
-        self.device, self.dtype = k.device, k.dtype
+        self.device, self.dtype, self.index = k.device, k.dtype, device
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.n_seqs, self.pages_per_seq = page_table.shape
         self.c = nnc_paged_kv(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if codes else None, v_scale.data_ptr() if codes else None,
@@ -541,37 +556,33 @@ class PagedKV:
 def op_kv_write_paged(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, seq: Optional[torch.Tensor] = None):
     """nnc_op_kv_write_paged: rows k, v [tokens][n_kv_heads][head_dim] to positions `pos` of sequences `seq` (None: token t is
     sequence t's).  k and v have the same strides (slices of one fused projection do)."""
-    _rows(k, "k")
-    _rows(v, "v")
-    _need(k.dtype is v.dtype and k.dtype in _TYPES and k.dtype is not torch.float8_e4m3fn, "k, v: float32, bfloat16 or float16")
-    ks = k.stride()
-    tokens = k.shape[0]
-    _need(v.shape == k.shape and v.stride() == ks and k.shape[1] == cache.n_kv_heads and k.shape[2] == cache.head_dim,
-          "k, v: [tokens][n_kv_heads][head_dim] of the cache, with the same strides")
-    _same_device(cache.device, k, v, pos, seq)
-    _launch(lib.nnc_op_kv_write_paged, "nnc_op_kv_write_paged", cache.device, cache.ref, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], tokens,
-            ks[0], ks[1], _index(pos, tokens, "pos"), _index(seq, tokens, "seq") if seq is not None else None)
+    device = cache.index
+    rows = kind, row, head = _rows(k, device, "k")
+    shape = tokens, heads, d = k.shape
+    if _rows(v, device, "v") != rows or v.shape != shape or heads != cache.n_kv_heads or d != cache.head_dim:
+        raise ValueError("k, v: [tokens][n_kv_heads][head_dim] of the cache, of one type with the same strides")
+    _launch(lib.nnc_op_kv_write_paged, device, cache.ref, k.data_ptr(), v.data_ptr(), kind, tokens, row, head,
+            _index(pos, tokens, device, "pos"), None if seq is None else _index(seq, tokens, device, "seq"))
 
 
 def op_kv_read_paged(cache: PagedKV, pos: torch.Tensor, seq: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
                      out=None):
     """nnc_op_kv_read_paged: (k, v), [tokens][n_kv_heads][head_dim], of positions `pos` of sequences `seq`.  out: None (then
     padding tokens' rows hold anything), or a pair of tensors with the same strides."""
-    tokens = pos.shape[0]
+    device, tokens = cache.index, pos.shape[0]
     shape = (tokens, cache.n_kv_heads, cache.head_dim)
     if out is None:
         dtype = dtype or (torch.bfloat16 if cache.dtype is torch.float8_e4m3fn else cache.dtype)
-        k, v = torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device)
+        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        v = torch.empty_like(k)
     else:
         k, v = out
-        _rows(k, "out")
-        _rows(v, "out")
-        _need(k.shape == shape and v.shape == shape and k.stride() == v.stride() and k.dtype is v.dtype and (dtype or k.dtype) is k.dtype and _disjoint(k) and _disjoint(v),
-              "out: two tensors [tokens][n_kv_heads][head_dim] of one type with the same strides, no rows that overlap")
-    _need(k.dtype in _TYPES and k.dtype is not torch.float8_e4m3fn, "dtype: float32, bfloat16 or float16")
-    _same_device(cache.device, k, v, pos, seq)
-    _launch(lib.nnc_op_kv_read_paged, "nnc_op_kv_read_paged", cache.device, cache.ref, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], tokens,
-            k.stride(0), k.stride(1), _index(pos, tokens, "pos"), _index(seq, tokens, "seq") if seq is not None else None)
+    rows = kind, row, head = _rows(k, device, "dtype or out")
+    if out is not None and (k.shape != shape or v.shape != shape or _rows(v, device, "out") != rows or (dtype or k.dtype) is not k.dtype
+                            or not _disjoint(k) or not _disjoint(v)):
+        raise ValueError("out: two tensors [tokens][n_kv_heads][head_dim] of one type with the same strides, no rows that overlap")
+    _launch(lib.nnc_op_kv_read_paged, device, cache.ref, k.data_ptr(), v.data_ptr(), kind, tokens, row, head,
+            _index(pos, tokens, device, "pos"), None if seq is None else _index(seq, tokens, device, "seq"))
     return k, v
 
 
@@ -584,22 +595,27 @@ def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, sc
                          scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, want_lse: bool = False):
     """nnc_op_attn_decode_paged: q [batch][n_q_heads][head_dim] (rows may be apart) against the first lens[b] positions of each
     sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  Returns out, or (out, lse)."""
-    _rows(q, "q")
+    device = cache.index
+    kind, row, head = _rows(q, device, "q")
     batch, nq, d = q.shape
-    _need(q.dtype in _TYPES and q.dtype is not torch.float8_e4m3fn and d == cache.head_dim and (q.stride(1) == d or nq == 1),
-          "q: [batch][n_q_heads][head_dim] of float32, bfloat16 or float16, heads next to each other")
+    if d != cache.head_dim or (head != d and nq > 1):
+        raise ValueError("q: [batch][n_q_heads][head_dim] of the cache's head_dim, heads next to each other")
+    if batch < 2:
+        row = nq * d
     if out is None:
-        out = torch.empty((batch, nq, d), dtype=q.dtype, device=q.device)
+        out, out_row = torch.empty_like(q) if q.is_contiguous() else torch.empty((batch, nq, d), dtype=q.dtype, device=q.device), nq * d
     else:
-        _rows(out, "out")
-        _need(out.shape == q.shape and out.dtype is q.dtype and (out.stride(1) == d or nq == 1) and _disjoint(out),
-              "out: q's shape and type, heads next to each other, no rows that overlap")
-    lse = torch.empty((batch, nq), dtype=torch.float32, device=q.device) if want_lse else None
+        out_kind, out_row, out_head = _rows(out, device, "out")
+        if out.shape != q.shape or out_kind != kind or (out_head != d and nq > 1) or not _disjoint(out):
+            raise ValueError("out: q's shape and type, heads next to each other, no rows that overlap")
+        if batch < 2:
+            out_row = nq * d
+    lse = q.new_empty((batch, nq), dtype=torch.float32) if want_lse else None
     if scratch is None:
-        scratch = attn_paged_scratch(q.device)
-    _need(scratch.is_contiguous(), "scratch: a contiguous tensor (attn_paged_scratch)")
-    _same_device(cache.device, q, lens, out, scratch)
-    _launch(lib.nnc_op_attn_decode_paged, "nnc_op_attn_decode_paged", cache.device, q.data_ptr(), cache.ref, _index(lens, batch, "lens"), out.data_ptr(),
-            lse.data_ptr() if want_lse else None, _TYPES[q.dtype], batch, nq, q.stride(0), out.stride(0),
-            d ** -0.5 if scale is None else scale, window, scratch.data_ptr(), scratch.nbytes)
+        scratch = attn_paged_scratch(cache.device)
+    elif scratch.get_device() != device or not scratch.is_contiguous():
+        raise ValueError("scratch: a contiguous tensor on the call's CUDA device (attn_paged_scratch)")
+    _launch(lib.nnc_op_attn_decode_paged, device, q.data_ptr(), cache.ref, _index(lens, batch, device, "lens"), out.data_ptr(),
+            lse.data_ptr() if want_lse else None, kind, batch, nq, row, out_row, d ** -0.5 if scale is None else scale, window,
+            scratch.data_ptr(), scratch.nbytes)
     return (out, lse) if want_lse else out

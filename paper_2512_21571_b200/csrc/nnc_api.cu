@@ -734,13 +734,27 @@ int nnc_trace_dump(void *out, int max_records) {
 static __device__ int g_op_status;
 static __device__ uint32_t g_op_gemv_ctr[8][4];   // work counters of the last 8 nnc_op_gemv calls, used in rotation
 
+// What a device's calls have in common, looked up by its first one.
+struct OpDevice {
+    int sms, *status;
+    bool known;
+};
+static OpDevice g_op_devices[64];
+
 static int op_ctx(LaunchCtx &lc, void *stream) {
-    int dev = 0, sms = 0;
+    int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return NNC_ERR_CUDA;
-    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return NNC_ERR_CUDA;
-    int *status = nullptr;
-    if (cudaGetSymbolAddress((void **)&status, g_op_status) != cudaSuccess) return NNC_ERR_CUDA;
-    lc = LaunchCtx{(cudaStream_t)stream, sms, false, nullptr, status};
+    OpDevice none = {};
+    OpDevice &d = dev < 64 ? g_op_devices[dev] : none;
+    if (!__atomic_load_n(&d.known, __ATOMIC_ACQUIRE)) {   // threads that look it up at once write the same values
+        int sms = 0, *status = nullptr;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return NNC_ERR_CUDA;
+        if (cudaGetSymbolAddress((void **)&status, g_op_status) != cudaSuccess) return NNC_ERR_CUDA;
+        __atomic_store_n(&d.sms, sms, __ATOMIC_RELAXED);
+        __atomic_store_n(&d.status, status, __ATOMIC_RELAXED);
+        __atomic_store_n(&d.known, true, __ATOMIC_RELEASE);
+    }
+    lc = LaunchCtx{(cudaStream_t)stream, __atomic_load_n(&d.sms, __ATOMIC_RELAXED), false, nullptr, __atomic_load_n(&d.status, __ATOMIC_RELAXED)};
     return NNC_OK;
 }
 

@@ -255,6 +255,37 @@ def test_codes_of_rows_with_zeros_infinities_nan_and_extreme_sizes(nnc):
     assert (k[8] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_codes_of_rows_with_infinities_and_nan_anywhere(nnc, dtype, d):
+    """Every row's scale is its own finite values', whatever its neighbours in the same warp hold."""
+    g = _gen(d)
+    x = _randn(g, 40, 3, d, dtype=dtype)
+    for t in range(40):
+        for h in range(3):
+            kind = (3 * t + h) % 7
+            at = (11 * t + 5 * h) % d
+            if kind == 1: x[t, h, at] = math.inf
+            if kind == 2: x[t, h, at] = -math.inf
+            if kind == 3: x[t, h, at] = math.nan
+            if kind == 4: x[t, h, at], x[t, h, (at + 9) % d] = math.nan, math.inf
+            if kind == 5: x[t, h] = math.nan
+            if kind == 6: x[t, h] = -math.inf
+    y = x.flip(0).contiguous()
+    cache = _paged(nnc, E4M3, [40], 16, 3, d, 1)
+    pos, seq = _ints(range(40)), _ints([0] * 40)
+    nnc.op_kv_write_paged(cache, x, y, pos, seq)
+    for got, src, scale in zip(nnc.op_kv_read_paged(cache, pos, seq, dtype=F32), (x, y), (cache.k_scale, cache.v_scale)):
+        finite = src.double().where(src.isfinite(), 0.0)
+        want, e = quantise64(finite)
+        assert torch.equal(got.isnan(), src.isnan())
+        edge = 448 * power64(e)[..., None]
+        want = torch.where(src == math.inf, edge, torch.where(src == -math.inf, -edge, want))
+        assert torch.equal(got.double().where(~src.isnan(), 0.0), want.where(~src.isnan(), 0.0))
+        at = cache.page_table[0, pos.long() // 16].long(), pos.long() % 16
+        assert torch.equal(scale[at[0], :, at[1]].double() - 127, e)
+
+
 def test_16_bit_rows_are_copied_bit_for_bit(nnc):
     for t in (BF16, F16):
         cache = _paged(nnc, t, [32], 16, 2, 64, 1)
