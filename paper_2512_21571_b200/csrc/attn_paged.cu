@@ -209,6 +209,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     constexpr float kLift = BF ? 0.f : 14.f;
     extern __shared__ __align__(128) char smem[];
     __shared__ AttnShared sh;
+    pdl_launch_dependents();
+    pdl_wait();   // lengths, tables and rows may be the preceding kernel's
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     const int g8 = lane >> 2, t4 = lane & 3;
@@ -867,13 +869,9 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     const long long fit = (long long)(p.part_floats / (2 * S::kSlotFloats));
     if (ctas > fit) ctas = fit;
     if (ctas > tiles) ctas = tiles;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = S::kSmem;
-    cfg.stream = lc.stream;
-    if (lc.launches) ++*lc.launches;
-    return cudaLaunchKernelEx(&cfg, kern, p);
+    LaunchCtx early = lc;
+    early.pdl = true;   // the kernel waits for its predecessor itself
+    return launch_smem(early, kern, dim3((unsigned)ctas), dim3(kWarps * 32), (size_t)S::kSmem, p);
 }
 
 // 16-bit results: queries as one exact term, probabilities as two; fp32 results: as many terms as fp32 has bits for

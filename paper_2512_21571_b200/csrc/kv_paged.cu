@@ -114,6 +114,8 @@ __global__ void __launch_bounds__(256) kv_rows_kernel(const RowsParams p) {
     constexpr int kLanes = D / 8, kRows = 256 / kLanes;   // rows a CTA takes at once
     constexpr int kOutside = TYPE == NNC_F32 ? 32 : 16;   // bytes of a lane's eight elements outside the cache
     const int lane = threadIdx.x % kLanes;
+    pdl_launch_dependents();
+    pdl_wait();
     const unsigned rows = (unsigned)p.n_tokens * (unsigned)p.c.n_kv;
     const unsigned row0 = blockIdx.x * (unsigned)(kRows * R) + threadIdx.x / kLanes;
     int s[R], n[R], h[R], page[R];
@@ -228,11 +230,13 @@ cudaError_t launch_sized(const LaunchCtx &lc, const RowsParams &p) {
     constexpr int kRows = 256 / (D / 8);
     const long long rows = (long long)p.n_tokens * p.c.n_kv;
     const long long once = (rows + kRows - 1) / kRows;
+    LaunchCtx early = lc;
+    early.pdl = true;   // the kernel waits for its predecessor itself
     // Two rows a thread where that still leaves every SM several CTAs; otherwise one, for the shortest way through.  Reading
     // 63315 rows of 8 heads x 128 codes: 40 us with one, 33.7 with two, 34.2 with three, 34.6 with four
     if (once >= 16ll * lc.sm_count)
-        return launch(lc, kv_rows_kernel<D, KV, TYPE, WRITE, 2>, dim3((unsigned)((once + 1) / 2)), dim3(256), p);
-    return launch(lc, kv_rows_kernel<D, KV, TYPE, WRITE, 1>, dim3((unsigned)once), dim3(256), p);
+        return launch(early, kv_rows_kernel<D, KV, TYPE, WRITE, 2>, dim3((unsigned)((once + 1) / 2)), dim3(256), p);
+    return launch(early, kv_rows_kernel<D, KV, TYPE, WRITE, 1>, dim3((unsigned)once), dim3(256), p);
 }
 
 template <int D, int KV>

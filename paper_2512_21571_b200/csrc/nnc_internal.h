@@ -19,10 +19,11 @@ struct LaunchCtx {
 };
 
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch(const LaunchCtx &lc, void (*kern)(KArgs...), dim3 grid, dim3 block, Args... args) {
+inline cudaError_t launch_smem(const LaunchCtx &lc, void (*kern)(KArgs...), dim3 grid, dim3 block, size_t dynamic_smem, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = dynamic_smem;
     cfg.stream = lc.stream;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -31,6 +32,11 @@ inline cudaError_t launch(const LaunchCtx &lc, void (*kern)(KArgs...), dim3 grid
     cfg.numAttrs = lc.pdl ? 1 : 0;
     if (lc.launches) ++*lc.launches;
     return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch(const LaunchCtx &lc, void (*kern)(KArgs...), dim3 grid, dim3 block, Args... args) {
+    return launch_smem(lc, kern, grid, block, 0, args...);
 }
 
 // Raises a kernel's dynamic shared-memory limit once per device (the attribute belongs to the device's copy of the

@@ -62,6 +62,8 @@ __device__ __forceinline__ float2 turn_of(int pos, double freq, float amplitude,
 template <int TYPE, bool INTERLEAVED, int M>
 __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
     constexpr int el = TYPE == NNC_F32 ? 4 : 2;
+    pdl_launch_dependents();
+    pdl_wait();
     extern __shared__ float4 turn[];   // [tokens_per_cta][4][rot / 16]: two pairs each; lanes of one head read side by side
     const int half = p.rot / 2, rot_units = half / 8;
     const int t0 = blockIdx.x * p.tokens_per_cta, tokens = min(p.tokens_per_cta, p.n_tokens - t0);
@@ -135,6 +137,8 @@ __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
 template <int TYPE, bool INTERLEAVED>
 __global__ void __launch_bounds__(512) rope_plain_kernel(const RopeParams p) {
     typedef Scalar<TYPE> E;
+    pdl_launch_dependents();
+    pdl_wait();
     extern __shared__ float4 turn4[];
     float2 *turn = reinterpret_cast<float2 *>(turn4);   // [tokens_per_cta][rot / 2]
     const int half = p.rot / 2;
@@ -167,9 +171,9 @@ cudaError_t launch_typed(const LaunchCtx &lc, const RopeParams &p, bool vec, boo
     auto kern = !vec ? (interleaved ? rope_plain_kernel<TYPE, true> : rope_plain_kernel<TYPE, false>)
               : many ? (interleaved ? rope_kernel<TYPE, true, M> : rope_kernel<TYPE, false, M>)
                      : (interleaved ? rope_kernel<TYPE, true, 1> : rope_kernel<TYPE, false, 1>);
-    if (lc.launches) ++*lc.launches;
-    kern<<<grid, block, smem, lc.stream>>>(p);
-    return cudaGetLastError();
+    LaunchCtx early = lc;
+    early.pdl = true;   // the kernels wait for their predecessor themselves
+    return launch_smem(early, kern, grid, block, (size_t)smem, p);
 }
 
 }  // namespace
