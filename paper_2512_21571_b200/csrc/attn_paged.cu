@@ -30,9 +30,9 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr float kLn2 = 0.69314718055994530942f;
-// partial results that one CTA joins: up to kMaxJoin at once, in groups of kJoinGroup first where there are more (one SM reads
+// partial results that one CTA joins: up to Shape::kMaxJoin at once, in groups of kJoinGroup first where there are more (one SM reads
 // them at some 100 GB/s, so a long list is cheaper in two rounds)
-constexpr int kMaxJoin = 64, kJoinGroup = 24;
+constexpr int kJoinGroup = 24;
 
 struct PagedAttnParams {
     PagedView c;
@@ -50,7 +50,7 @@ struct PagedAttnParams {
 
 template <int D, int NT, int KV, int QT>
 struct Shape {
-    static constexpr int kCtas = NT == 1 && QT == 1 ? 3 : 2;   // resident per SM
+    static constexpr int kCtas = (NT == 1 && (QT == 1 || KV != NNC_BF16)) || (NT == 2 && D == 64 && QT == 1) ? 3 : 2;   // resident per SM
     static constexpr int kBytes = KV == NNC_E4M3 ? 1 : 2;
     static constexpr int kRow = D * kBytes;                  // bytes of a row
     static constexpr int kPB = kRow == 256 ? 16 : 32;        // positions of a warp's block
@@ -64,6 +64,7 @@ struct Shape {
     static constexpr int kRounds = kCtas == 3 ? kOwn : 1;    // warps hand their tiles to one another in so many rounds,
     static constexpr int kOnce = kOwn / kRounds;             // so many tiles a warp at once,
     static constexpr int kHand = kWarps * 3 * kOnce * 4 * 32 * 4;   // in so many bytes,
+    static constexpr int kMaxJoin = NT == 1 ? 64 : 32;
     static constexpr int kJoin = 8 * NT * kMaxJoin * 12 + 8 * NT * 8;   // or (m, l), weights and sums where results are joined
     static constexpr int kComb = kHand > kJoin ? kHand : kJoin;
     static constexpr int kSmem = kWarps * kStages * kStage + kComb;
@@ -746,9 +747,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     if (sh.split[0].c_lo < 0 && sh.split[1].c_lo < 0) return;
     if (tid < 2 && sh.split[tid].c_lo >= 0) {
         auto &s = sh.split[tid];
-        const int pieces = s.c_hi - s.c_lo + 1, group = pieces <= kMaxJoin ? 0 : (cta - s.c_lo) / kJoinGroup;
+        const int pieces = s.c_hi - s.c_lo + 1, group = pieces <= S::kMaxJoin ? 0 : (cta - s.c_lo) / kJoinGroup;
         const int g_lo = s.c_lo + group * kJoinGroup;
-        const int expected = pieces <= kMaxJoin ? pieces : min(kJoinGroup, s.c_hi - g_lo + 1);
+        const int expected = pieces <= S::kMaxJoin ? pieces : min(kJoinGroup, s.c_hi - g_lo + 1);
         // tickets: [0, max) for an item's first (or only) group, [max, 2 max) for its later ones (their first CTA may start another
         // item's first group), [2 max, 3 max) for the groups' results
         uint32_t *ticket = p.tickets + (group ? kPagedMaxCtas : 0) + g_lo;
@@ -758,15 +759,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     // The rows to be joined come into the ring's memory, all of them requested at once (a loop of copies and a loop of sums: this
     // code runs once, so what it costs is fetching it and one trip to memory).
     float2 *ml = reinterpret_cast<float2 *>(comb);                       // [pieces][8 NT]
-    float *wgt = reinterpret_cast<float *>(ml + kMaxJoin * 8 * NT);      // [8 NT][kMaxJoin]
-    float2 *tot = reinterpret_cast<float2 *>(wgt + kMaxJoin * 8 * NT);   // [8 NT]: M, L
+    float *wgt = reinterpret_cast<float *>(ml + S::kMaxJoin * 8 * NT);      // [8 NT][S::kMaxJoin]
+    float2 *tot = reinterpret_cast<float2 *>(wgt + S::kMaxJoin * 8 * NT);   // [8 NT]: M, L
     const uint32_t ring0 = (uint32_t)__cvta_generic_to_shared(smem), ml0 = (uint32_t)__cvta_generic_to_shared(ml);
 #pragma unroll 1
     for (int x = 0; x < 2; ++x) {
         const int c_lo = sh.split[x].c_lo, c_hi = sh.split[x].c_hi, pieces = c_hi - c_lo + 1;
         if (c_lo < 0 || !sh.split[x].last) continue;
         const int q_head = sh.split[x].q_head, cols = sh.split[x].heads_here * (D / 4), b = sh.split[x].b;
-        const bool grouped = pieces > kMaxJoin;
+        const bool grouped = pieces > S::kMaxJoin;
         int c0 = grouped ? c_lo + (cta - c_lo) / kJoinGroup * kJoinGroup : c_lo, apart = 1;   // CTAs c0, c0 + apart, ...
         int n = grouped ? min(kJoinGroup, c_hi - c0 + 1) : pieces;
 #pragma unroll 1
@@ -804,8 +805,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                         const float M = warp_max(fmaxf(u.x, v.x));
                         const float ref = M == -INFINITY ? 0.f : M;
                         const float wu = exp2f(u.x - ref), wv = exp2f(v.x - ref);
-                        if (lane < n) wgt[h * kMaxJoin + lane] = wu;
-                        if (lane + 32 < n) wgt[h * kMaxJoin + lane + 32] = wv;
+                        if (lane < n) wgt[h * S::kMaxJoin + lane] = wu;
+                        if (lane + 32 < n) wgt[h * S::kMaxJoin + lane + 32] = wv;
                         const float L = warp_sum(fmaf(wu, u.y, wv * v.y));
                         if (lane == 0) tot[h] = make_float2(M, L);
                     }
@@ -820,7 +821,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                     if (lo > 0) sum = *slot0;   // what the pieces before these gave
 #pragma unroll 4
                     for (int i = lo; i < hi; ++i) {
-                        const float w = wgt[h * kMaxJoin + i];
+                        const float w = wgt[h * S::kMaxJoin + i];
                         const float4 v = rows[(i - lo) * cols + col];
                         sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
                     }
