@@ -32,7 +32,7 @@ constexpr int kWarps = 4;
 constexpr float kLn2 = 0.69314718055994530942f;
 // partial results that one CTA joins: up to Shape::kMaxJoin at once, in groups of kJoinGroup first where there are more (one SM reads
 // them at some 100 GB/s, so a long list is cheaper in two rounds)
-constexpr int kJoinGroup = 24;
+constexpr int kJoinGroup = 16;
 
 struct PagedAttnParams {
     PagedView c;
@@ -53,12 +53,12 @@ struct Shape {
     static constexpr int kCtas = (NT == 1 && (QT == 1 || KV != NNC_BF16)) || (NT == 2 && D == 64 && QT == 1) ? 3 : 2;   // resident per SM
     static constexpr int kBytes = KV == NNC_E4M3 ? 1 : 2;
     static constexpr int kRow = D * kBytes;                  // bytes of a row
-    static constexpr int kPB = kRow == 256 ? 16 : 32;        // positions of a warp's block
+    static constexpr int kPB = 4096 / kRow;                  // positions of a warp's block: 4 KB of keys, as many of values
     static constexpr int kSub = kPB / 16;
     static constexpr int kTile = kWarps * kPB;
     static constexpr int kData = 2 * kPB * kRow;             // K rows, then V rows
     static constexpr int kStage = kData + (KV == NNC_E4M3 ? 2 * kPB : 0);   // then K scales, V scales
-    static constexpr int kStages = kCtas == 3 ? (kData == 8192 ? 2 : 4) : kData == 8192 ? 3 : 5;
+    static constexpr int kStages = kCtas == 3 ? 2 : 3;
     static constexpr int kTilesD = D / 16;                   // 16-row tiles of O^T
     static constexpr int kOwn = kTilesD / kWarps;            // tiles that a warp merges
     static constexpr int kRounds = kCtas == 3 ? kOwn : 1;    // warps hand their tiles to one another in so many rounds,
@@ -336,14 +336,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     float o[NT][S::kTilesD][4], m_run[NT][2], l_run[NT][2];
     int piece_first = now.index;   // place of the piece's first tile
 
-    // Queries of the (sequence, head) at `now`: lane (g8, t4) holds head g8's elements of contraction columns 2 t4, 2 t4 + 1, 2 t4 + 8,
+    // Queries of a (sequence, head): lane (g8, t4) holds head g8's elements of contraction columns 2 t4, 2 t4 + 1, 2 t4 + 8,
     // 2 t4 + 9 of every step of 16; with codes, a key's four neighbouring codes 4 t4 .. 4 t4 + 3 stand in those columns.
     // They are all requested before any is used, and wait as they are in the fragments' registers.
-    auto load_queries = [&]() {
+    auto load_queries = [&](const Place &at_piece) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int g = now.chunk * (8 * NT) + nt * 8 + g8;
-            const long long at = now.b * p.q_stride + (long long)(now.head * p.group + (g < p.group ? g : 0)) * D + (CODES ? 4 : 2) * t4;
+            const int g = at_piece.chunk * (8 * NT) + nt * 8 + g8;
+            const long long at = at_piece.b * p.q_stride + (long long)(at_piece.head * p.group + (g < p.group ? g : 0)) * D + (CODES ? 4 : 2) * t4;
             constexpr int kApart = CODES ? 2 : 8;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
@@ -712,9 +712,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     // One loop for filling the ring and for the steady state, so that its code exists once: a launch fetches every instruction
     // that it runs from memory.
     find_pages();
+    load_queries(now);   // before the rows: behind them in the memory system they would come last
     bool begins = true;
     for (int stage = 0, fill = 0, requests = S::kStages; now.index < t1; requests = 1) {
-        if (begins) load_queries();   // before the rows: behind them in the memory system they would come last
 #pragma unroll 1
         for (; requests > 0; --requests) {   // the stage that the step before this one used, or at first all of them
             if (ahead.index < t1) {
@@ -734,8 +734,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         products(stage);
         __syncwarp();
         begins = now.tile + 1 == now.r.tiles;
+        Place next = now;
+        step<TILE>(p, next);
+        if (begins && next.index < t1) load_queries(next);   // on their way while this piece ends
         if (begins || now.index + 1 == t1) end_piece();
-        step<TILE>(p, now);
+        now = next;
         if (begins) piece_first = now.index;
         stage = stage + 1 == S::kStages ? 0 : stage + 1;
     }
