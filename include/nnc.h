@@ -296,7 +296,8 @@ int nnc_op_attn_decode_static(const float *q, const void *kcache, const void *vc
  * (nnc_op_attn_decode_paged), read rows back (nnc_op_kv_read_paged).  Positions, sequences, page tables and lengths
  * are DEVICE arrays that a kernel reads when it runs, so a captured graph follows them from replay to replay.  Like
  * the other operations, each launches on `cuda_stream` of the current device, allocates nothing and writes only the
- * rows it names. */
+ * rows it names.  Their kernels are launched with programmatic stream serialization and wait for the preceding kernel before
+ * they read anything, so consecutive calls overlap their launches and keep their order. */
 
 typedef enum { NNC_F32 = 0, NNC_BF16 = 1, NNC_F16 = 2, NNC_E4M3 = 3 } nnc_type;
 
@@ -335,7 +336,7 @@ int nnc_op_rope(const void *x, void *y, int32_t type, int32_t n_tokens, int32_t 
  * sequence s lies in slot n % page_size of page page_table[s * pages_per_seq + n / page_size].
  *   k, v             [n_pages][n_kv_heads][page_size][head_dim] of `type` (NNC_BF16, NNC_F16 or NNC_E4M3), 16-byte aligned
  *   k_scale, v_scale NNC_E4M3 only: one byte a row, [n_pages][n_kv_heads][page_size], 16-byte aligned: the row's values
- *                    are code * 2^(byte - 127).  NULL otherwise
+ *                    are code * 2^(byte - 127), bytes of 67 .. 187 (what nnc_op_kv_write_paged writes).  NULL otherwise
  *   page_table       int32 [n_seqs][pages_per_seq]; entries that no call reaches may hold anything.  Sequences may share pages
  *                    (a common prefix) that no call writes
  *   page_size 16, 32, 64, 128 or 256; head_dim 64 or 128.
@@ -355,7 +356,7 @@ typedef struct {
  * h * head_stride + i.  16-bit caches hold the value rounded to nearest even (a row of the cache's own type is copied); an E4M3
  * row holds codes for the scale 2^e, e the smallest integer with max|x| <= 448 * 2^e over the row's finite values, kept
  * inside [-60, 60] (0 for a row without any but zeros), rounded to nearest even, saturating (infinities too); NaN stays NaN.  Pointers and
- * strides of k and v are multiples of 16 bytes. */
+ * strides of k and v are multiples of 16 bytes, and they do not overlap the cache. */
 int nnc_op_kv_write_paged(const nnc_paged_kv *cache, const void *k, const void *v, int32_t type, int32_t n_tokens,
                           int64_t row_stride, int64_t head_stride, const int32_t *pos, const int32_t *seq, void *cuda_stream);
 

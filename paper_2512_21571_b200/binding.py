@@ -460,9 +460,11 @@ def _rows(t: torch.Tensor, device: int, what: str):
     if kind == 3 or t.dim() != 3 or t.get_device() != device:
         raise ValueError(f"{what}: [tokens][heads][head_dim] of float32, bfloat16 or float16 on one CUDA device with the other tensors of the call")
     row, head, one = t.stride()
-    if one != 1:
+    tokens, heads, d = t.shape
+    if one != 1 and d > 1:
         raise ValueError(f"{what}: elements of a head next to each other")
-    return kind, row, head
+    head = head if heads > 1 else d          # strides that nothing is reached by
+    return kind, row if tokens > 1 else heads * head, head
 
 
 def _index(t: torch.Tensor, n: int, device: int, what: str) -> int:
@@ -598,18 +600,16 @@ def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, sc
     device = cache.index
     kind, row, head = _rows(q, device, "q")
     batch, nq, d = q.shape
-    if d != cache.head_dim or (head != d and nq > 1):
+    if d != cache.head_dim or head != d:
         raise ValueError("q: [batch][n_q_heads][head_dim] of the cache's head_dim, heads next to each other")
-    if batch < 2:
-        row = nq * d
+    if not 0 <= window < 1 << 31:
+        raise ValueError("window: 0 or a number of positions")
     if out is None:
         out, out_row = torch.empty_like(q) if q.is_contiguous() else torch.empty((batch, nq, d), dtype=q.dtype, device=q.device), nq * d
     else:
         out_kind, out_row, out_head = _rows(out, device, "out")
-        if out.shape != q.shape or out_kind != kind or (out_head != d and nq > 1) or not _disjoint(out):
+        if out.shape != q.shape or out_kind != kind or out_head != d or not _disjoint(out):
             raise ValueError("out: q's shape and type, heads next to each other, no rows that overlap")
-        if batch < 2:
-            out_row = nq * d
     lse = q.new_empty((batch, nq), dtype=torch.float32) if want_lse else None
     if scratch is None:
         scratch = attn_paged_scratch(cache.device)

@@ -3,23 +3,27 @@
 //   s_n = scale q.k_n,  o = sum_n exp(s_n - m) v_n / sum_n exp(s_n - m),  n over the attended positions
 //
 // Bound by reading every attended key and value row once.  How it gets there:
-//   - The work is the list of tiles (4 * PB positions of one sequence and KV head; its query heads ride along in groups of
-//     up to 16), in the order sequence, head, position.  The lengths live on the device, so every CTA adds up the list
-//     itself and takes an equal contiguous share; two CTAs are resident per SM.  A share may end inside a (sequence, head):
-//     such pieces leave partial results (m, l, o~) that the CTA finishing last joins in list order (a ticket word;
-//     nobody waits), so the result does not depend on who was last.
-//   - A warp owns PB positions of every tile and runs its own ring of shared-memory stages, filled by 16-byte asynchronous
-//     copies that run ahead across heads and sequences; no barrier in the steady state.  Rows outside the attended
-//     range are filled with zeros instead of being read, so nothing stored there can reach a product.
+//   - The work is a list of tiles (4 warps' blocks of positions of one sequence and KV head; its query heads ride along in
+//     groups of up to 16), in the order sequence, head, position, with one more place per head for what it costs to begin and
+//     to end it.  The lengths live on the device, so every CTA adds up the list itself and takes an equal contiguous share.
+//     A share may end inside a (sequence, head): such pieces leave partial results (m, l, o~) that the CTA finishing last joins in
+//     list order (a ticket word; nobody waits), so the result does not depend on who was last.
+//   - A warp owns 4 KB of key rows and as much of value rows of every tile and runs its own ring of shared-memory stages, filled by
+//     16-byte asynchronous copies that run ahead across heads and sequences; no barrier in the steady state.  Rows outside the
+//     attended range are filled with zeros instead of being read, so nothing stored there can reach a product.
+//   - Two or three CTAs per SM: three (168 registers, rings of two stages) where the products' operands fit without spilling.  61
+//     E4M3 sequences of up to 9000 positions: 112 us with two, 101.5 us with three; two operands of 128-element heads spill
+//     there and are slower (58.5 -> 64.7 us for 32 x 8192, 2 heads, 16 queries each).
 //   - Both products run on the warp-level tensor-core path in transposed form: S^T = K Q^T and O^T = V^T P^T, so 16
-//     positions (16 head-dimension elements) fill the 16-row operand and 8 query heads are the 8-column operand.  A
-//     tcgen05 tile would be 128 rows for the same 8 columns and wants its operand staged in its own layout, E4M3 codes
-//     converted first; the products take under a quarter of the issue slots at full memory rate, so that buys nothing.
+//     positions (16 head-dimension elements) fill the 16-row operand and 8 query heads are the 8-column operand: the tensor pipe is
+//     busy 13 % of the time at 95 % of the measured copy bandwidth.  A tcgen05 tile would have 128 rows for the same 8 columns,
+//     for more of a pipe that does not limit.
 //   - E4M3 codes are fp16 values exactly; key scales multiply the scores, value scales (powers of two) are added to the
-//     exponents of the probabilities that weigh the codes, so no code is ever multiplied by a scale.
+//     exponents of the probabilities that weigh the codes, so no code is ever multiplied by a scale.  (The warp-level product of
+//     8-bit operands is built from fp16 ones on this machine, at more instructions than these conversions: measured, 147 -> 179 us.)
 // Numerics: scores, maxima, sums and outputs are fp32.  Queries enter exactly (16-bit types) or as enough terms for fp32 (three
-// bf16 or two fp16 terms); probabilities as two bf16 or fp16 terms (three bf16 for fp32 results): 2^-17 or better, below the
-// rounding of a 16-bit result, where one bf16 term would be as large as it.
+// bf16 or two fp16 terms).  Probabilities: two bf16 or fp16 terms (2^-16, 2^-21), three bf16 for fp32 results of a bf16 cache; for bf16
+// results of codes one fp16 term (2^-11, an eighth of the result's own half step), where one bf16 term would be as large as it.
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
@@ -211,7 +215,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     extern __shared__ __align__(128) char smem[];
     __shared__ AttnShared sh;
     pdl_launch_dependents();
-    pdl_wait();   // lengths, tables and rows may be the preceding kernel's
+    pdl_wait();   // lengths, tables, queries and rows may be the preceding kernel's
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     const int g8 = lane >> 2, t4 = lane & 3;
@@ -287,7 +291,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         for (int u = 0; u < S::kSub; ++u) {
             pages[u] = -1;
             if (p0 + 16 * u < ahead.r.end)
-                pages[u] = __ldg(p.c.table + (long long)ahead.b * p.c.pages_per_seq + ((p0 + 16 * u) >> p.c.page_shift));
+                pages[u] = p.c.table[(long long)ahead.b * p.c.pages_per_seq + ((p0 + 16 * u) >> p.c.page_shift)];
         }
     };
     uint32_t present = 0;   // a bit per 16 positions of each stage: its page exists
@@ -878,7 +882,8 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     return launch_smem(early, kern, dim3((unsigned)ctas), dim3(kWarps * 32), (size_t)S::kSmem, p);
 }
 
-// 16-bit results: queries as one exact term, probabilities as two; fp32 results: as many terms as fp32 has bits for
+// 16-bit results: queries as one exact term, probabilities as two (one, where that is far below the result's rounding); fp32
+// results: as many terms as fp32 has bits for
 template <int D, int NT>
 cudaError_t launch_typed(const LaunchCtx &lc, const PagedAttnParams &p, int kv, int type) {
     const bool f32 = type == NNC_F32, bf16_out = type == NNC_BF16;

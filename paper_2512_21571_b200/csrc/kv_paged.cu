@@ -183,8 +183,8 @@ __global__ void __launch_bounds__(256) kv_rows_kernel(const RowsParams p) {
             uint32_t ke[R], ve[R];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                kc[i] = *reinterpret_cast<const uint2 *>(p.c.k + at[i] * D + lane * 8);
-                vc[i] = *reinterpret_cast<const uint2 *>(p.c.v + at[i] * D + lane * 8);
+                kc[i] = __ldcg(reinterpret_cast<const uint2 *>(p.c.k + at[i] * D + lane * 8));
+                vc[i] = __ldcg(reinterpret_cast<const uint2 *>(p.c.v + at[i] * D + lane * 8));
                 ke[i] = p.c.k_scale[at[i]];
                 ve[i] = p.c.v_scale[at[i]];
             }

@@ -11,8 +11,12 @@ template <int TYPE> struct Vec8 { uint4 q[TYPE == NNC_F32 ? 2 : 1]; };   // eigh
 
 template <int TYPE> __device__ __forceinline__ Vec8<TYPE> load8(const char *p) {
     Vec8<TYPE> r;
-    r.q[0] = reinterpret_cast<const uint4 *>(p)[0];
-    if constexpr (TYPE == NNC_F32) r.q[1] = reinterpret_cast<const uint4 *>(p)[1];
+    if constexpr (TYPE == NNC_F32) {   // the second vector finds the first one's sectors in L1
+        r.q[0] = reinterpret_cast<const uint4 *>(p)[0];
+        r.q[1] = reinterpret_cast<const uint4 *>(p)[1];
+    } else {
+        r.q[0] = __ldcg(reinterpret_cast<const uint4 *>(p));   // used once
+    }
     return r;
 }
 template <int TYPE> __device__ __forceinline__ void store8(char *p, const Vec8<TYPE> &r) {

@@ -642,12 +642,82 @@ def test_other_streams_and_refusals_of_the_binding(nnc, scratch):
            lambda: nnc.PagedKV(cache.k, cache.v[:1], cache.page_table),
            lambda: nnc.PagedKV(cache.k, cache.v, cache.page_table, torch.zeros(1, device="cuda"), None),
            lambda: nnc.op_rope(q, _ints([0, 1]), torch.zeros(64, device="cuda"))]
+    bad += [lambda w=w: nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch, window=w) for w in (-1, 1 << 31, 1 << 32)]
     for f in bad:
         with pytest.raises(ValueError):
             f()
     for f in (lambda: nnc.op_attn_decode_paged(q.half(), cache, _ints(lens), scratch=scratch),
               lambda: nnc.op_attn_decode_paged(q[:, :7], cache, _ints(lens), scratch=scratch),
-              lambda: nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch[:1 << 20]),
-              lambda: nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch, window=-1)):
+              lambda: nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch[:1 << 20])):
         with pytest.raises(nnc.NncError):
             f()
+
+
+@pytest.mark.parametrize("kv", [BF16, E4M3], ids=str)
+def test_calls_in_a_row_see_one_another(nnc, scratch, kv):
+    """Rotate in place, append, attend, read back, over and over on the same buffers without a pause: every call works on what the one
+    before it left, although their launches overlap."""
+    heads, group, d, batch = 2, 2, 64, 300
+    cache = _paged(nnc, kv, [200] * batch, 16, heads, d, 5)
+    freq, _ = nnc.rope_frequencies(d)
+    g = _gen(23)
+    fused = _randn(g, batch, heads * (group + 2), d, dtype=BF16)
+    start = fused.clone()
+    nq, rounds = heads * group, 60
+    seq = torch.arange(batch, device="cuda", dtype=torch.int32)
+    pos = [torch.full((batch,), i, dtype=torch.int32, device="cuda") for i in range(rounds)]
+    lens = [p + 1 for p in pos]
+    outs, rows, turned = [], [], []
+    for i in range(rounds):
+        nnc.op_rope(fused[:, :nq + heads], pos[i], freq, out=fused[:, :nq + heads])        # turns the last round's result further
+        nnc.op_kv_write_paged(cache, fused[:, nq:nq + heads], fused[:, nq + heads:], pos[i], seq)
+        outs.append(nnc.op_attn_decode_paged(fused[:, :nq], cache, lens[i], scratch=scratch, want_lse=True))
+        rows.append(nnc.op_kv_read_paged(cache, pos[i], seq, dtype=F32)[0])
+        turned.append(fused[:, :nq + heads].clone())
+    torch.cuda.synchronize()
+    x = start.clone()
+    hold = (lambda t: quantise64(t)[0]) if kv is E4M3 else (lambda t: t.double())
+    keys = []
+    for i in range(rounds):
+        x[:, :nq + heads] = nnc.op_rope(x[:, :nq + heads], pos[i], freq)
+        torch.cuda.synchronize()
+        assert torch.equal(turned[i], x[:, :nq + heads])
+        keys.append(hold(x[:, nq:nq + heads]))
+        assert torch.equal(rows[i].double(), keys[-1])
+    for i in (0, 1, 2, 17, 31, rounds - 1):
+        k = torch.stack(keys[:i + 1], 2)                                                    # [batch][heads][positions][d]
+        v = hold(start[:, nq + heads:])[:, :, None].expand(-1, -1, i + 1, -1)
+        _check_attention(outs[i][0][:40], outs[i][1][:40], turned[i][:40, :nq], (k, v), [i + 1] * 40, d ** -0.5, 0, kv)
+    assert nnc.op_status() == 0
+
+
+def test_first_calls_may_be_captured(tmp_path):
+    """A process whose first calls of the operations lie inside a stream capture."""
+    import subprocess
+    import sys
+    prog = tmp_path / "child.py"
+    prog.write_text("""
+import sys, torch
+sys.path[:0] = [%r, %r]
+from paper_2512_21571_b200 import binding as nnc
+cache = nnc.PagedKV.empty(4, 16, 1, 64, torch.bfloat16, 1, 2)
+cache.page_table[0] = torch.arange(2)
+x = torch.randn(1, 2, 64, device="cuda").to(torch.bfloat16)
+pos, lens = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+freq, _ = nnc.rope_frequencies(64)
+scratch = nnc.attn_paged_scratch()
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    y = nnc.op_rope(x, pos, freq)
+    nnc.op_kv_write_paged(cache, y[:, :1], y[:, 1:], pos)
+    out = nnc.op_attn_decode_paged(y, cache, lens, scratch=scratch)
+    k, v = nnc.op_kv_read_paged(cache, pos)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(y, x) and torch.equal(k, x[:, :1]) and torch.equal(v, x[:, 1:])
+assert torch.equal(out, x[:, 1:].expand(-1, 2, -1)) and nnc.op_status() == 0
+print("captured")
+""" % (__file__.rsplit("/tests/", 1)[0], __file__.rsplit("/tests/", 1)[0] + "/tests"))
+    r = subprocess.run([sys.executable, str(prog)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stdout + r.stderr
