@@ -48,7 +48,7 @@ struct PagedAttnParams {
     uint32_t *tickets;
     size_t part_floats;
     long long q_stride, out_stride;   // elements
-    int batch, group, chunks, window;   // chunks: groups of NT * 8 query heads per KV head
+    int batch, group, chunks, window;   // chunks: groups of NT * 8 query heads per KV head, one row of the grid each
     float scale_log2;
 };
 
@@ -168,7 +168,7 @@ template <int TILE> __device__ __forceinline__ Reach reach_of(const PagedAttnPar
 // a tile, and its place in the list
 struct Place {
     Reach r;
-    int b, head, chunk, tile;   // head: KV head; chunk: which 8 NT of its query heads
+    int b, head, tile;   // head: KV head
     int index;
 };
 template <int TILE> __device__ __forceinline__ void step(const PagedAttnParams &p, Place &at) {
@@ -176,8 +176,6 @@ template <int TILE> __device__ __forceinline__ void step(const PagedAttnParams &
     if (++at.tile < at.r.tiles) return;
     ++at.index;
     at.tile = 0;
-    if (++at.chunk < p.chunks) return;
-    at.chunk = 0;
     if (++at.head < p.c.n_kv) return;
     at.head = 0;
     do {
@@ -220,7 +218,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     const int g8 = lane >> 2, t4 = lane & 3;
     // ---- the list: how many places there are, and where this CTA's share begins ----
-    const int heads = p.c.n_kv * p.chunks, most = p.c.pages_per_seq << p.c.page_shift;
+    const int heads = p.c.n_kv, most = p.c.pages_per_seq << p.c.page_shift;
     const int per = (p.batch + kWarps * 32 - 1) / (kWarps * 32);
     const int b_lo = min(tid * per, p.batch), b_hi = min(b_lo + per, p.batch);
     int mine = 0, odd = 0;   // odd: an empty sequence, or a length that does not fit
@@ -237,7 +235,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     }
     if (lane == 31) sh.sums[warp] = incl;
     if (__syncthreads_or(odd)) {   // zeros for sequences with nothing to attend to; lengths that do not fit are reported
-        for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+        for (int b = blockIdx.y == 0 ? blockIdx.x : p.batch; b < p.batch; b += gridDim.x) {
             const int len = p.lens[b], n_q = p.c.n_kv * p.group;
             if (len > most && tid == 0) paged_complain(p.c);
             if (len > 0) continue;
@@ -250,7 +248,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sh.sums[w]; all += sh.sums[w]; }
     const int total = all * heads;                             // places; the host bounds them by 2^30
     const int share = (total + gridDim.x - 1) / gridDim.x;     // of every CTA but the last ones
-    const int cta = blockIdx.x;
+    const int cta = blockIdx.x, chunk = blockIdx.y;            // chunk: which 8 NT query heads of every KV head
+    float *const part = p.part + (size_t)chunk * gridDim.x * 2 * S::kSlotFloats;
+    uint32_t *const tickets = p.tickets + chunk * gridDim.x;
     if ((long long)cta * share >= total) return;
     const int t0 = cta * share, t1 = min(t0 + share, total);
     {
@@ -272,10 +272,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     ahead.b = sh.first_b;
     ahead.r = reach_of<TILE>(p, p.lens[ahead.b]);
     {
-        const int at = sh.first_rest / ahead.r.places();
-        ahead.tile = sh.first_rest - at * ahead.r.places();
-        ahead.head = at / p.chunks;
-        ahead.chunk = at - ahead.head * p.chunks;
+        ahead.head = sh.first_rest / ahead.r.places();
+        ahead.tile = sh.first_rest - ahead.head * ahead.r.places();
     }
     ahead.index = t0;
     if (ahead.tile == ahead.r.tiles) { --ahead.index; --ahead.tile; step<TILE>(p, ahead); }   // the place after its tiles
@@ -346,7 +344,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     auto load_queries = [&](const Place &at_piece) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int g = at_piece.chunk * (8 * NT) + nt * 8 + g8;
+            const int g = chunk * (8 * NT) + nt * 8 + g8;
             const long long at = at_piece.b * p.q_stride + (long long)(at_piece.head * p.group + (g < p.group ? g : 0)) * D + (CODES ? 4 : 2) * t4;
             constexpr int kApart = CODES ? 2 : 8;
 #pragma unroll
@@ -366,7 +364,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     auto begin_piece = [&]() {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const bool there = now.chunk * (8 * NT) + nt * 8 + g8 < p.group;
+            const bool there = chunk * (8 * NT) + nt * 8 + g8 < p.group;
             float f[D / 16][4];
 #pragma unroll
             for (int s = 0; s < D / 16; ++s)
@@ -426,7 +424,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     auto prefetch_queries = [&]() {
         constexpr int size = TYPE == NNC_F32 ? 4 : 2;
         const int at = (warp * 32 + lane) * 128;   // a line each
-        const int q_head = ahead.head * p.group + ahead.chunk * (8 * NT), heads_here = min(8 * NT, p.group - ahead.chunk * (8 * NT));
+        const int q_head = ahead.head * p.group + chunk * (8 * NT), heads_here = min(8 * NT, p.group - chunk * (8 * NT));
         if (at < heads_here * D * size)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(p.q + (ahead.b * p.q_stride + (long long)q_head * D) * size + at));
     };
@@ -623,11 +621,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         const int item_lo = now.index - now.tile, item_hi = item_lo + now.r.tiles;   // places of this (sequence, head)'s tiles
         const int first = piece_first;
         const bool whole = first == item_lo && now.index + 1 == item_hi;
-        const int q_head = now.head * p.group + now.chunk * (8 * NT), heads_here = min(8 * NT, p.group - now.chunk * (8 * NT));
+        const int q_head = now.head * p.group + chunk * (8 * NT), heads_here = min(8 * NT, p.group - chunk * (8 * NT));
         const long long out_at = now.b * p.out_stride + (long long)q_head * D, lse_at = (long long)now.b * (p.c.n_kv * p.group) + q_head;
         // partial results: slot 0 of a CTA for a piece that continues an earlier CTA's, slot 1 for one that starts here
-        float *slot = p.part + (size_t)(2 * cta + (first == item_lo ? 1 : 0)) * S::kSlotFloats;
-        if (!whole && !NNC_BC((size_t)(2 * cta + 2) * S::kSlotFloats <= p.part_floats, 3201)) return;
+        float *slot = part + (size_t)(2 * cta + (first == item_lo ? 1 : 0)) * S::kSlotFloats;
+        if (!whole && !NNC_BC((size_t)(2 * (chunk * gridDim.x + cta) + 2) * S::kSlotFloats <= p.part_floats, 3201)) return;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -759,7 +757,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         const int expected = pieces <= S::kMaxJoin ? pieces : min(kJoinGroup, s.c_hi - g_lo + 1);
         // tickets: [0, max) for an item's first (or only) group, [max, 2 max) for its later ones (their first CTA may start another
         // item's first group), [2 max, 3 max) for the groups' results
-        uint32_t *ticket = p.tickets + (group ? kPagedMaxCtas : 0) + g_lo;
+        uint32_t *ticket = tickets + (group ? kPagedMaxCtas : 0) + g_lo;
         s.last = take_ticket(ticket, expected);
     }
     __syncthreads();
@@ -780,8 +778,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
 #pragma unroll 1
         for (bool final = !grouped;;) {
             // the first piece of a (sequence, head) lies in its CTA's slot 1, the others in slot 0
-            float *const slot_a = p.part + (size_t)(2 * c0 + (c0 == c_lo ? 1 : 0)) * S::kSlotFloats;
-            const float *const slot_b = p.part + (size_t)(2 * c0) * S::kSlotFloats;   // the i-th from there, i > 0
+            float *const slot_a = part + (size_t)(2 * c0 + (c0 == c_lo ? 1 : 0)) * S::kSlotFloats;
+            const float *const slot_b = part + (size_t)(2 * c0) * S::kSlotFloats;   // the i-th from there, i > 0
             const size_t step = (size_t)(2 * apart) * S::kSlotFloats;
             for (int i = tid; i < n * 4 * NT; i += kWarps * 32) {   // 16 bytes: two heads' words
                 const int from = i / (4 * NT);
@@ -854,7 +852,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
             __syncthreads();   // what is copied next goes where these weights and rows are
             if (final) break;
             const int groups = (pieces + kJoinGroup - 1) / kJoinGroup;
-            if (tid == 0) sh.split[x].last = take_ticket(p.tickets + 2 * kPagedMaxCtas + c_lo, groups);
+            if (tid == 0) sh.split[x].last = take_ticket(tickets + 2 * kPagedMaxCtas + c_lo, groups);
             __syncthreads();
             if (!sh.split[x].last) break;
             c0 = c_lo; apart = kJoinGroup; n = groups; final = true;
@@ -870,16 +868,20 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     cudaError_t e = ensure_dynamic_smem(kern, S::kSmem, &raised);
     if (e != cudaSuccess) return e;
     const long long most = ((long long)p.c.pages_per_seq << p.c.page_shift);
-    const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile + 1) * p.batch * p.c.n_kv * p.chunks;   // the longest list the table allows
+    const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile + 1) * p.batch * p.c.n_kv;   // the longest list the table allows
     if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
     long long ctas = (long long)S::kCtas * lc.sm_count;
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
     const long long fit = (long long)(p.part_floats / (2 * S::kSlotFloats));
     if (ctas > fit) ctas = fit;
+    // Query heads beyond one CTA's go to CTAs of their own that take the same shares at the same time, so that a row that the one
+    // has read from memory is in L2 for the others
+    ctas /= p.chunks;
     if (ctas > tiles) ctas = tiles;
+    if (ctas < 1) ctas = 1;
     LaunchCtx early = lc;
     early.pdl = true;   // the kernel waits for its predecessor itself
-    return launch_smem(early, kern, dim3((unsigned)ctas), dim3(kWarps * 32), (size_t)S::kSmem, p);
+    return launch_smem(early, kern, dim3((unsigned)ctas, (unsigned)p.chunks), dim3(kWarps * 32), (size_t)S::kSmem, p);
 }
 
 // 16-bit results: queries as one exact term, probabilities as two (one, where that is far below the result's rounding); fp32
@@ -907,8 +909,13 @@ cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_page
     p.batch = batch; p.window = window;
     p.group = n_q_heads / cache.n_kv_heads;
     p.scale_log2 = scale * 1.4426950408889634f;
-    const bool two = p.group > 8;   // one 8-column operand, or two, that share every key and value fragment
-    p.chunks = two ? (p.group + 15) / 16 : 1;
+    // Query heads in groups of 8.  Two groups as two operands of one CTA share every key and value fragment: 32 x 8192 E4M3 of 64
+    // elements, 16 heads: 45.5 us against 55.6 with a CTA each.  Not with an odd number of groups, where half of the last pair would be
+    // empty (64 x 8192, 17 heads: 89.7 us in pairs, 76 apart), and not where few (sequence, head)s share the whole GPU, whose
+    // joins are half as large apart (one of 131072, 16 heads: 32.7 and 25.7 us).
+    const int eights = (p.group + 7) / 8;
+    const bool two = eights % 2 == 0 && (long long)batch * cache.n_kv_heads >= 16;
+    p.chunks = two ? eights / 2 : eights;
     if (cache.head_dim == 64) return two ? launch_typed<64, 2>(lc, p, cache.type, type) : launch_typed<64, 1>(lc, p, cache.type, type);
     return two ? launch_typed<128, 2>(lc, p, cache.type, type) : launch_typed<128, 1>(lc, p, cache.type, type);
 }

@@ -1033,6 +1033,7 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
                              void *scratch, size_t scratch_bytes, void *cuda_stream) {
     if (!paged_ok(cache) || batch < 0 || batch > cache->n_seqs || window < 0) return NNC_ERR_INVALID_ARG;
     if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads) return NNC_ERR_INVALID_ARG;
+    if (n_q_heads / cache->n_kv_heads > 65535 * 8) return NNC_ERR_CAPACITY;   // rows of the grid
     if (type != NNC_F32 && type != NNC_BF16 && type != NNC_F16) return NNC_ERR_INVALID_ARG;
     if (cache->type != NNC_E4M3 && type != NNC_F32 && type != cache->type) return NNC_ERR_INVALID_ARG;
     if (batch == 0) return NNC_OK;

@@ -398,7 +398,8 @@ TYPES = [(BF16, BF16), (F16, F16), (E4M3, BF16), (E4M3, F16), (BF16, F32), (F16,
 
 @pytest.mark.parametrize("kv,dtype", TYPES, ids=str)
 @pytest.mark.parametrize("heads,group,d,page,window", [(1, 1, 128, 16, 0), (2, 4, 128, 64, 0), (8, 2, 64, 32, 0), (1, 8, 64, 256, 0), (2, 7, 128, 128, 100),
-                                                       (1, 9, 64, 16, 0), (2, 16, 128, 64, 33), (1, 17, 128, 32, 0), (1, 40, 64, 64, 1), (3, 5, 64, 16, 250)])
+                                                       (1, 9, 64, 16, 0), (2, 16, 128, 64, 33), (1, 17, 128, 32, 0), (1, 40, 64, 64, 1), (3, 5, 64, 16, 250),
+                                                       (2, 12, 64, 32, 0), (3, 32, 64, 256, 90), (2, 31, 128, 16, 0)])
 def test_attention(nnc, scratch, kv, dtype, heads, group, d, page, window):
     lens = [0, 1, 15, 16, 17, 64, 0, 65, 127, 129, 700, 3]
     cache = _paged(nnc, kv, lens, page, heads, d, heads * 100 + group)
@@ -419,7 +420,7 @@ def test_attention(nnc, scratch, kv, dtype, heads, group, d, page, window):
 
 
 @pytest.mark.parametrize("kv,dtype", [(BF16, BF16), (E4M3, F32), (F16, F16)], ids=str)
-@pytest.mark.parametrize("batch,heads,group,length", [(1, 8, 4, 5000), (1, 1, 16, 30011), (300, 2, 2, 33), (37, 4, 3, 1024)])
+@pytest.mark.parametrize("batch,heads,group,length", [(1, 8, 4, 5000), (1, 1, 16, 30011), (300, 2, 2, 33), (37, 4, 3, 1024), (20, 1, 16, 2500), (8, 2, 32, 3001), (2, 1, 80, 9000)])
 def test_attention_split_over_many_and_few_ctas(nnc, scratch, kv, dtype, batch, heads, group, length):
     lens = [length - (b * 37) % length for b in range(batch)]
     cache = _paged(nnc, kv, lens, 64, heads, 128, batch)
