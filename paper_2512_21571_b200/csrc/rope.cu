@@ -1,11 +1,14 @@
 // Rotary positions on rows of heads: y = R(position * freq) x on the first rotary_dim elements of every head.
 //
 // Bound by reading x and writing y.  The angles depend on the token and the pair only, so a CTA works out the cosines and
-// sines of its tokens once, in shared memory, and all heads use them.  A thread owns eight pairs of one head (two 16-byte
+// sines of its tokens once, in shared memory, and all heads use them.  A thread owns up to eight pairs of one head (two 16-byte
 // loads and stores of 16-bit values) in several tokens, whose loads are on their way while the angles are worked out.  The
 // angle is position * freq in 64 bits, reduced to an eighth of a turn before it is rounded to fp32: what is left then is off by
 // at most 2^-28 turns, however far the position.
-#include "vec8.cuh"
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "nnc_internal.h"
 
 namespace nnc {
 
@@ -25,6 +28,56 @@ struct RopeParams {
 
 // tokens whose loads a thread has in flight when there are many
 template <int TYPE> constexpr int kMany = TYPE == NNC_F32 ? 2 : 3;
+
+// N neighbouring elements
+template <int TYPE, int N> struct Piece {
+    static constexpr int kWords = N * (TYPE == NNC_F32 ? 4 : 2) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char *p) {
+        if constexpr (kWords >= 4) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) {
+                // 16-bit values are used once; the second vector of fp32 values finds the first one's sectors in L1
+                const uint4 v = kWords == 4 ? __ldcg(reinterpret_cast<const uint4 *>(p)) : reinterpret_cast<const uint4 *>(p)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (kWords == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x; w[1] = v.y;
+        } else {
+            w[0] = *reinterpret_cast<const uint32_t *>(p);
+        }
+    }
+    __device__ __forceinline__ void store(char *p) const {
+        if constexpr (kWords >= 4) {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) reinterpret_cast<uint4 *>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        } else if constexpr (kWords == 2) {
+            *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        } else {
+            *reinterpret_cast<uint32_t *>(p) = w[0];
+        }
+    }
+    __device__ __forceinline__ void get(float (&f)[N]) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (TYPE == NNC_F32) f[i] = __uint_as_float(w[i]);
+            else if constexpr (TYPE == NNC_BF16) f[i] = i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+            else f[i] = __half2float(__ushort_as_half((uint16_t)(w[i / 2] >> (16 * (i & 1)))));
+        }
+    }
+    __device__ __forceinline__ void put(const float (&f)[N]) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (TYPE == NNC_F32) w[i] = __float_as_uint(f[i]);
+            else if constexpr (TYPE == NNC_BF16) w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+            else {
+                const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+    }
+};
 
 template <int TYPE> struct Scalar {
     typedef uint16_t raw;
@@ -57,36 +110,36 @@ __device__ __forceinline__ float2 turn_of(int pos, double freq, float amplitude,
     return make_float2(c * amplitude, s * amplitude);
 }
 
-// Vector form: a unit is eight pairs (or, past the rotated part, eight elements that only pass through).  Thread: one unit of
-// one head (more, if a token has more units than the CTA has threads), in M tokens.
-template <int TYPE, bool INTERLEAVED, int M>
+// Vector form: a unit is N pairs (or, past the rotated part, N elements that only pass through).  Thread: one unit of one head
+// (more, if a token has more units than the CTA has threads), in M tokens.
+template <int TYPE, bool INTERLEAVED, int N, int M>
 __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
     constexpr int el = TYPE == NNC_F32 ? 4 : 2;
     pdl_launch_dependents();
     pdl_wait();
-    extern __shared__ float4 turn[];   // [tokens_per_cta][4][rot / 16]: two pairs each; lanes of one head read side by side
-    const int half = p.rot / 2, rot_units = half / 8;
+    extern __shared__ float4 turn[];   // [tokens_per_cta][N / 2][rot / 2N]: two pairs each; lanes of one head read side by side
+    const int half = p.rot / 2, rot_units = half / N;
     const int t0 = blockIdx.x * p.tokens_per_cta, tokens = min(p.tokens_per_cta, p.n_tokens - t0);
     const int per_token = p.n_heads * p.units;
     const int first = threadIdx.x / per_token;                       // the thread's first token; past it, every abreast-th
     const int each = p.abreast > 1 ? per_token : (int)blockDim.x;    // units that the CTA's threads cover of a token
-    Vec8<TYPE> a[M], b[M];
+    Piece<TYPE, N> a[M], b[M];
     long long x_at = 0, y_at = 0;
     int u = 0, at_a = 0, at_b = 0;
     auto load = [&](int r) {
         const int h = r / p.units;
         u = r - h * p.units;
-        if (u >= rot_units) at_a = at_b = p.rot + 8 * (u - rot_units);
-        else if (INTERLEAVED) { at_a = 16 * u; at_b = at_a + 8; }
-        else { at_a = 8 * u; at_b = half + 8 * u; }
+        if (u >= rot_units) at_a = at_b = p.rot + N * (u - rot_units);
+        else if (INTERLEAVED) { at_a = 2 * N * u; at_b = at_a + N; }
+        else { at_a = N * u; at_b = half + N * u; }
         x_at = (long long)(t0 + first) * p.x_row + h * p.x_head;
         y_at = (long long)(t0 + first) * p.y_row + h * p.y_head;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             if (first + m * p.abreast >= tokens) break;
             const char *x = p.x + (x_at + (long long)(m * p.abreast) * p.x_row) * el;
-            a[m] = load8<TYPE>(x + at_a * el);
-            if (u < rot_units) b[m] = load8<TYPE>(x + at_b * el);
+            a[m].load(x + at_a * el);
+            if (u < rot_units) b[m].load(x + at_b * el);
         }
     };
     int r = threadIdx.x - first * per_token;
@@ -94,7 +147,7 @@ __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
     if (in) load(r);
     for (int k = threadIdx.x; k < tokens * half; k += blockDim.x) {
         const int t = k / half, i = k - t * half;
-        reinterpret_cast<float2 *>(turn)[((t * 4 + (i & 7) / 2) * rot_units + i / 8) * 2 + (i & 1)] =
+        reinterpret_cast<float2 *>(turn)[((t * (N / 2) + i % N / 2) * rot_units + i / N) * 2 + (i & 1)] =
             turn_of(p.pos[t0 + t], p.freq[i], p.amplitude, p.inverse);
     }
     __syncthreads();
@@ -106,26 +159,27 @@ __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
             if (t >= tokens) break;
             char *y = p.y + (y_at + (long long)(m * p.abreast) * p.y_row) * el;
             if (u < rot_units) {
-                float fa[8], fb[8];
-                unpack8<TYPE>(a[m], fa);
-                unpack8<TYPE>(b[m], fb);
+                float fa[N], fb[N];
+                a[m].get(fa);
+                b[m].get(fb);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float4 cs = turn[(t * 4 + q) * rot_units + u];   // pairs 2q and 2q + 1
+                for (int q = 0; q < N / 2; ++q) {
+                    const float4 cs = turn[(t * (N / 2) + q) * rot_units + u];   // pairs 2q and 2q + 1
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int j = 2 * q + e;
-                        float &xa = INTERLEAVED ? (j < 4 ? fa[2 * j & 7] : fb[2 * j & 7]) : fa[j];
-                        float &xb = INTERLEAVED ? (j < 4 ? fa[(2 * j & 7) + 1] : fb[(2 * j & 7) + 1]) : fb[j];
+                        float &xa = INTERLEAVED ? (j < N / 2 ? fa[2 * j % N] : fb[2 * j % N]) : fa[j];
+                        float &xb = INTERLEAVED ? (j < N / 2 ? fa[2 * j % N + 1] : fb[2 * j % N + 1]) : fb[j];
                         const float c = e ? cs.z : cs.x, s = e ? cs.w : cs.y, va = xa, vb = xb;
                         xa = va * c - vb * s;
                         xb = vb * c + va * s;
                     }
                 }
-                a[m] = pack8<TYPE>(fa);
-                store8<TYPE>(y + at_b * el, pack8<TYPE>(fb));
+                a[m].put(fa);
+                b[m].put(fb);
+                b[m].store(y + at_b * el);
             }
-            store8<TYPE>(y + at_a * el, a[m]);
+            a[m].store(y + at_a * el);
         }
         r += each;
         if (r >= per_token) break;
@@ -165,15 +219,25 @@ __global__ void __launch_bounds__(512) rope_plain_kernel(const RopeParams p) {
     }
 }
 
-template <int TYPE>
-cudaError_t launch_typed(const LaunchCtx &lc, const RopeParams &p, bool vec, bool many, bool interleaved, dim3 grid, dim3 block, int smem) {
+template <int TYPE, int N>
+cudaError_t launch_sized(const LaunchCtx &lc, const RopeParams &p, bool many, bool interleaved, dim3 grid, dim3 block, int smem) {
     constexpr int M = kMany<TYPE>;
-    auto kern = !vec ? (interleaved ? rope_plain_kernel<TYPE, true> : rope_plain_kernel<TYPE, false>)
-              : many ? (interleaved ? rope_kernel<TYPE, true, M> : rope_kernel<TYPE, false, M>)
-                     : (interleaved ? rope_kernel<TYPE, true, 1> : rope_kernel<TYPE, false, 1>);
     LaunchCtx early = lc;
     early.pdl = true;   // the kernels wait for their predecessor themselves
-    return launch_smem(early, kern, grid, block, (size_t)smem, p);
+    if constexpr (N == 1) return launch_smem(early, interleaved ? rope_plain_kernel<TYPE, true> : rope_plain_kernel<TYPE, false>, grid, block, (size_t)smem, p);
+    else
+        return launch_smem(early, many ? (interleaved ? rope_kernel<TYPE, true, N, M> : rope_kernel<TYPE, false, N, M>)
+                                       : (interleaved ? rope_kernel<TYPE, true, N, 1> : rope_kernel<TYPE, false, N, 1>), grid, block, (size_t)smem, p);
+}
+
+template <int TYPE>
+cudaError_t launch_typed(const LaunchCtx &lc, const RopeParams &p, int n, bool many, bool interleaved, dim3 grid, dim3 block, int smem) {
+    switch (n) {
+        case 8: return launch_sized<TYPE, 8>(lc, p, many, interleaved, grid, block, smem);
+        case 4: return launch_sized<TYPE, 4>(lc, p, many, interleaved, grid, block, smem);
+        case 2: return launch_sized<TYPE, 2>(lc, p, many, interleaved, grid, block, smem);
+        default: return launch_sized<TYPE, 1>(lc, p, many, interleaved, grid, block, smem);
+    }
 }
 
 }  // namespace
@@ -188,11 +252,17 @@ cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, i
     p.n_tokens = n_tokens; p.n_heads = n_heads; p.rot = rotary_dim;
     p.amplitude = amplitude; p.inverse = inverse;
     const bool copy_rest = x != y && rotary_dim < head_dim;
-    // vectors need whole groups of eight pairs, whole pieces of eight of what passes through, and 16-byte rows and heads
-    bool vec = half % 8 == 0 && head_dim % 8 == 0 && !(((uintptr_t)x | (uintptr_t)y) & 15);
-    for (int64_t s : {x_row, x_head, y_row, y_head}) vec = vec && (s * el) % 16 == 0;
-    p.units = vec ? half / 8 : half;
-    if (copy_rest) p.units += vec ? (head_dim - rotary_dim) / 8 : head_dim - rotary_dim;
+    // the largest piece of n elements that pairs, what passes through, pointers and strides are all whole multiples of (16-byte
+    // vectors at most).  8192 x 40 heads of 80 bf16: 20 of them turned 57 us with n = 2, 40 turned 38 with n = 4; 99 and 88 with n = 1
+    int n = 8;
+    for (; n > 1; n /= 2) {
+        const int bytes = n * el < 16 ? n * el : 16;
+        bool fits = half % n == 0 && head_dim % n == 0 && !(((uintptr_t)x | (uintptr_t)y) % bytes);
+        for (int64_t s : {x_row, x_head, y_row, y_head}) fits = fits && (s * el) % bytes == 0;
+        if (fits) break;
+    }
+    p.units = half / n;
+    if (copy_rest) p.units += (head_dim - rotary_dim) / n;
     const long long per_token = (long long)n_heads * p.units;
     // A CTA's threads take one token abreast where that gives them 128 units or more, and else as many as give 256.  With enough
     // tokens for several CTAs per SM a thread has kMany of them in flight; otherwise one, for the shortest way through.
@@ -202,16 +272,16 @@ cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, i
     long long threads = abreast * per_token;
     if (threads > 512) threads = 512;
     p.abreast = (int)abreast;
-    const bool many = vec && n_tokens >= 4ll * abreast * m * lc.sm_count;
+    const bool many = n > 1 && n_tokens >= 4ll * abreast * m * lc.sm_count;
     long long tokens = abreast * (many ? m : 1);
-    if (!vec) tokens = 1;
+    if (n == 1) tokens = 1;
     p.tokens_per_cta = (int)tokens;
     const dim3 grid((unsigned)((n_tokens + tokens - 1) / tokens)), block((unsigned)((threads + 31) / 32 * 32));
     const int smem = (int)(tokens * half * sizeof(float2));
     switch (type) {
-        case NNC_F32: return launch_typed<NNC_F32>(lc, p, vec, many, interleaved, grid, block, smem);
-        case NNC_BF16: return launch_typed<NNC_BF16>(lc, p, vec, many, interleaved, grid, block, smem);
-        default: return launch_typed<NNC_F16>(lc, p, vec, many, interleaved, grid, block, smem);
+        case NNC_F32: return launch_typed<NNC_F32>(lc, p, n, many, interleaved, grid, block, smem);
+        case NNC_BF16: return launch_typed<NNC_BF16>(lc, p, n, many, interleaved, grid, block, smem);
+        default: return launch_typed<NNC_F16>(lc, p, n, many, interleaved, grid, block, smem);
     }
 }
 

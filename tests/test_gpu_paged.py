@@ -72,7 +72,9 @@ def _check_rope(y, x, pos, freq, **kw):
 @pytest.mark.parametrize("dtype", [BF16, F16, F32], ids=str)
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("tokens,heads,d,rot", [(1, 1, 64, 64), (1, 40, 128, 128), (3, 5, 80, 20), (7, 3, 96, 48), (5, 2, 66, 66), (2, 3, 9, 2),
-                                                (33, 1, 256, 128), (17, 70, 192, 64), (301, 2, 128, 32), (2, 2, 1024, 1024)])
+                                                (33, 1, 256, 128), (17, 70, 192, 64), (301, 2, 128, 32), (2, 2, 1024, 1024),
+                                                (5, 3, 96, 24), (7, 2, 84, 40), (1801, 33, 128, 128), (2003, 24, 96, 48), (1999, 40, 80, 20),
+                                                (2500, 30, 96, 24), (40001, 1, 64, 64), (9001, 3, 40, 8)])
 def test_rope(nnc, dtype, interleaved, tokens, heads, d, rot):
     g = _gen(tokens * 1000 + d)
     x = _randn(g, tokens, heads, d, dtype=dtype)
@@ -652,6 +654,28 @@ def test_other_streams_and_refusals_of_the_binding(nnc, scratch):
               lambda: nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch[:1 << 20])):
         with pytest.raises(nnc.NncError):
             f()
+
+
+def test_lists_past_their_count_are_refused_and_long_tables_are_not(nnc, scratch):
+    """Tables that reach 2^30 positions: the list of tiles they allow is refused where it passes 2^30, and costs nothing else."""
+    k, v = (torch.zeros(3, 1024, 16, 64, dtype=BF16, device="cuda") for _ in range(2))
+    table = torch.full((2, 1 << 26), -1, dtype=torch.int32, device="cuda")
+    table[0, :2] = _ints([2, 0])
+    table[1, -1] = 1
+    cache = nnc.PagedKV(k, v, table[:, :1 << 22].contiguous())
+    with pytest.raises(nnc.NncError) as e:
+        nnc.op_attn_decode_paged(torch.zeros(2, 1024, 64, dtype=BF16, device="cuda"), cache, _ints([1, 1]), scratch=scratch)
+    assert e.value.status == -3
+    few = nnc.PagedKV(k.view(3 * 1024, 1, 16, 64), v.view(3 * 1024, 1, 16, 64), table[:, :67000000].contiguous())
+    x = _randn(_gen(1), 2, 1, 64, dtype=BF16)
+    pos = 67000000 * 16 - 1
+    few.page_table[1, -1] = 7
+    nnc.op_kv_write_paged(few, x, x, _ints([17, pos]))
+    nnc.op_kv_write_paged(few, x[:1], x[:1], _ints([16]), _ints([0]))
+    out, lse = nnc.op_attn_decode_paged(x, few, _ints([18, pos + 1]), window=2, scratch=scratch, want_lse=True)
+    assert nnc.op_status() == 0
+    held = [[x[:1].double().transpose(0, 1).expand(1, 2, 64), torch.stack([torch.zeros(1, 64, device="cuda").double(), x[1].double()], 1)] for _ in range(2)]
+    _check_attention(out, lse, x, held, [2, 2], 0.125, 0, BF16)
 
 
 @pytest.mark.parametrize("kv", [BF16, E4M3], ids=str)
