@@ -423,54 +423,19 @@ def op_attn_prefill_f16(qkv: torch.Tensor, k16: torch.Tensor, v16: torch.Tensor,
 
 # ---- rotary positions and the paged key-value cache --------------------------------------------------------------
 
+# These calls are marshalled by the extension module _calls (csrc/torch_calls.cpp) instead of ctypes: a decoding step makes several a
+# layer, and the way through Python took longer than their kernels.  It calls the entry points of the library loaded above.
+try:
+    from . import _calls
+except ImportError as e:
+    raise ImportError("paper_2512_21571_b200/_calls.so is missing or does not fit this torch: build it with "
+                      "`python -m paper_2512_21571_b200.build` (or __graft_entry__.build()); there is no fallback implementation") from e
+_calls.bind(*(C.cast(getattr(lib, n), C.c_void_p).value for n in
+              ("nnc_op_rope", "nnc_op_kv_write_paged", "nnc_op_kv_read_paged", "nnc_op_attn_decode_paged")), NncError)
+
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp_turns": 3, "ramp_index": 4}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
 ATTN_PAGED_SCRATCH_BYTES = 16 << 20
-
-
-_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-
-
-def _launch(fn, device: int, *args):
-    """The C call on the tensors' own device and that device's current stream, whichever device is current."""
-    if device == _current_device():
-        rc = fn(*args, _current_stream(device))
-    else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _current_stream(device))
-    if rc:
-        raise NncError(rc, fn.__name__)
-
-
-def _disjoint(t: torch.Tensor) -> bool:
-    """No two elements of t share memory (as far as sorted strides show it)."""
-    if t.is_contiguous():
-        return True
-    span = 1
-    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
-        if stride < span:
-            return False
-        span += stride * (n - 1)
-    return True
-
-
-def _rows(t: torch.Tensor, device: int, what: str):
-    """The type number and the strides between rows and heads of t, [tokens][heads][head_dim] with contiguous heads."""
-    kind = _TYPES.get(t.dtype, 3)
-    if kind == 3 or t.dim() != 3 or t.get_device() != device:
-        raise ValueError(f"{what}: [tokens][heads][head_dim] of float32, bfloat16 or float16 on one CUDA device with the other tensors of the call")
-    row, head, one = t.stride()
-    tokens, heads, d = t.shape
-    if one != 1 and d > 1:
-        raise ValueError(f"{what}: elements of a head next to each other")
-    head = head if heads > 1 else d          # strides that nothing is reached by
-    return kind, row if tokens > 1 else heads * head, head
-
-
-def _index(t: torch.Tensor, n: int, device: int, what: str) -> int:
-    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != device:
-        raise ValueError(f"{what}: {n} contiguous int32 numbers on the call's CUDA device")
-    return t.data_ptr()
 
 
 def _device(t: torch.Tensor, what: str) -> int:
@@ -495,21 +460,7 @@ def op_rope(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interl
             inverse: bool = False, out: Optional[torch.Tensor] = None):
     """nnc_op_rope: x [tokens][heads][head_dim] (any strides between rows and heads) turned by int32 `positions`; the first
     2 * len(freq) elements of each head turn.  out: None, x itself, or a tensor of x's shape and type that x does not overlap."""
-    device = _device(x, "x")
-    kind, row, head = _rows(x, device, "x")
-    tokens, heads, d = x.shape
-    if out is None:
-        out = torch.empty_like(x) if x.is_contiguous() else torch.empty((tokens, heads, d), dtype=x.dtype, device=x.device)
-        out_row, out_head = heads * d, d
-    else:
-        out_kind, out_row, out_head = _rows(out, device, "out")
-        if out.shape != x.shape or out_kind != kind or not _disjoint(out):
-            raise ValueError("out: x's shape and type, no rows that overlap")
-    if freq.dtype is not torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.get_device() != device:
-        raise ValueError("freq: contiguous float64 numbers on the call's CUDA device")
-    _launch(lib.nnc_op_rope, device, x.data_ptr(), out.data_ptr(), kind, tokens, heads, d, row, head, out_row, out_head,
-            _index(positions, tokens, device, "positions"), freq.data_ptr(), 2 * freq.shape[0], interleaved, inverse, amplitude)
-    return out
+    return _calls.rope(x, positions, freq, interleaved, amplitude, inverse, out)
 
 
 class PagedKV:
@@ -543,7 +494,7 @@ class PagedKV:
         self.c = nnc_paged_kv(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if codes else None, v_scale.data_ptr() if codes else None,
                               page_table.data_ptr(), _TYPES[k.dtype], self.n_pages, self.page_size, self.n_kv_heads, self.head_dim,
                               self.n_seqs, self.pages_per_seq)
-        self.ref = C.byref(self.c)
+        self.ref, self.address = C.byref(self.c), C.addressof(self.c)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_seqs: int, pages_per_seq: int,
@@ -558,34 +509,15 @@ class PagedKV:
 def op_kv_write_paged(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, seq: Optional[torch.Tensor] = None):
     """nnc_op_kv_write_paged: rows k, v [tokens][n_kv_heads][head_dim] to positions `pos` of sequences `seq` (None: token t is
     sequence t's).  k and v have the same strides (slices of one fused projection do)."""
-    device = cache.index
-    rows = kind, row, head = _rows(k, device, "k")
-    shape = tokens, heads, d = k.shape
-    if _rows(v, device, "v") != rows or v.shape != shape or heads != cache.n_kv_heads or d != cache.head_dim:
-        raise ValueError("k, v: [tokens][n_kv_heads][head_dim] of the cache, of one type with the same strides")
-    _launch(lib.nnc_op_kv_write_paged, device, cache.ref, k.data_ptr(), v.data_ptr(), kind, tokens, row, head,
-            _index(pos, tokens, device, "pos"), None if seq is None else _index(seq, tokens, device, "seq"))
+    _calls.kv_write(cache.address, cache.index, k, v, pos, seq)
 
 
 def op_kv_read_paged(cache: PagedKV, pos: torch.Tensor, seq: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
                      out=None):
     """nnc_op_kv_read_paged: (k, v), [tokens][n_kv_heads][head_dim], of positions `pos` of sequences `seq`.  out: None (then
     padding tokens' rows hold anything), or a pair of tensors with the same strides."""
-    device, tokens = cache.index, pos.shape[0]
-    shape = (tokens, cache.n_kv_heads, cache.head_dim)
-    if out is None:
-        dtype = dtype or (torch.bfloat16 if cache.dtype is torch.float8_e4m3fn else cache.dtype)
-        k = torch.empty(shape, dtype=dtype, device=cache.device)
-        v = torch.empty_like(k)
-    else:
-        k, v = out
-    rows = kind, row, head = _rows(k, device, "dtype or out")
-    if out is not None and (k.shape != shape or v.shape != shape or _rows(v, device, "out") != rows or (dtype or k.dtype) is not k.dtype
-                            or not _disjoint(k) or not _disjoint(v)):
-        raise ValueError("out: two tensors [tokens][n_kv_heads][head_dim] of one type with the same strides, no rows that overlap")
-    _launch(lib.nnc_op_kv_read_paged, device, cache.ref, k.data_ptr(), v.data_ptr(), kind, tokens, row, head,
-            _index(pos, tokens, device, "pos"), None if seq is None else _index(seq, tokens, device, "seq"))
-    return k, v
+    k, v = (None, None) if out is None else out
+    return _calls.kv_read(cache.address, cache.index, pos, seq, dtype, k, v)
 
 
 def attn_paged_scratch(device="cuda") -> torch.Tensor:
@@ -597,25 +529,4 @@ def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, sc
                          scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, want_lse: bool = False):
     """nnc_op_attn_decode_paged: q [batch][n_q_heads][head_dim] (rows may be apart) against the first lens[b] positions of each
     sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  Returns out, or (out, lse)."""
-    device = cache.index
-    kind, row, head = _rows(q, device, "q")
-    batch, nq, d = q.shape
-    if d != cache.head_dim or head != d:
-        raise ValueError("q: [batch][n_q_heads][head_dim] of the cache's head_dim, heads next to each other")
-    if not 0 <= window < 1 << 31:
-        raise ValueError("window: 0 or a number of positions")
-    if out is None:
-        out, out_row = torch.empty_like(q) if q.is_contiguous() else torch.empty((batch, nq, d), dtype=q.dtype, device=q.device), nq * d
-    else:
-        out_kind, out_row, out_head = _rows(out, device, "out")
-        if out.shape != q.shape or out_kind != kind or out_head != d or not _disjoint(out):
-            raise ValueError("out: q's shape and type, heads next to each other, no rows that overlap")
-    lse = q.new_empty((batch, nq), dtype=torch.float32) if want_lse else None
-    if scratch is None:
-        scratch = attn_paged_scratch(cache.device)
-    elif scratch.get_device() != device or not scratch.is_contiguous():
-        raise ValueError("scratch: a contiguous tensor on the call's CUDA device (attn_paged_scratch)")
-    _launch(lib.nnc_op_attn_decode_paged, device, q.data_ptr(), cache.ref, _index(lens, batch, device, "lens"), out.data_ptr(),
-            lse.data_ptr() if want_lse else None, kind, batch, nq, row, out_row, d ** -0.5 if scale is None else scale, window,
-            scratch.data_ptr(), scratch.nbytes)
-    return (out, lse) if want_lse else out
+    return _calls.attn(cache.address, cache.index, q, lens, scale, window, scratch, out, want_lse)

@@ -43,8 +43,33 @@ def _compile(src: str, verbose: bool, checked: bool = False) -> str:
     return obj
 
 
+CALLS = os.path.join(_HERE, "_calls.so")   # marshalling of the paged-cache operations for torch tensors (csrc/torch_calls.cpp)
+
+
+def build_calls(force: bool = False) -> str:
+    """Builds the extension module _calls.so with g++ against the headers of the running Python and torch."""
+    import sysconfig
+    src = os.path.join(CSRC, "torch_calls.cpp")
+    newest = max(os.path.getmtime(p) for p in (src, os.path.join(os.path.dirname(_HERE), "include", "nnc.h")))
+    if not force and os.path.exists(CALLS) and os.path.getmtime(CALLS) >= newest:
+        return CALLS
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *["-I" + i for i in include], src, "-o", CALLS + ".new", "-L" + os.path.join(root, "lib"), "-ltorch_cpu", "-lc10", "-lc10_cuda",
+           "-ltorch_python"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for {src}:\n{r.stdout}\n{r.stderr}")
+    os.replace(CALLS + ".new", CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
-    """Builds libnnc.so, or with checked=True the bounds-checked debugging build libnnc_checked.so."""
+    """Builds libnnc.so, or with checked=True the bounds-checked debugging build libnnc_checked.so; and _calls.so, which serves both."""
     lib = LIB_CHECKED if checked else LIB
     if force:
         for s in sources():
@@ -52,7 +77,9 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
             if os.path.exists(o):
                 os.remove(o)
     with concurrent.futures.ThreadPoolExecutor(max_workers=8) as ex:
+        calls = ex.submit(build_calls, force)
         objs = list(ex.map(lambda s: _compile(s, verbose, checked), sources()))
+        calls.result()
     if force or not os.path.exists(lib) or os.path.getmtime(lib) < max(os.path.getmtime(o) for o in objs):
         cmd = ["nvcc", "-shared", "-o", lib, *objs, "-gencode", "arch=compute_100a,code=sm_100a", "-cudart", "static"]
         subprocess.check_call(cmd)
