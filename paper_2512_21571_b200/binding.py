@@ -1,4 +1,5 @@
-"""ctypes binding of libnnc.so: same names as the C ABI (include/nnc.h), argument marshalling only.
+"""ctypes binding of libnnc.so: same names as the C ABI (include/nnc.h), argument marshalling only.  The paged-cache operations at
+the end are marshalled by an extension module (csrc/torch_calls.cpp) that calls the same library.
 
 PyTorch is used for device memory and the CUDA stream; every step of the forward pass runs inside the library's
 kernels.  Importing this module loads the shared library and raises if it has not been built -- there is no
