@@ -19,7 +19,8 @@
 //     busy 13 % of the time at 95 % of the measured copy bandwidth.  A tcgen05 tile would have 128 rows for the same 8 columns,
 //     for more of a pipe that does not limit.
 //   - E4M3 codes are fp16 values exactly; key scales multiply the scores, value scales (powers of two) are added to the
-//     exponents of the probabilities that weigh the codes, so no code is ever multiplied by a scale.  (The warp-level product of
+//     exponents of the probabilities that weigh the codes, so no code is ever multiplied by a scale.  Those weights have a running
+//     maximum of their own: the softmax's sum is taken of the probabilities themselves, whose reach has nothing to do with the values'.  (The warp-level product of
 //     8-bit operands is built from fp16 ones on this machine, at more instructions than these conversions: measured, 147 -> 179 us.)
 // Numerics: scores, maxima, sums and outputs are fp32.  Queries enter exactly (16-bit types) or as enough terms for fp32 (three
 // bf16 or two fp16 terms).  Probabilities: two bf16 or fp16 terms (2^-16, 2^-21), three bf16 for fp32 results of a bf16 cache; for bf16
@@ -76,7 +77,7 @@ struct Shape {
 };
 
 struct AttnShared {
-    float ml[kWarps][8][2];
+    float ml[kWarps][8][3];   // references of o~ and of l, and l
     int sums[kWarps];
     int first_b, first_rest;
     struct { int c_lo, c_hi, q_head, heads_here, b, last; } split[2];   // this CTA's partial results: slot 0's and slot 1's
@@ -336,6 +337,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     uint32_t qf[NT][QT][D / 16][2];
     float qmul[NT][2];
     float o[NT][S::kTilesD][4], m_run[NT][2], l_run[NT][2];
+    float mv_run[NT][2];   // codes: the maximum of score + value exponent, which o~ refers to; otherwise that is m_run
     int piece_first = now.index;   // place of the piece's first tile
 
     // Queries of a (sequence, head): lane (g8, t4) holds head g8's elements of contraction columns 2 t4, 2 t4 + 1, 2 t4 + 8,
@@ -404,7 +406,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 qmul[nt][e] = p.scale_log2 * __shfl_sync(0xffffffffu, undo, (2 * t4 + e) * 4);
-                m_run[nt][e] = -INFINITY;
+                m_run[nt][e] = mv_run[nt][e] = -INFINITY;
                 l_run[nt][e] = 0.f;
             }
 #pragma unroll
@@ -486,24 +488,23 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         }
         const uint32_t here = present >> (stage * S::kSub) & ((1u << S::kSub) - 1u);
         const bool full = p0 >= now.r.start && p0 + PB <= now.r.end && here == (1u << S::kSub) - 1u;
-        float back[S::kSub][2];   // 2^-exponent of the value rows
+        float ev[S::kSub][2];   // exponents of the value rows
 #pragma unroll
         for (int u = 0; u < S::kSub; ++u)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {   // rows g8 and g8 + 8
-                float ks = 1.f, ev = 0.f;
+                float ks = 1.f;
                 if constexpr (CODES) {
                     const uint32_t bk = (uint8_t)scales[16 * u + g8 + 8 * r], bv = (uint8_t)scales[PB + 16 * u + g8 + 8 * r];
                     ks = __uint_as_float(bk << 23);
-                    ev = __uint_as_float(0x4b000000u | bv) - 8388735.f;   // bv - 127: 2^23 + bv as fp32, no conversion
-                    back[u][r] = __uint_as_float(0x7f000000u - (bv << 23));
+                    ev[u][r] = __uint_as_float(0x4b000000u | bv) - 8388735.f;   // bv - 127: 2^23 + bv as fp32, no conversion
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         float &x = s[u][nt][2 * r + e];
-                        x = CODES ? fmaf(x, qmul[nt][e] * ks, ev) : x * qmul[nt][e];
+                        x *= CODES ? qmul[nt][e] * ks : qmul[nt][e];
                     }
             }
         if (!full) {
@@ -513,38 +514,54 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                 for (int r = 0; r < 2; ++r) {
                     const int pos = p0 + 16 * u + g8 + 8 * r;
                     if ((here >> u & 1u) && pos >= now.r.start && pos < now.r.end) continue;
-                    back[u][r] = 1.f;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) s[u][nt][2 * r] = s[u][nt][2 * r + 1] = -INFINITY;
                 }
         }
-        // ---- online softmax; with codes, of the scores plus the value rows' exponents ----
+        // ---- online softmax; with codes, a second one of the scores plus the value rows' exponents for what weighs the codes ----
         uint32_t pf[S::kSub][NT][PT][2];
         float alpha[NT][2];
+        auto top_of = [&](int nt, int e) {   // of this block's scores
+            float mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < S::kSub; ++u) mx = fmaxf(mx, fmaxf(s[u][nt][e], s[u][nt][2 + e]));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            return fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+        };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float mx = -INFINITY;
+                if constexpr (CODES) {
+                    const float m_new = fmaxf(m_run[nt][e], top_of(nt, e)), ref = m_new == -INFINITY ? 0.f : m_new;
+                    float sum = 0.f;
 #pragma unroll
-                for (int u = 0; u < S::kSub; ++u) mx = fmaxf(mx, fmaxf(s[u][nt][e], s[u][nt][2 + e]));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                const float m_new = fmaxf(m_run[nt][e], mx);
+                    for (int u = 0; u < S::kSub; ++u)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            float &x = s[u][nt][2 * r + e];
+                            sum += exp2_flush(x - ref);
+                            x += ev[u][r];
+                        }
+                    l_run[nt][e] = fmaf(l_run[nt][e], exp2_flush(m_run[nt][e] - ref), sum);
+                    m_run[nt][e] = m_new;
+                }
+                float &m = CODES ? mv_run[nt][e] : m_run[nt][e];
+                const float m_new = fmaxf(m, top_of(nt, e));
                 const float ref = (m_new == -INFINITY ? 0.f : m_new) - kLift;   // nothing attended so far: every weight is 0
-                alpha[nt][e] = exp2_flush(m_run[nt][e] - kLift - ref);
-                m_run[nt][e] = m_new;
+                alpha[nt][e] = exp2_flush(m - kLift - ref);
+                m = m_new;
                 float sum = 0.f;
 #pragma unroll
                 for (int u = 0; u < S::kSub; ++u)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float w = exp2_flush(s[u][nt][2 * r + e] - ref);
-                        s[u][nt][2 * r + e] = w;
-                        sum = CODES ? fmaf(w, back[u][r], sum) : sum + w;
+                        float &x = s[u][nt][2 * r + e];
+                        x = exp2_flush(x - ref);
+                        sum += x;
                     }
-                l_run[nt][e] = fmaf(l_run[nt][e], alpha[nt][e], sum);
+                if constexpr (!CODES) l_run[nt][e] = fmaf(l_run[nt][e], alpha[nt][e], sum);
             }
 #pragma unroll
             for (int u = 0; u < S::kSub; ++u) {
@@ -634,7 +651,12 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                 l += __shfl_xor_sync(0xffffffffu, l, 4);
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
-                if (g8 == 0) { sh.ml[warp][2 * t4 + e][0] = m_run[nt][e] == -INFINITY ? -INFINITY : m_run[nt][e] - kLift; sh.ml[warp][2 * t4 + e][1] = l; }
+                if (g8 == 0) {
+                    float *const ml = sh.ml[warp][2 * t4 + e];
+                    ml[0] = (CODES ? mv_run[nt][e] : m_run[nt][e]) - kLift;
+                    ml[1] = CODES ? m_run[nt][e] : ml[0];
+                    ml[2] = l;
+                }
             }
             float M[2], L[2], wgt[kWarps][2];
 #pragma unroll
@@ -654,13 +676,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                     for (int e = 0; e < 2; ++e) {
                         M[e] = -INFINITY;
 #pragma unroll
-                        for (int w = 0; w < kWarps; ++w) M[e] = fmaxf(M[e], sh.ml[w][2 * t4 + e][0]);
+                        for (int w = 0; w < kWarps; ++w) M[e] = fmaxf(M[e], sh.ml[w][2 * t4 + e][1]);
                         const float ref = M[e] == -INFINITY ? 0.f : M[e];
                         L[e] = 0.f;
 #pragma unroll
                         for (int w = 0; w < kWarps; ++w) {
-                            wgt[w][e] = exp2f(sh.ml[w][2 * t4 + e][0] - ref);
-                            L[e] = fmaf(wgt[w][e], sh.ml[w][2 * t4 + e][1], L[e]);
+                            const float *const ml = sh.ml[w][2 * t4 + e];
+                            wgt[w][e] = exp2f(ml[0] - ref);   // o~ refers to M from here on
+                            L[e] = fmaf(CODES ? exp2f(ml[1] - ref) : wgt[w][e], ml[2], L[e]);
                         }
                     }
                 }
