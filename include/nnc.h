@@ -336,7 +336,9 @@ int nnc_op_rope(const void *x, void *y, int32_t type, int32_t n_tokens, int32_t 
  * sequence s lies in slot n % page_size of page page_table[s * pages_per_seq + n / page_size].
  *   k, v             [n_pages][n_kv_heads][page_size][head_dim] of `type` (NNC_BF16, NNC_F16 or NNC_E4M3), 16-byte aligned
  *   k_scale, v_scale NNC_E4M3 only: one byte a row, [n_pages][n_kv_heads][page_size], 16-byte aligned: the row's values
- *                    are code * 2^(byte - 127), bytes of 67 .. 187 (what nnc_op_kv_write_paged writes).  NULL otherwise
+ *                    are code * 2^(byte - 127), bytes of 67 .. 187 (what nnc_op_kv_write_paged writes).  NULL otherwise.  The attention
+ *                    keeps a position's weight to 2^-39 of the largest product of a weight and its value row's scale, rows of zeros
+ *                    not counted: scales larger than their rows need cost the other rows' accuracy
  *   page_table       int32 [n_seqs][pages_per_seq]; entries that no call reaches may hold anything.  Sequences may share pages
  *                    (a common prefix) that no call writes
  *   page_size 16, 32, 64, 128 or 256; head_dim 64 or 128.

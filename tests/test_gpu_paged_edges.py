@@ -4,7 +4,7 @@ infinities, long shares.  Plain 64-bit forms and bounds as in test_gpu_paged."""
 import pytest
 import torch
 
-from test_gpu_paged import BF16, E4M3, F32, _check_attention, _gen, _ints, _randn, nnc, quantise64, scratch  # noqa: F401
+from test_gpu_paged import BF16, E4M3, F16, F32, _check_attention, _gen, _ints, _paged, _randn, nnc, quantise64, scratch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,37 @@ def test_a_row_of_large_values_leaves_the_sum_of_the_weights_alone(nnc, scratch,
         nnc.op_kv_write_paged(cache, k, v, _ints(range(n)), _ints([0] * n))
         out, lse = nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch, want_lse=True)
         _check_attention(out, lse, q, [t * batch for t in _held(k, v)], lens, d ** -0.5, 0, E4M3)
+
+
+# ---- rows of zeros ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-5, 1e-7, 1e-10])
+@pytest.mark.parametrize("n,d,group", [(513, 64, 3), (70, 128, 1), (5000, 128, 16)])
+def test_value_rows_of_zeros_take_no_bits_from_the_others(nnc, scratch, dtype, size, n, d, group):
+    """Rows of zeros, written or never written, at scores up to 14 above the others: their codes are 0 and weigh nothing in the
+    result, so its accuracy is the other rows'."""
+    g = _gen(n + group)
+    heads = 2
+    q = _randn(g, 3, heads * group, d)
+    q[:, :, 0] = 3.0
+    k, v = (_randn(g, n, heads, d) for _ in range(2))
+    v *= size
+    k[:, :, 0] = 0
+    for row, above in ((0, 14.0), (n // 2, 10.0), (n - 2, 0.0), (n - 1, -3.0)):
+        v[row] = 0
+        k[row, :, 0] = above / 3.0 / d ** -0.5
+    cache = _paged(nnc, E4M3, [n, n, 40], 32, heads, d, 1)
+    for b in range(2):
+        nnc.op_kv_write_paged(cache, k, v, _ints(range(n)), _ints([b] * n))
+    table = cache.page_table[2, :2].long()
+    for pool, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):       # the third sequence: as PagedKV.empty leaves it
+        pool.view(torch.uint8)[table], scale[table] = 0, 127
+    nnc.op_kv_write_paged(cache, k[:7], v[:7], _ints(range(7)), _ints([2] * 7))
+    held = _held(k, v)
+    zeros = torch.zeros(heads, 33, d, device="cuda").double()
+    held = [t * 2 + [torch.cat([t[0][:, :7], zeros], 1)] for t in held]
+    out, lse = nnc.op_attn_decode_paged(q.to(dtype), cache, _ints([n, n, 40]), scratch=scratch, want_lse=True)
+    _check_attention(out, lse, q.to(dtype), held, [n, n, 40], d ** -0.5, 0, E4M3)
+    nothing, _ = nnc.op_attn_decode_paged(q.to(dtype), cache, _ints([1, 1, 0]), scratch=scratch, want_lse=True)
+    assert (nothing == 0).all()                                                     # nothing but a row of zeros
