@@ -484,7 +484,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         s[u][nt][x] = acc[0][u][nt][x] + acc[1][u][nt][x];
-                        if constexpr (QT > 1) s[u][nt][x] += acc[2][u][nt][x];
+                        // (an infinity is the first terms': the lower ones may be 0 or of the other sign, and make NaN of it)
+                        if constexpr (QT > 1) s[u][nt][x] += fabsf(s[u][nt][x]) == INFINITY ? 0.f : acc[2][u][nt][x];
                     }
         }
         const uint32_t here = present >> (stage * S::kSub) & ((1u << S::kSub) - 1u);

@@ -1,5 +1,6 @@
 """Attention over the paged cache where its operands leave the ordinary: rows of zeros, scales at the ends of their range,
 infinities, long shares.  Plain 64-bit forms and bounds as in test_gpu_paged."""
+import math
 
 import pytest
 import torch
@@ -72,3 +73,35 @@ def test_value_rows_of_zeros_take_no_bits_from_the_others(nnc, scratch, dtype, s
     _check_attention(out, lse, q.to(dtype), held, [n, n, 40], d ** -0.5, 0, E4M3)
     nothing, _ = nnc.op_attn_decode_paged(q.to(dtype), cache, _ints([1, 1, 0]), scratch=scratch, want_lse=True)
     assert (nothing == 0).all()                                                     # nothing but a row of zeros
+
+
+# ---- infinities ------------------------------------------------------------------------------------------------------
+
+def _drop(held, gone):
+    n = held[0][0].shape[1]
+    keep = [i for i in range(n) if i not in gone]
+    return [[t[0][:, keep]] for t in held], n - len(gone)
+
+
+@pytest.mark.parametrize("kv,dtype", [(BF16, F32), (F16, F32), (BF16, BF16), (F16, F16)], ids=str)
+@pytest.mark.parametrize("n", [40, 3001])
+def test_infinite_keys_take_their_rows_out_or_decide(nnc, scratch, kv, dtype, n):
+    """A score of -infinity weighs nothing; one of +infinity leaves no number."""
+    g = _gen(n)
+    d, heads, group = 128, 2, 4
+    q = _randn(g, 1, heads * group, d, dtype=dtype)
+    q[0, :, 5] = torch.tensor([-1.3, -0.7, 1.1, -2.9] * heads, device="cuda", dtype=dtype)    # head 2 of each group meets +infinity
+    k, v = (_randn(g, n, heads, d, dtype=kv) for _ in range(2))
+    rows = [3, n // 2, n - 1]
+    for r in rows:
+        k[r, :, 5] = math.inf
+    cache = _paged(nnc, kv, [n], 16, heads, d, 1)
+    nnc.op_kv_write_paged(cache, k, v, _ints(range(n)), _ints([0] * n))
+    out, lse = nnc.op_attn_decode_paged(q, cache, _ints([n]), scratch=scratch, want_lse=True)
+    decided = [2, 6]
+    others = [0, 1, 3, 4, 5, 7]
+    assert out[0, decided].isnan().all()
+    held, left = _drop([[t.double().transpose(0, 1)] for t in (k, v)], rows)
+    split = lambda t: t.unflatten(1, (heads, group))[:, :, [0, 1, 3]].flatten(1, 2)
+    _check_attention(split(out), split(lse[..., None])[..., 0], split(q), held, [left], d ** -0.5, 0, kv)
+    assert lse[0, others].isfinite().all()
