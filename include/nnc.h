@@ -376,6 +376,8 @@ int nnc_op_kv_read_paged(const nnc_paged_kv *cache, void *k, void *v, int32_t ty
  *           the cache outside that range are never read into the result (they may hold anything)
  *   scale   multiplies q.k before the softmax
  *   lse     fp32 [batch][n_q_heads] or NULL: log(sum exp) of the scaled scores, natural logarithm
+ * Scores are a softmax's whatever their size: -infinity weighs nothing, +infinity or NaN leave a head no number.  Every other
+ * attended position has a positive weight, so a column of values with an infinity gives that infinity (both signs, or NaN: NaN).
  * A sequence with nothing to attend to (lens <= 0) gets a row of zeros and lse = -infinity.  A length beyond the table's
  * reach counts as the longest the table holds, and a page out of range as absent; both set the status word.
  * scratch: DEVICE, 256-byte aligned, NNC_ATTN_PAGED_SCRATCH_BYTES; its first NNC_ATTN_PAGED_TICKET_BYTES must be zero before

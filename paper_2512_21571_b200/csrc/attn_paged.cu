@@ -80,6 +80,7 @@ struct Shape {
 struct AttnShared {
     float ml[kWarps][8][3];   // references of o~ and of l, and l
     int sums[kWarps];
+    uint32_t odd[32];   // what a piece's values hold besides finite numbers (odd_values)
     int first_b, first_rest;
     struct { int c_lo, c_hi, q_head, heads_here, b, last; } split[2];   // this CTA's partial results: slot 0's and slot 1's
 };
@@ -651,6 +652,35 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     // ---- results.  A warp's fragments of O^T tile i: rows d0 (and d1) of two heads ----
     float (*comb)[3][S::kOnce][32][4] = reinterpret_cast<float (*)[3][S::kOnce][32][4]>(smem + kWarps * S::kStages * S::kStage);
 
+    // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs, or
+    // NaN, leave no number).  The products cannot say so: a weight's lower term, or a weight below the smallest, is 0, and 0 or a negative
+    // number times infinity makes NaN.  So a piece that ends with anything but finite sums looks through its rows again, a row
+    // a warp: three bits a column, for +infinity, -infinity and NaN.
+    constexpr int kCols = D / 32;   // columns a lane
+    auto odd_values = [&](int p_lo, int p_hi) {
+        if (tid < 32) sh.odd[tid] = 0u;
+        __syncthreads();
+        uint32_t bits = 0;
+#pragma unroll 4
+        for (int pos = p_lo + warp; pos < p_hi; pos += kWarps) {
+            const int page = p.c.table[(long long)now.b * p.c.pages_per_seq + (pos >> p.c.page_shift)];
+            if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
+            const uint32_t *row = reinterpret_cast<const uint32_t *>(p.c.v + paged_row(p.c, page, now.head, pos & ((1 << p.c.page_shift) - 1)) * ROW) + lane * (kCols / 2);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) {
+                constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+                const uint32_t x = row[i / 2] >> (16 * (i & 1)) & 0xffffu, size = x & 0x7fffu;
+                if (size >= kInf) bits |= (size > kInf ? 4u : x == size ? 1u : 2u) << (3 * i);
+            }
+        }
+        if (bits) atomicOr(&sh.odd[lane], bits);
+        __syncthreads();
+    };
+    auto odd_or = [&](int d, float sum) {
+        const uint32_t bits = sh.odd[d / kCols] >> (3 * (d % kCols)) & 7u;
+        return bits == 0u ? sum : bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
+    };
+
     auto end_piece = [&]() {
         const int item_lo = now.index - now.tile, item_hi = item_lo + now.r.tiles;   // places of this (sequence, head)'s tiles
         const int first = piece_first;
@@ -659,6 +689,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
         const long long out_at = now.b * p.out_stride + (long long)q_head * D, lse_at = (long long)now.b * (p.c.n_kv * p.group) + q_head;
         // partial results: slot 0 of a CTA for a piece that continues an earlier CTA's, slot 1 for one that starts here
         float *slot = part + (size_t)(2 * cta + (first == item_lo ? 1 : 0)) * S::kSlotFloats;
+        float all_sums = 0.f;
+        if constexpr (!CODES) {   // (a code is never infinite, and NaN comes through by itself)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < S::kTilesD; ++i) all_sums += (o[nt][i][0] + o[nt][i][1]) + (o[nt][i][2] + o[nt][i][3]);
+        }
+        bool odd = !(fabsf(all_sums) < INFINITY);
         if (!whole && !NNC_BC((size_t)(2 * (chunk * gridDim.x + cta) + 2) * S::kSlotFloats <= p.part_floats, 3201)) return;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -687,7 +725,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                         if (to == warp) { own[j][0] = v[0]; own[j][1] = v[1]; own[j][2] = v[2]; own[j][3] = v[3]; }
                         else *reinterpret_cast<float4 *>(comb[to][warp < to ? warp : warp - 1][j][lane]) = make_float4(v[0], v[1], v[2], v[3]);
                     }
-                __syncthreads();
+                if (CODES || nt > 0 || round > 0) __syncthreads();
+                else {
+                    odd = __syncthreads_or(odd);
+                    if (odd) {
+                        const int base = now.r.start & ~15;
+                        odd_values(max(now.r.start, base + (first - item_lo) * TILE), min(now.r.end, base + (now.tile + 1) * TILE));
+                    }
+                }
                 if (round == 0) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
@@ -725,6 +770,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                     for (int j = 0; j < S::kOnce; ++j) {
                         const int i = warp * S::kOwn + round * S::kOnce + j;
                         const int d0 = CODES ? 16 * i + 2 * g8 : 16 * i + g8, d1 = CODES ? d0 + 1 : d0 + 8;
+                        if (!CODES && odd) { sum[j][e] = odd_or(d0, sum[j][e]); sum[j][2 + e] = odd_or(d1, sum[j][2 + e]); }
                         if (whole) {
                             store_out<TYPE>(p, out_at + h * D + d0, sum[j][e] * inv);
                             store_out<TYPE>(p, out_at + h * D + d1, sum[j][2 + e] * inv);
@@ -864,11 +910,22 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
                     float4 *slot0 = reinterpret_cast<float4 *>(slot_a) + col;
                     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (lo > 0) sum = *slot0;   // what the pieces before these gave
+                    const float4 from = sum;
 #pragma unroll 4
                     for (int i = lo; i < hi; ++i) {
                         const float w = wgt[h * S::kMaxJoin + i];
                         const float4 v = rows[(i - lo) * cols + col];
                         sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
+                    }
+                    if (!CODES && !(fabsf((sum.x + sum.y) + (sum.z + sum.w)) < INFINITY)) {   // an infinite piece counts whatever it weighs
+                        auto add = [](float w, float v, float sum) { return fabsf(v) == INFINITY ? sum + v : fmaf(w, v, sum); };
+                        sum = from;
+#pragma unroll 1
+                        for (int i = lo; i < hi; ++i) {
+                            const float w = wgt[h * S::kMaxJoin + i];
+                            const float4 v = rows[(i - lo) * cols + col];
+                            sum.x = add(w, v.x, sum.x); sum.y = add(w, v.y, sum.y); sum.z = add(w, v.z, sum.z); sum.w = add(w, v.w, sum.w);
+                        }
                     }
                     const float2 ML = tot[h];
                     if (!final || hi < n) {

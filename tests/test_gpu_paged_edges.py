@@ -105,3 +105,36 @@ def test_infinite_keys_take_their_rows_out_or_decide(nnc, scratch, kv, dtype, n)
     split = lambda t: t.unflatten(1, (heads, group))[:, :, [0, 1, 3]].flatten(1, 2)
     _check_attention(split(out), split(lse[..., None])[..., 0], split(q), held, [left], d ** -0.5, 0, kv)
     assert lse[0, others].isfinite().all()
+
+
+@pytest.mark.parametrize("kv,dtype", [(BF16, F32), (F16, F32), (BF16, BF16), (F16, F16)], ids=str)
+@pytest.mark.parametrize("n,d,group,window", [(1, 64, 1, 0), (40, 128, 4, 0), (40, 128, 4, 30), (700, 64, 12, 0), (30011, 128, 5, 0), (9000, 64, 17, 8100)])
+@pytest.mark.parametrize("spread", [1.0, 12.0])
+def test_infinite_values_are_what_a_weighted_sum_makes_of_them(nnc, scratch, kv, dtype, n, d, group, window, spread):
+    """Every attended weight is positive, however small: one infinity in a column of values is the column's result, two of
+    different signs and NaN leave no number, the other columns are finite."""
+    g = _gen(n + d)
+    heads = 2
+    q = (_randn(g, 2, heads * group, d) * spread).to(dtype)
+    k, v = (_randn(g, n, heads, d, dtype=kv) for _ in range(2))
+    first = max(0, n - window) if window else 0
+    at = lambda f: first + int((n - 1 - first) * f)
+    for f, column, x in ((0.0, 1, math.inf), (0.31, 2, -math.inf), (0.5, 9, math.inf), (0.9, 9, math.inf), (0.2, 33, math.inf), (0.7, 33, -math.inf),
+                         (0.4, 40, math.nan), (0.6, 41, math.inf), (0.61, 41, math.nan), (1.0, 63, -math.inf), (0.77, d - 2, math.inf)):
+        v[at(f), 1 if column == 9 else slice(None), column] = x
+    cache = _paged(nnc, kv, [n, n], 64, heads, d, 1)
+    for b in range(2):
+        nnc.op_kv_write_paged(cache, k, v, _ints(range(n)), _ints([b] * n))
+    out, lse = nnc.op_attn_decode_paged(q, cache, _ints([n, n]), window=window, scratch=scratch, want_lse=True)
+    seen = v[first:].double()
+    plus, minus, nan = (seen == math.inf).any(0), (seen == -math.inf).any(0), seen.isnan().any(0)         # [heads][d]
+    lost, up, down = nan | (plus & minus), plus & ~minus & ~nan, minus & ~plus & ~nan
+    got = out.unflatten(1, (heads, group))
+    for mask, test in ((lost, got.isnan()), (up, got == math.inf), (down, got == -math.inf)):
+        mask = mask[None, :, None].expand_as(got)
+        assert test[mask].all() and not test[~mask].any()
+    # the finite columns, against the values without the others
+    clean = torch.where((plus | minus | nan)[None], 0.0, v.nan_to_num(0.0, 0.0, 0.0).double())
+    held = [[x.double().transpose(0, 1)] * 2 for x in (k, clean)]
+    finite = torch.where((plus | minus | nan)[None, :, None].expand_as(got), torch.zeros((), dtype=out.dtype, device="cuda"), got).flatten(1, 2)
+    _check_attention(finite, lse, q, held, [n, n], d ** -0.5, window, kv)
