@@ -207,7 +207,7 @@ template <int TYPE> __device__ __forceinline__ void store_out(const PagedAttnPar
 template <int D, int NT, int KV, int QT, int PT>
 __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn_paged_kernel(const PagedAttnParams p) {
     typedef Shape<D, NT, KV, QT> S;
-    constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3, kFresh = QT > 1;
+    constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3;
     constexpr int PB = S::kPB, TILE = S::kTile, ROW = S::kRow;
     // the queries' and the results' type goes with the number of terms (launch_typed)
     constexpr int TYPE = QT > 1 ? NNC_F32 : BF || (CODES && PT == 1) ? NNC_BF16 : NNC_F16;
@@ -589,28 +589,19 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
 #pragma unroll
                 for (int i = 0; i < PT; ++i) { pf[u][nt][i][0] = transpose8(lo[i]); pf[u][nt][i][1] = transpose8(hi[i]); }
             }
-            // fp32 results: a block's products get a sum of their own that is then added in fp32 (the tensor cores' cut of every
-            // addition would pile up over a long share); 16-bit results are rounded far above that
-            if (!kFresh && __any_sync(0xffffffffu, alpha[nt][0] != 1.f || alpha[nt][1] != 1.f)) {
-#pragma unroll
-                for (int i = 0; i < S::kTilesD; ++i) {
-                    o[nt][i][0] *= alpha[nt][0]; o[nt][i][1] *= alpha[nt][1]; o[nt][i][2] *= alpha[nt][0]; o[nt][i][3] *= alpha[nt][1];
-                }
-            }
         }
         // ---- O^T += V^T P^T.  o[nt][i]: columns are heads 2 t4, 2 t4 + 1; rows are elements 16 i + g8 and 16 i + 8 + g8, or
-        //      with codes 16 i + 2 g8 and 16 i + 2 g8 + 1 ----
+        //      with codes 16 i + 2 g8 and 16 i + 2 g8 + 1.  A block's products get a sum of their own that is then added in fp32: the
+        //      tensor cores cut what they add, always towards zero, which over a share of 131072 positions comes to 2e-4 of the result ----
         int subs = 1;   // 16-position parts that hold anything: what was not copied may be no number
         if constexpr (S::kSub > 1) subs = min(S::kSub, (now.r.end - p0 + 15) >> 4);
 #pragma unroll
         for (int i = 0; i < S::kTilesD; i += 2) {
             float fresh[NT][2][4];
-            if constexpr (kFresh) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) fresh[nt][e][0] = fresh[nt][e][1] = fresh[nt][e][2] = fresh[nt][e][3] = 0.f;
-            }
+                for (int e = 0; e < 2; ++e) fresh[nt][e][0] = fresh[nt][e][1] = fresh[nt][e][2] = fresh[nt][e][3] = 0.f;
 #pragma unroll
             for (int u = 0; u < S::kSub; ++u) {
                 if (u >= subs) break;
@@ -633,19 +624,14 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int j = 0; j < PT; ++j) {
-                            if constexpr (kFresh) mma16816<BF>(fresh[nt][e], a[e][0], a[e][1], a[e][2], a[e][3], pf[u][nt][j]);
-                            else mma16816<BF>(o[nt][i + e], a[e][0], a[e][1], a[e][2], a[e][3], pf[u][nt][j]);
-                        }
+                        for (int j = 0; j < PT; ++j) mma16816<BF>(fresh[nt][e], a[e][0], a[e][1], a[e][2], a[e][3], pf[u][nt][j]);
             }
-            if constexpr (kFresh) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) o[nt][i + e][x] = fmaf(o[nt][i + e][x], alpha[nt][x & 1], fresh[nt][e][x]);
-            }
+                    for (int x = 0; x < 4; ++x) o[nt][i + e][x] = fmaf(o[nt][i + e][x], alpha[nt][x & 1], fresh[nt][e][x]);
         }
     };
 

@@ -138,3 +138,31 @@ def test_infinite_values_are_what_a_weighted_sum_makes_of_them(nnc, scratch, kv,
     held = [[x.double().transpose(0, 1)] * 2 for x in (k, clean)]
     finite = torch.where((plus | minus | nan)[None, :, None].expand_as(got), torch.zeros((), dtype=out.dtype, device="cuda"), got).flatten(1, 2)
     _check_attention(finite, lse, q, held, [n, n], d ** -0.5, window, kv)
+
+
+# ---- long shares -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kv,dtype", [(F16, F16), (BF16, BF16), (E4M3, F16), (E4M3, BF16)], ids=str)
+def test_16_bit_results_of_a_share_of_131072_positions_carry_no_drift(nnc, scratch, kv, dtype):
+    """600 sequences that share one run of pages, so that a CTA sums up whole sequences: the mean distance of all results from the
+    rounded exact ones, which shows sums that are cut at every addition."""
+    n, d, batch = 131072, 64, 600
+    g = _gen(5)
+    k, v = _randn(g, n, 1, d) * 0.5, _randn(g, n, 1, d).abs() + 0.5                 # sums of one sign
+    pages = n // 256
+    cache = nnc.PagedKV.empty(pages, 256, 1, d, kv, batch, pages)
+    cache.page_table[:] = torch.arange(pages, device="cuda", dtype=torch.int32)
+    nnc.op_kv_write_paged(cache, k, v, _ints(range(n)), torch.zeros(n, dtype=torch.int32, device="cuda"))
+    q = _randn(g, batch, 1, d, dtype=dtype)
+    out = nnc.op_attn_decode_paged(q, cache, torch.full((batch,), n, dtype=torch.int32, device="cuda"), scratch=scratch)
+    hold = (lambda x: quantise64(x)[0]) if kv is E4M3 else (lambda x: x.to(kv).double())
+    k64, v64 = hold(k)[:, 0], hold(v)[:, 0]
+    want = torch.softmax(q[:, 0].double() @ k64.T * d ** -0.5, -1) @ v64
+    off = ((out[:, 0].double() - want.to(dtype).double()) / want).mean().item()
+    # Against the exact values themselves the mean would be the inputs' rounding: the results of one column lie closer together than a
+    # step of bf16.  Against the rounded ones, an error moves as many results by a whole step as make it up in the mean.  Of 38400
+    # results, each off by at most half a step either way, the mean has a spread of at most eps / 2 / sqrt(3 * 38400), of which five are
+    # allowed.  Cuts inside one block's sum (64 positions a warp, two or three terms: 12 additions at 2^-23) and the weights'
+    # own rounding (2^-21) are systematic at most.
+    allowed = 5 * torch.finfo(dtype).eps / 2 / math.sqrt(3 * batch * d) + 12 * 2.0 ** -23 + 2.0 ** -21
+    assert abs(off) <= allowed, (off, allowed)
