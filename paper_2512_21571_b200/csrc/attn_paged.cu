@@ -23,9 +23,10 @@
 //     maximum of their own, over the rows that are not all zeros: the softmax's sum is taken of the probabilities themselves, whose reach
 //     has nothing to do with the values'.  (Looking for rows of zeros: 32 x 8192 with bf16 results 92.9 -> 95.5 us.)  (The warp-level product of
 //     8-bit operands is built from fp16 ones on this machine, at more instructions than these conversions: measured, 147 -> 179 us.)
-// Numerics: scores, maxima, sums and outputs are fp32.  Queries enter exactly (16-bit types) or as enough terms for fp32 (three
-// bf16 or two fp16 terms).  Probabilities: two bf16 or fp16 terms (2^-16, 2^-21), three bf16 for fp32 results of a bf16 cache; for bf16
-// results of codes one fp16 term (2^-11, an eighth of the result's own half step), where one bf16 term would be as large as it.
+// Numerics: scores, maxima, sums and outputs are fp32.  Queries enter exactly (16-bit types) or as three bf16 or two fp16 terms, and
+// probabilities as three bf16 or two fp16 terms whatever the results' type: 24 and 22 bits, so that the only rounding a caller
+// sees is the result's.  (One term less for 16-bit results moved them by up to 2^-18, bf16 results of codes by 2^-12, and took, 32 x 8192 with 4 and 16
+// query heads per KV head: bf16 174 and 173 us instead of 174 and 188, codes 98 and 143 instead of 102 and 157.)
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
@@ -54,9 +55,9 @@ struct PagedAttnParams {
     float scale_log2;
 };
 
-template <int D, int NT, int KV, int QT>
+template <int D, int NT, int KV, int TYPE>
 struct Shape {
-    static constexpr int kCtas = (NT == 1 && (QT == 1 || KV != NNC_BF16)) || (NT == 2 && D == 64 && QT == 1) ? 3 : 2;   // resident per SM
+    static constexpr int kCtas = (NT == 1 && (TYPE != NNC_F32 || KV != NNC_BF16)) || (NT == 2 && D == 64 && TYPE != NNC_F32) ? 3 : 2;   // resident per SM
     static constexpr int kBytes = KV == NNC_E4M3 ? 1 : 2;
     static constexpr int kRow = D * kBytes;                  // bytes of a row
     static constexpr int kPB = 4096 / kRow;                  // positions of a warp's block: 4 KB of keys, as many of values
@@ -203,14 +204,13 @@ template <int TYPE> __device__ __forceinline__ void store_out(const PagedAttnPar
     else reinterpret_cast<__half *>(p.out)[at] = __float2half_rn(v);
 }
 
-// QT, PT: terms of the queries and of the probabilities
-template <int D, int NT, int KV, int QT, int PT>
-__global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn_paged_kernel(const PagedAttnParams p) {
-    typedef Shape<D, NT, KV, QT> S;
+// NT: groups of 8 query heads; TYPE: the queries' and the results'
+template <int D, int NT, int KV, int TYPE>
+__global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) attn_paged_kernel(const PagedAttnParams p) {
+    typedef Shape<D, NT, KV, TYPE> S;
     constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3;
+    constexpr int PT = BF ? 3 : 2, QT = TYPE == NNC_F32 ? PT : 1;   // terms of the probabilities and of the queries
     constexpr int PB = S::kPB, TILE = S::kTile, ROW = S::kRow;
-    // the queries' and the results' type goes with the number of terms (launch_typed)
-    constexpr int TYPE = QT > 1 ? NNC_F32 : BF || (CODES && PT == 1) ? NNC_BF16 : NNC_F16;
     // fp16 probabilities are scaled by 2^14, so that small ones keep their bits (the sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 14.f;
     extern __shared__ __align__(128) char smem[];
@@ -943,11 +943,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, QT>::kCtas) attn
     }
 }
 
-template <int D, int NT, int KV, int QT, int PT>
+template <int D, int NT, int KV, int TYPE>
 cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
-    typedef Shape<D, NT, KV, QT> S;
+    typedef Shape<D, NT, KV, TYPE> S;
     static unsigned long long raised = 0;
-    auto kern = attn_paged_kernel<D, NT, KV, QT, PT>;
+    auto kern = attn_paged_kernel<D, NT, KV, TYPE>;
     cudaError_t e = ensure_dynamic_smem(kern, S::kSmem, &raised);
     if (e != cudaSuccess) return e;
     const long long most = ((long long)p.c.pages_per_seq << p.c.page_shift);
@@ -967,14 +967,12 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     return launch_smem(early, kern, dim3((unsigned)ctas, (unsigned)p.chunks), dim3(kWarps * 32), (size_t)S::kSmem, p);
 }
 
-// 16-bit results: queries as one exact term, probabilities as two (one, where that is far below the result's rounding); fp32
-// results: as many terms as fp32 has bits for
 template <int D, int NT>
 cudaError_t launch_typed(const LaunchCtx &lc, const PagedAttnParams &p, int kv, int type) {
-    const bool f32 = type == NNC_F32, bf16_out = type == NNC_BF16;
-    if (kv == NNC_BF16) return f32 ? launch_one<D, NT, NNC_BF16, 3, 3>(lc, p) : launch_one<D, NT, NNC_BF16, 1, 2>(lc, p);
-    if (kv == NNC_F16) return f32 ? launch_one<D, NT, NNC_F16, 2, 2>(lc, p) : launch_one<D, NT, NNC_F16, 1, 2>(lc, p);
-    return f32 ? launch_one<D, NT, NNC_E4M3, 2, 2>(lc, p) : bf16_out ? launch_one<D, NT, NNC_E4M3, 1, 1>(lc, p) : launch_one<D, NT, NNC_E4M3, 1, 2>(lc, p);
+    const bool f32 = type == NNC_F32;
+    if (kv == NNC_BF16) return f32 ? launch_one<D, NT, NNC_BF16, NNC_F32>(lc, p) : launch_one<D, NT, NNC_BF16, NNC_BF16>(lc, p);
+    if (kv == NNC_F16) return f32 ? launch_one<D, NT, NNC_F16, NNC_F32>(lc, p) : launch_one<D, NT, NNC_F16, NNC_F16>(lc, p);
+    return f32 ? launch_one<D, NT, NNC_E4M3, NNC_F32>(lc, p) : type == NNC_BF16 ? launch_one<D, NT, NNC_E4M3, NNC_BF16>(lc, p) : launch_one<D, NT, NNC_E4M3, NNC_F16>(lc, p);
 }
 
 }  // namespace

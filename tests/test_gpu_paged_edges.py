@@ -166,3 +166,30 @@ def test_16_bit_results_of_a_share_of_131072_positions_carry_no_drift(nnc, scrat
     # own rounding (2^-21) are systematic at most.
     allowed = 5 * torch.finfo(dtype).eps / 2 / math.sqrt(3 * batch * d) + 12 * 2.0 ** -23 + 2.0 ** -21
     assert abs(off) <= allowed, (off, allowed)
+
+
+# ---- what 16-bit results lose ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kv,dtype", [(BF16, BF16), (F16, F16), (E4M3, BF16), (E4M3, F16)], ids=str)
+def test_16_bit_results_are_rounded_once(nnc, scratch, kv, dtype):
+    """Two positions with exact scores: a result is the exact one's rounding, unless that lies within fp32's errors of a tie."""
+    batch, heads, group, d = 512, 4, 4, 64
+    g = _gen(31)
+    q, k = torch.zeros(batch, heads * group, d, device="cuda"), torch.zeros(2 * batch, heads, d, device="cuda")
+    q[..., 0], k[..., 0] = _randn(g, batch, heads * group), _randn(g, 2 * batch, heads).clamp(-2, 2)
+    q, v = q.clamp(-4, 4).to(dtype), _randn(g, 2 * batch, heads, d)
+    cache = nnc.PagedKV.empty(batch, 16, heads, d, kv, batch, 1)
+    cache.page_table[:, 0] = torch.arange(batch, device="cuda", dtype=torch.int32)
+    seq, pos = _ints([b for b in range(batch) for _ in range(2)]), _ints([0, 1] * batch)
+    nnc.op_kv_write_paged(cache, k, v, pos, seq)
+    out = nnc.op_attn_decode_paged(q, cache, _ints([2] * batch), scale=0.125, scratch=scratch)
+    hold = (lambda x: quantise64(x)[0]) if kv is E4M3 else (lambda x: x.to(kv).double())
+    k64, v64 = (hold(x).view(batch, 2, heads, d) for x in (k, v))
+    score = 0.125 * torch.einsum("bhgd,bnhd->bhgn", q.double().view(batch, heads, group, d), k64)
+    p = torch.softmax(score, -1)
+    want, size = (torch.einsum("bhgn,bnhd->bhgd", p, x).reshape(out.shape) for x in (v64, v64.abs()))
+    step = torch.exp2(torch.floor(torch.log2(want.abs().clamp(min=2.0 ** -14 if dtype is F16 else 2.0 ** -126)))) * torch.finfo(dtype).eps
+    # fp32 part, of sum p |v|: scores of at most 1.5 binary digits, from exact products (2^-23 of a weight), exp2 (2^-22) and the same in
+    # the other weight, the weights' terms (2^-22), sum, reciprocal and products (five times 2^-24): below 2^-20
+    off = (out.double() - want).abs() - step / 2 - 2.0 ** -20 * size
+    assert (off <= 0).all(), ((off > 0).sum().item(), (off / step).max().item())
