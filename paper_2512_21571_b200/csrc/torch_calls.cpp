@@ -254,8 +254,10 @@ PyObject *attn(PyObject *const *a) {
     }
     const bool want_lse = truth(a[8]);
     if (want_lse) lse = at::empty({in.tokens, in.heads}, q.options().dtype(at::kFloat));
-    if (a[6] == Py_None) scratch = at::zeros({(int64_t)NNC_ATTN_PAGED_SCRATCH_BYTES}, q.options().dtype(at::kByte));
-    else {
+    if (a[6] == Py_None) {   // the tickets alone have to be zero
+        scratch = at::empty({(int64_t)NNC_ATTN_PAGED_SCRATCH_BYTES}, q.options().dtype(at::kByte));
+        scratch.narrow(0, 0, NNC_ATTN_PAGED_TICKET_BYTES).zero_();
+    } else {
         scratch = tensor(a[6], "scratch");
         if (!scratch.is_cuda() || scratch.get_device() != device || !scratch.is_contiguous()) refuse("scratch: a contiguous tensor on the call's CUDA device (attn_paged_scratch)");
     }

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_paged import BF16, E4M3, F16, F32, _check_attention, _gen, _ints, _paged, _randn, nnc, quantise64, scratch  # noqa: F401
+from test_gpu_paged import BF16, E4M3, F16, F32, _check_attention, _fill, _gen, _ints, _paged, _randn, nnc, quantise64, scratch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -193,3 +193,25 @@ def test_16_bit_results_are_rounded_once(nnc, scratch, kv, dtype):
     # the other weight, the weights' terms (2^-22), sum, reciprocal and products (five times 2^-24): below 2^-20
     off = (out.double() - want).abs() - step / 2 - 2.0 ** -20 * size
     assert (off <= 0).all(), ((off > 0).sum().item(), (off / step).max().item())
+
+
+# ---- the binding -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("lens", [[5], [4097], [30011, 0, 70000]])
+def test_a_call_without_scratch_clears_the_tickets_of_its_own(nnc, scratch, lens):
+    """The scratch that such a call makes may be memory that held anything, and only its first bytes are cleared."""
+    cache = _paged(nnc, BF16, lens, 64, 2, 128, 1, nan=False)
+    _fill(nnc, cache, lens, 1)
+    q = _randn(_gen(3), len(lens), 8, 128, dtype=BF16)
+    want = nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch, want_lse=True)
+    for _ in range(3):
+        used = [torch.full((16 << 20,), 0xff, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        at = {t.data_ptr() for t in used}
+        del used
+        got = nnc.op_attn_decode_paged(q, cache, _ints(lens), want_lse=True)
+        own = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")      # the freed scratch again: what the call left
+        assert own.data_ptr() in at and not own[:8192].any()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        if lens == [5]:                                                     # one CTA per head: nothing is split, nothing else written
+            assert (own[8192:] == 0xff).all()
+        del own
