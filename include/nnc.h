@@ -383,7 +383,7 @@ int nnc_op_kv_read_paged(const nnc_paged_kv *cache, void *k, void *v, int32_t ty
  * scratch: DEVICE, 256-byte aligned, NNC_ATTN_PAGED_SCRATCH_BYTES; its first NNC_ATTN_PAGED_TICKET_BYTES must be zero before
  * the first call and are left zero by every call.  Calls that share a scratch must not overlap on the device (captured
  * graphs included).  Results do not depend on scheduling: partial results are joined in a fixed order.  q, out and
- * their strides are multiples of 16 bytes. */
+ * their strides are multiples of 16 bytes.  out may be q itself (with the same strides); other overlaps are not allowed. */
 #define NNC_ATTN_PAGED_SCRATCH_BYTES (16u << 20)
 #define NNC_ATTN_PAGED_TICKET_BYTES 8192
 int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, void *out, float *lse, int32_t type,

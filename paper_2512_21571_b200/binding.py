@@ -516,7 +516,7 @@ def op_kv_write_paged(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, pos: tor
 def op_kv_read_paged(cache: PagedKV, pos: torch.Tensor, seq: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
                      out=None):
     """nnc_op_kv_read_paged: (k, v), [tokens][n_kv_heads][head_dim], of positions `pos` of sequences `seq`.  out: None (then
-    padding tokens' rows hold anything), or a pair of tensors with the same strides."""
+    padding tokens' rows hold anything), or a pair of tensors with the same strides and no memory in common."""
     k, v = (None, None) if out is None else out
     return _calls.kv_read(cache.address, cache.index, pos, seq, dtype, k, v)
 
@@ -529,5 +529,6 @@ def attn_paged_scratch(device="cuda") -> torch.Tensor:
 def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, scale: Optional[float] = None, window: int = 0,
                          scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, want_lse: bool = False):
     """nnc_op_attn_decode_paged: q [batch][n_q_heads][head_dim] (rows may be apart) against the first lens[b] positions of each
-    sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  Returns out, or (out, lse)."""
+    sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  out: None, q itself, or a tensor of q's
+    shape and type that q does not overlap.  Returns out, or (out, lse)."""
     return _calls.attn(cache.address, cache.index, q, lens, scale, window, scratch, out, want_lse)

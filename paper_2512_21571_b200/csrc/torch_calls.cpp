@@ -94,6 +94,63 @@ bool disjoint(const at::Tensor &t) {
     return true;
 }
 
+// Memory that a call reads or writes: `size` bytes from `base` plus every sum of its steps, each taken 0 .. count - 1 times.
+struct Region {
+    struct Step { int64_t bytes, count; };
+    int64_t base, size;
+    Step steps[2];
+    bool empty() const { return size == 0 || steps[0].count == 0 || steps[1].count == 0; }
+    int64_t end() const { return base + steps[0].bytes * (steps[0].count - 1) + steps[1].bytes * (steps[1].count - 1) + size; }
+};
+
+Region region_of(const at::Tensor &t, const Rows &r) {
+    const int64_t el = t.element_size();
+    return {reinterpret_cast<int64_t>(t.data_ptr()), r.d * el, {{r.row * el, r.tokens}, {r.head * el, r.heads}}};
+}
+
+Region pool_of(const nnc_paged_kv &c, const void *pool) {   // as far as pages reach
+    const int64_t bytes = (c.type == NNC_E4M3 ? 1 : 2) * (int64_t)c.n_kv_heads * c.page_size * c.head_dim * c.n_pages;
+    return {reinterpret_cast<int64_t>(pool), bytes, {{0, 1}, {0, 1}}};
+}
+
+struct Term { int64_t bytes, lo, hi; };   // taken lo .. hi times
+
+// whether apart + (a sum of the terms from `at` on) can lie in [lo, hi].  Terms are sorted, longest first, so that each leaves few choices.
+bool reaches(int64_t apart, const Term *at, const Term *end, int64_t lo, int64_t hi) {
+    if (at == end) return lo <= apart && apart <= hi;
+    int64_t least = 0, most = 0;
+    for (const Term *t = at + 1; t != end; ++t) { least += t->lo * t->bytes; most += t->hi * t->bytes; }
+    auto floor_div = [](int64_t a, int64_t b) { return a / b - (a % b != 0 && a < 0); };
+    const int64_t first = std::max(at->lo, -floor_div(apart + most - lo, at->bytes)), last = std::min(at->hi, floor_div(hi - apart - least, at->bytes));
+    for (int64_t n = first; n <= last; ++n)
+        if (reaches(apart + n * at->bytes, at + 1, end, lo, hi)) return true;
+    return false;
+}
+
+// whether two regions have a byte in common, exactly
+bool meet(const Region &a, const Region &b) {
+    if (a.empty() || b.empty() || a.end() <= b.base || b.end() <= a.base) return false;
+    Term terms[4];
+    int n = 0;
+    auto add = [&](const Region::Step &s, int64_t lo, int64_t hi) {
+        if (s.bytes == 0 || s.count == 1) return;
+        for (int i = 0; i < n; ++i)
+            if (terms[i].bytes == s.bytes) { terms[i].lo += lo; terms[i].hi += hi; return; }   // the difference of the two alone matters
+        terms[n++] = {s.bytes, lo, hi};
+    };
+    for (const Region::Step &s : a.steps) add(s, 0, s.count - 1);
+    for (const Region::Step &s : b.steps) add(s, 1 - s.count, 0);
+    std::sort(terms, terms + n, [](const Term &x, const Term &y) { return x.bytes > y.bytes; });
+    return reaches(a.base - b.base, terms, terms + n, 1 - a.size, b.size - 1);
+}
+
+// out may be `in` itself, and otherwise has nothing in common with it
+void apart_or_same(const Region &out, const Region &in, const char *refusal) {
+    bool same = out.base == in.base;
+    for (int i = 0; i < 2; ++i) same = same && out.steps[i].bytes == in.steps[i].bytes;
+    if (!same && meet(out, in)) refuse(refusal);
+}
+
 void raise_status(int status, const char *what) {
     PyObject *e = PyObject_CallFunction(error_class, "is", status, what);
     if (e) {
@@ -163,6 +220,7 @@ PyObject *rope(PyObject *const *a) {
         out = tensor(a[6], "out");
         to = rows_of(out, device, "out");
         if (!to.like(in) || !disjoint(out)) refuse("out: x's shape and type, no rows that overlap");
+        apart_or_same(region_of(out, to), region_of(x, in), "out: x itself, or memory that x has no part of");
     }
     const bool interleaved = truth(a[3]), inverse = truth(a[5]);
     const float amplitude = number(a[4]);
@@ -185,6 +243,9 @@ PyObject *kv_write(PyObject *const *a) {
     const Rows rk = rows_of(k, device, "k"), rv = rows_of(v, device, "v");
     if (!rv.like(rk) || rv.row != rk.row || rv.head != rk.head || rk.heads != c.n_kv_heads || rk.d != c.head_dim)
         refuse("k, v: [tokens][n_kv_heads][head_dim] of the cache, of one type with the same strides");
+    for (const void *pool : {c.k, c.v})
+        for (const at::Tensor *t : {&k, &v})
+            if (meet(region_of(*t, rk), pool_of(c, pool))) refuse("k, v: memory that the cache has no part of");
     const int32_t *at_pos = index_of(pos, rk.tokens, device, "pos");
     const int32_t *at_seq = a[5] == Py_None ? nullptr : index_of(tensor(a[5], "seq"), rk.tokens, device, "seq");
     launch(device, "nnc_op_kv_write_paged", [&](void *stream) {
@@ -208,6 +269,7 @@ PyObject *kv_read(PyObject *const *a) {
     }
     at::Tensor k, v;
     Rows r{};
+    if ((a[5] == Py_None) != (a[6] == Py_None)) refuse("out: two tensors, or None");
     if (a[5] == Py_None) {
         const auto options = at::TensorOptions().dtype(dtype).device(at::kCUDA, static_cast<c10::DeviceIndex>(device));
         k = at::empty({tokens, c.n_kv_heads, c.head_dim}, options);
@@ -221,6 +283,10 @@ PyObject *kv_read(PyObject *const *a) {
         if (!rv.like(r) || rv.row != r.row || rv.head != r.head || r.tokens != tokens || r.heads != c.n_kv_heads || r.d != c.head_dim ||
             (a[4] != Py_None && r.type != type_of(dtype)) || !disjoint(k) || !disjoint(v))
             refuse("out: two tensors [tokens][n_kv_heads][head_dim] of one type with the same strides, no rows that overlap");
+        if (meet(region_of(k, r), region_of(v, r))) refuse("out: two tensors with no memory in common");
+        for (const void *pool : {c.k, c.v})
+            for (const at::Tensor *t : {&k, &v})
+                if (meet(region_of(*t, r), pool_of(c, pool))) refuse("out: memory that the cache has no part of");
     }
     const int32_t *at_pos = index_of(pos, tokens, device, "pos");
     const int32_t *at_seq = a[3] == Py_None ? nullptr : index_of(tensor(a[3], "seq"), tokens, device, "seq");
@@ -251,6 +317,9 @@ PyObject *attn(PyObject *const *a) {
         out = tensor(a[7], "out");
         to = rows_of(out, device, "out");
         if (!to.like(in) || to.head != in.d || !disjoint(out)) refuse("out: q's shape and type, heads next to each other, no rows that overlap");
+        apart_or_same(region_of(out, to), region_of(q, in), "out: q itself, or memory that q has no part of");
+        for (const void *pool : {c.k, c.v})
+            if (meet(region_of(out, to), pool_of(c, pool))) refuse("out: memory that the cache has no part of");
     }
     const bool want_lse = truth(a[8]);
     if (want_lse) lse = at::empty({in.tokens, in.heads}, q.options().dtype(at::kFloat));

@@ -215,3 +215,73 @@ def test_a_call_without_scratch_clears_the_tickets_of_its_own(nnc, scratch, lens
         if lens == [5]:                                                     # one CTA per head: nothing is split, nothing else written
             assert (own[8192:] == 0xff).all()
         del own
+
+
+def test_outputs_that_overlap_what_a_call_reads_are_refused(nnc, scratch):
+    """Exactly those: parts of one buffer that have no element in common are as good as two buffers."""
+    freq, _ = nnc.rope_frequencies(64)
+    pos = _ints([3, 5, 7, 9])
+    buf = torch.zeros(20000, dtype=BF16, device="cuda")
+    rows = lambda at, row, head: torch.as_strided(buf, (4, 3, 64), (row, head, 1), at)
+    touches = lambda a, b: bool(set(_elements(a)) & set(_elements(b)))
+    _elements = lambda t: torch.arange(20000).as_strided(t.shape, t.stride(), t.storage_offset()).flatten().tolist()
+    g = torch.Generator().manual_seed(2)
+    kinds = [(192, 64), (64, 256), (1000, 72), (384, 128), (400, 128), (72, 1000), (200, 64), (1, 64 * 8), (64, 0)]
+    seen = set()
+    for _ in range(400):
+        (rx, hx), (ry, hy) = (kinds[int(torch.randint(len(kinds) if i == 0 else len(kinds) - 2, (1,), generator=g))] for i in range(2))
+        ax, ay = (int(torch.randint(0, 600, (1,), generator=g)) for _ in range(2))
+        x, y = rows(ax, rx, hx), rows(ay, ry, hy)
+        if x.data_ptr() == y.data_ptr() and x.stride() == y.stride():
+            continue
+        seen.add(touches(x, y))
+        if touches(x, y):
+            with pytest.raises(ValueError, match="no part of"):
+                nnc.op_rope(x, pos, freq, out=y)
+        else:
+            assert nnc.op_rope(x, pos, freq, out=y) is y
+    assert seen == {False, True}
+    fused = torch.zeros(5, 12, 64, dtype=BF16, device="cuda")                       # heads of one projection, next to one another
+    five = _ints([0] * 5)
+    nnc.op_rope(fused[:, :4], five, freq, out=fused[:, 4:8])
+    nnc.op_rope(fused[:, :4], five, freq, out=fused[:, :4])
+    for out in (fused[:, 3:7], fused[:, 1:5]):
+        with pytest.raises(ValueError):
+            nnc.op_rope(fused[:, :4], five, freq, out=out)
+    nnc.op_rope(fused[:1, :4], five[:1], freq, out=fused[1:2, :4])
+    # the cache's operations
+    cache = _paged(nnc, BF16, [40], 16, 2, 64, 1)
+    held = _fill(nnc, cache, [40], 1)
+    three, zero = _ints([1, 2, 30]), _ints([0, 0, 0])
+    pair = torch.zeros(3, 4, 64, dtype=BF16, device="cuda")
+    nnc.op_kv_read_paged(cache, three, zero, out=(pair[:, :2], pair[:, 2:]))
+    pool = cache.k.flatten(0, 2)[:6].view(3, 2, 64)
+    for out in ((pair[:, :2], pair[:, :2]), (pair[:, :2], pair[:, 1:3]), (None, pair[:, :2]), (pair[:, :2], pool), (pool, pair[:, :2])):
+        with pytest.raises(ValueError):
+            nnc.op_kv_read_paged(cache, three, zero, out=out)
+    with pytest.raises(ValueError):
+        nnc.op_kv_write_paged(cache, pool, torch.zeros_like(pool), three, zero)
+    # attention: q itself is allowed, its neighbours are not
+    q = _randn(_gen(4), 1, 8, 64, dtype=BF16)
+    want = nnc.op_attn_decode_paged(q, cache, _ints([40]), scratch=scratch)
+    wide = torch.zeros(1, 16, 64, dtype=BF16, device="cuda")
+    wide[:, 2:10] = q
+    with pytest.raises(ValueError):
+        nnc.op_attn_decode_paged(wide[:, 2:10], cache, _ints([40]), scratch=scratch, out=wide[:, 4:12])
+    nnc.op_attn_decode_paged(wide[:, 2:10], cache, _ints([40]), scratch=scratch, out=wide[:, 2:10])
+    assert torch.equal(wide[:, 2:10], want) and not wide[:, :2].any() and not wide[:, 10:].any()
+
+
+@pytest.mark.parametrize("kv,dtype", [(BF16, BF16), (E4M3, F32)], ids=str)
+@pytest.mark.parametrize("heads,group", [(2, 4), (1, 16), (1, 40)])
+def test_attention_over_its_own_queries(nnc, scratch, kv, dtype, heads, group):
+    lens = [30000, 0, 17, 9000]
+    cache = _paged(nnc, kv, lens, 64, heads, 128, 1)
+    _fill(nnc, cache, lens, 1)
+    q = _randn(_gen(3), len(lens), heads * group, 128, dtype=dtype)
+    want, lse = nnc.op_attn_decode_paged(q, cache, _ints(lens), scratch=scratch, want_lse=True)
+    for _ in range(5):
+        own = q.clone()
+        got, again = nnc.op_attn_decode_paged(own, cache, _ints(lens), scratch=scratch, out=own, want_lse=True)
+        assert got is own or got.data_ptr() == own.data_ptr()
+        assert torch.equal(own, want) and torch.equal(lse, again)
