@@ -457,10 +457,33 @@ def rope_frequencies(rotary_dim: int, theta: float = 1e6, scaling: str = "plain"
     return freq.to(device), amplitude.value
 
 
+class _Rope(torch.autograd.Function):
+    """op_rope for an x that requires a gradient: the rotation is linear, and its transpose is the inverse rotation."""
+
+    @staticmethod
+    def forward(ctx, x, positions, freq, interleaved, amplitude, inverse):
+        ctx.save_for_backward(positions, freq)
+        ctx.how = interleaved, amplitude, inverse
+        return _calls.rope(x, positions, freq, interleaved, amplitude, inverse, None)
+
+    @staticmethod
+    def backward(ctx, grad):
+        positions, freq = ctx.saved_tensors
+        interleaved, amplitude, inverse = ctx.how
+        if grad.stride(-1) != 1:   # a sum's gradient is one number, expanded
+            grad = grad.contiguous()
+        return op_rope(grad, positions, freq, interleaved, amplitude, not inverse), None, None, None, None, None
+
+
 def op_rope(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0,
             inverse: bool = False, out: Optional[torch.Tensor] = None):
     """nnc_op_rope: x [tokens][heads][head_dim] (any strides between rows and heads) turned by int32 `positions`; the first
-    2 * len(freq) elements of each head turn.  out: None, x itself, or a tensor of x's shape and type that x does not overlap."""
+    2 * len(freq) elements of each head turn.  out: None, x itself, or a tensor of x's shape and type that x does not overlap.
+    Gradients flow through it with respect to x, if out is None; `positions` and `freq` stay as they are until the backward pass."""
+    if getattr(x, "requires_grad", False) and torch.is_grad_enabled():
+        if out is not None:
+            raise ValueError("out: None for an x that requires a gradient")
+        return _Rope.apply(x, positions, freq, interleaved, amplitude, inverse)
     return _calls.rope(x, positions, freq, interleaved, amplitude, inverse, out)
 
 
@@ -509,7 +532,8 @@ class PagedKV:
 
 def op_kv_write_paged(cache: PagedKV, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, seq: Optional[torch.Tensor] = None):
     """nnc_op_kv_write_paged: rows k, v [tokens][n_kv_heads][head_dim] to positions `pos` of sequences `seq` (None: token t is
-    sequence t's).  k and v have the same strides (slices of one fused projection do)."""
+    sequence t's).  k and v have the same strides (slices of one fused projection do).  The cache's operations and its attention are
+    for serving: no gradient flows through them."""
     _calls.kv_write(cache.address, cache.index, k, v, pos, seq)
 
 

@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -127,6 +128,14 @@ bool reaches(int64_t apart, const Term *at, const Term *end, int64_t lo, int64_t
     return false;
 }
 
+// A tensor that a call writes to.  Where autograd keeps it for a backward pass, that pass has to see that it changed.
+void written(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void writable(const at::Tensor &t) {
+    if (t.requires_grad() && c10::GradMode::is_enabled()) refuse("out: no tensor that requires a gradient");
+}
+
 // whether two regions have a byte in common, exactly
 bool meet(const Region &a, const Region &b) {
     if (a.empty() || b.empty() || a.end() <= b.base || b.end() <= a.base) return false;
@@ -219,6 +228,7 @@ PyObject *rope(PyObject *const *a) {
     } else {
         out = tensor(a[6], "out");
         to = rows_of(out, device, "out");
+        writable(out);
         if (!to.like(in) || !disjoint(out)) refuse("out: x's shape and type, no rows that overlap");
         apart_or_same(region_of(out, to), region_of(x, in), "out: x itself, or memory that x has no part of");
     }
@@ -229,6 +239,7 @@ PyObject *rope(PyObject *const *a) {
                          static_cast<const double *>(freq.data_ptr()), (int32_t)(2 * freq.size(0)), interleaved, inverse, amplitude, stream);
     });
     if (a[6] != Py_None) {
+        written(out);
         Py_INCREF(a[6]);
         return a[6];
     }
@@ -279,6 +290,8 @@ PyObject *kv_read(PyObject *const *a) {
         k = tensor(a[5], "out");
         v = tensor(a[6], "out");
         r = rows_of(k, device, "out");
+        writable(k);
+        writable(v);
         const Rows rv = rows_of(v, device, "out");
         if (!rv.like(r) || rv.row != r.row || rv.head != r.head || r.tokens != tokens || r.heads != c.n_kv_heads || r.d != c.head_dim ||
             (a[4] != Py_None && r.type != type_of(dtype)) || !disjoint(k) || !disjoint(v))
@@ -293,6 +306,10 @@ PyObject *kv_read(PyObject *const *a) {
     launch(device, "nnc_op_kv_read_paged", [&](void *stream) {
         return call_read(&c, k.data_ptr(), v.data_ptr(), r.type, (int32_t)tokens, r.row, r.head, at_pos, at_seq, stream);
     });
+    if (a[5] != Py_None) {
+        written(k);
+        written(v);
+    }
     return pair(k, v);
 }
 
@@ -316,6 +333,7 @@ PyObject *attn(PyObject *const *a) {
     } else {
         out = tensor(a[7], "out");
         to = rows_of(out, device, "out");
+        writable(out);
         if (!to.like(in) || to.head != in.d || !disjoint(out)) refuse("out: q's shape and type, heads next to each other, no rows that overlap");
         apart_or_same(region_of(out, to), region_of(q, in), "out: q itself, or memory that q has no part of");
         for (const void *pool : {c.k, c.v})
@@ -334,6 +352,7 @@ PyObject *attn(PyObject *const *a) {
         return call_attn(q.data_ptr(), &c, at_lens, out.data_ptr(), want_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, in.type, (int32_t)in.tokens,
                          (int32_t)in.heads, in.row, to.row, scale, (int32_t)window, scratch.data_ptr(), scratch.nbytes(), stream);
     });
+    if (a[7] != Py_None) written(out);
     if (want_lse) return pair(out, lse);
     return THPVariable_Wrap(out);
 }

@@ -285,3 +285,61 @@ def test_attention_over_its_own_queries(nnc, scratch, kv, dtype, heads, group):
         got, again = nnc.op_attn_decode_paged(own, cache, _ints(lens), scratch=scratch, out=own, want_lse=True)
         assert got is own or got.data_ptr() == own.data_ptr()
         assert torch.equal(own, want) and torch.equal(lse, again)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_gradients_flow_through_the_rotation(nnc, interleaved, dtype):
+    """x + R x, a step further through autograd: the gradient is g + R^T g, the second derivative of a quadratic the product of both."""
+    g = _gen(8)
+    freq, _ = nnc.rope_frequencies(48, 1e4)
+    pos = _ints([2, 1000, 70001, 5])
+    rope = lambda t, **kw: nnc.op_rope(t, pos, freq, interleaved=interleaved, amplitude=1.5, **kw)
+    x, up = (_randn(g, 4, 3, 80, dtype=dtype) for _ in range(2))
+    leaf = x.clone().requires_grad_()
+    y = rope(leaf)
+    assert y.requires_grad and torch.equal(y.detach(), rope(x))
+    y.backward(up)
+    assert torch.equal(leaf.grad, rope(up, inverse=True))
+    leaf.grad = None
+    rope(leaf).sum().backward()                                       # an expanded gradient
+    assert torch.equal(leaf.grad, rope(torch.ones_like(x), inverse=True))
+    part = torch.zeros(4, 5, 80, dtype=dtype, device="cuda", requires_grad=True)       # some heads of a fused projection, not contiguous
+    rope(part[:, 1:4], inverse=True).backward(up)
+    assert torch.equal(part.grad[:, 1:4], rope(up)) and not part.grad[:, [0, 4]].any()
+    first, = torch.autograd.grad(rope(leaf), leaf, up.requires_grad_(), create_graph=True)
+    second, = torch.autograd.grad(first, up, x)
+    assert torch.equal(second, rope(x))
+    with torch.no_grad():
+        assert not rope(leaf).requires_grad
+    for out in (torch.empty_like(x), leaf):
+        with pytest.raises(ValueError):
+            rope(leaf, out=out)
+    with pytest.raises(ValueError):
+        rope(x, out=leaf)
+    with torch.no_grad():
+        rope(x, out=leaf)
+
+
+def test_gradients_notice_what_changed_before_them(nnc, scratch):
+    freq, _ = nnc.rope_frequencies(64)
+    pos = _ints([4])
+    leaf = torch.ones(1, 1, 64, device="cuda", requires_grad=True)
+    y = nnc.op_rope(leaf, pos, freq)
+    pos += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    kept = torch.ones(1, 1, 64, dtype=BF16, device="cuda")
+    cache = _paged(nnc, BF16, [1], 16, 1, 64, 1)
+    _fill(nnc, cache, [1], 1)
+    for overwrite in (lambda t: nnc.op_rope(t, pos, freq, out=t), lambda t: nnc.op_attn_decode_paged(t, cache, _ints([1]), scratch=scratch, out=t),
+                      lambda t: nnc.op_kv_read_paged(cache, _ints([0]), out=(t, torch.empty_like(t))),
+                      lambda t: nnc.op_kv_read_paged(cache, _ints([0]), out=(torch.empty_like(t), t))):
+        weight = torch.ones(1, 1, 64, dtype=BF16, device="cuda", requires_grad=True)
+        y = weight * kept                                             # keeps `kept` for the gradient
+        overwrite(kept)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    with torch.inference_mode():
+        t = torch.ones(1, 1, 64, dtype=BF16, device="cuda")
+        nnc.op_rope(t, pos, freq, out=t)
