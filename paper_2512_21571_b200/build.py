@@ -47,24 +47,31 @@ CALLS = os.path.join(_HERE, "_calls.so")   # marshalling of the paged-cache oper
 
 
 def build_calls(force: bool = False) -> str:
-    """Builds the extension module _calls.so with g++ against the headers of the running Python and torch."""
+    """Builds the extension module _calls.so with g++ against the headers of the running Python and torch; again when its sources
+    change, and when it was built for another Python or torch or with another command (CALLS.stamp says which)."""
+    import sys
     import sysconfig
-    src = os.path.join(CSRC, "torch_calls.cpp")
-    newest = max(os.path.getmtime(p) for p in (src, os.path.join(os.path.dirname(_HERE), "include", "nnc.h")))
-    if not force and os.path.exists(CALLS) and os.path.getmtime(CALLS) >= newest:
-        return CALLS
     import torch
+    src = os.path.join(CSRC, "torch_calls.cpp")
     root = os.path.dirname(torch.__file__)
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           *["-I" + i for i in include], src, "-o", CALLS + ".new", "-L" + os.path.join(root, "lib"), "-ltorch_cpu", "-lc10", "-lc10_cuda",
-           "-ltorch_python"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    compiler = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                *["-I" + i for i in include]]
+    libraries = ["-L" + os.path.join(root, "lib"), "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ltorch_python"]
+    stamp = "\n".join([sys.version, torch.__version__, *compiler, *libraries])   # (wherever this tree lies)
+    newest = max(os.path.getmtime(p) for p in (src, os.path.join(os.path.dirname(_HERE), "include", "nnc.h")))
+    if not force and os.path.exists(CALLS) and os.path.getmtime(CALLS) >= newest and os.path.exists(CALLS + ".stamp"):
+        with open(CALLS + ".stamp") as f:
+            if f.read() == stamp:
+                return CALLS
+    r = subprocess.run([*compiler, src, "-o", CALLS + ".new", *libraries], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed for {src}:\n{r.stdout}\n{r.stderr}")
     os.replace(CALLS + ".new", CALLS)
+    with open(CALLS + ".stamp", "w") as f:
+        f.write(stamp)
     return CALLS
 
 
