@@ -429,10 +429,20 @@ def op_attn_prefill_f16(qkv: torch.Tensor, k16: torch.Tensor, v16: torch.Tensor,
 try:
     from . import _calls
 except ImportError as e:
-    raise ImportError("paper_2512_21571_b200/_calls.so is missing or does not fit this torch: build it with "
-                      "`python -m paper_2512_21571_b200.build` (or __graft_entry__.build()); there is no fallback implementation") from e
-_calls.bind(*(C.cast(getattr(lib, n), C.c_void_p).value for n in
-              ("nnc_op_rope", "nnc_op_kv_write_paged", "nnc_op_kv_read_paged", "nnc_op_attn_decode_paged")), NncError)
+    class _Missing:
+        """Stands in for _calls: the model and the operations that ctypes marshals do not need it, the others raise."""
+
+        def __init__(self, why):
+            self._why = why
+
+        def __getattr__(self, name):
+            raise ImportError("paper_2512_21571_b200/_calls.so is missing or does not fit this torch: build it with "
+                              "`python -m paper_2512_21571_b200.build` (or __graft_entry__.build()); there is no fallback implementation") from self._why
+
+    _calls = _Missing(e)
+else:
+    _calls.bind(*(C.cast(getattr(lib, n), C.c_void_p).value for n in
+                  ("nnc_op_rope", "nnc_op_kv_write_paged", "nnc_op_kv_read_paged", "nnc_op_attn_decode_paged")), NncError)
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp_turns": 3, "ramp_index": 4}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}

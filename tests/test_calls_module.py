@@ -1,6 +1,7 @@
-"""The extension module that marshals the paged-cache operations (_calls.so): when it is built."""
+"""The extension module that marshals the paged-cache operations (_calls.so): when it is built, and what works without it."""
 import os
 import subprocess
+import sys
 
 import pytest
 
@@ -49,3 +50,30 @@ def test_a_module_without_a_stamp_is_built_again(compiler):
         f.write("of unknown origin")
     build.build_calls()
     assert len(runs) == 1 and open(build.CALLS).read() == "built 1"
+
+
+def test_the_rest_of_the_binding_does_without_the_module():
+    from paper_2512_21571_b200 import build
+    build.build()
+    prog = """
+import sys
+sys.path.insert(0, %r)
+sys.modules["paper_2512_21571_b200._calls"] = None          # as if it were missing
+from paper_2512_21571_b200 import binding as nnc
+import torch
+assert nnc.Model and nnc.bounds_check_report() == (-1, 0)
+freq, amplitude = nnc.rope_frequencies(64, device="cpu")
+assert freq[0] == 1.0
+x = torch.zeros(2, 2, 64)
+pos = torch.zeros(2, dtype=torch.int32)
+for call in (lambda: nnc.op_rope(x, pos, freq), lambda: nnc.op_rope(x, pos, freq, out=x)):
+    try:
+        call()
+    except ImportError as e:
+        assert "paper_2512_21571_b200.build" in str(e) and e.__cause__ is not None
+    else:
+        raise AssertionError("no error")
+print("done")
+""" % os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", prog], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "done" in r.stdout, r.stdout + r.stderr
