@@ -221,7 +221,7 @@ int nnc_op_gemm_swiglu_f16(const void *X, const void *W, void *Y, int32_t T, int
 int nnc_op_to_f16_scaled(const void *src, void *dst, size_t n, float *scales, uint32_t *scratch_word, void *cuda_stream);
 
 /* Status word of the nnc_op_* kernels (0 = no tensor-core kernel's bounded wait ran out and no paged-cache kernel met
- * an address out of range: NNC_STATUS_PAGED_ADDRESS); synchronises the device and clears the word.  status_out is a
+ * an address out of range: NNC_STATUS_PAGED_ADDRESS, beside the last code); synchronises the device and clears the word.  status_out is a
  * HOST pointer. */
 #define NNC_STATUS_PAGED_ADDRESS 0x100
 int nnc_op_status(int32_t *status_out);

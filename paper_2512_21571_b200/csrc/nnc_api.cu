@@ -731,12 +731,14 @@ int nnc_trace_dump(void *out, int max_records) {
 
 // ---- single operations ------------------------------------------------------------------------------
 
-static __device__ int g_op_status;
+// Two words that nnc_op_status reads as one: tensor-core kernels store a code in theirs when a wait runs out, paged-cache kernels set
+// a bit in theirs, which such a store must not erase.
+static __device__ int g_op_status[2];
 static __device__ uint32_t g_op_gemv_ctr[8][4];   // work counters of the last 8 nnc_op_gemv calls, used in rotation
 
 // What a device's calls have in common, looked up by its first one.
 struct OpDevice {
-    int sms, *status;
+    int sms, *status;   // status: the two words
     bool known;
 };
 static OpDevice g_op_devices[64];
@@ -840,9 +842,11 @@ int nnc_op_to_f16_scaled(const void *src, void *dst, size_t n, float *scales, ui
 
 int nnc_op_status(int32_t *status_out) {
     if (!status_out) return NNC_ERR_INVALID_ARG;
-    int zero = 0;
-    if (cudaMemcpyFromSymbol(status_out, g_op_status, 4) != cudaSuccess) return NNC_ERR_CUDA;
-    if (cudaMemcpyToSymbol(g_op_status, &zero, 4) != cudaSuccess) return NNC_ERR_CUDA;
+    int words[2];
+    const int zero[2] = {0, 0};
+    if (cudaMemcpyFromSymbol(words, g_op_status, sizeof words) != cudaSuccess) return NNC_ERR_CUDA;
+    if (cudaMemcpyToSymbol(g_op_status, zero, sizeof zero) != cudaSuccess) return NNC_ERR_CUDA;
+    *status_out = words[0] | words[1];
     return *status_out ? NNC_ERR_DEVICE_STATUS : NNC_OK;
 }
 
@@ -992,6 +996,12 @@ int nnc_op_rope(const void *x, void *y, int32_t type, int32_t n_tokens, int32_t 
     return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
 }
 
+static int paged_ctx(LaunchCtx &lc, void *stream) {
+    const int rc = op_ctx(lc, stream);
+    if (rc == NNC_OK) ++lc.status;   // the paged-cache kernels' word
+    return rc;
+}
+
 static bool paged_ok(const nnc_paged_kv *c) {
     if (!c || !c->k || !c->v || !c->page_table) return false;
     if (c->type != NNC_BF16 && c->type != NNC_F16 && c->type != NNC_E4M3) return false;
@@ -1014,7 +1024,7 @@ static int kv_rows_paged(const nnc_paged_kv *cache, bool write, void *k, void *v
     if (((uintptr_t)pos | (uintptr_t)seq) & 3) return NNC_ERR_INVALID_ARG;
     if ((int64_t)n_tokens * cache->n_kv_heads > 0x7fffffff) return NNC_ERR_CAPACITY;   // rows are counted in 32 bits
     LaunchCtx lc;
-    if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
     return launch_kv_paged(lc, *cache, write, k, v, type, n_tokens, row_stride, head_stride, pos, seq) == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
 }
 
@@ -1043,7 +1053,7 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
     if (((uintptr_t)lens | (uintptr_t)lse) & 3) return NNC_ERR_INVALID_ARG;
     if (((uintptr_t)scratch & 255) || scratch_bytes < NNC_ATTN_PAGED_SCRATCH_BYTES) return NNC_ERR_WORKSPACE;
     LaunchCtx lc;
-    if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
     cudaError_t e = launch_attn_paged(lc, q, *cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, window, scratch,
                                       scratch_bytes);
     if (e == cudaErrorInvalidValue) return NNC_ERR_CAPACITY;
