@@ -844,6 +844,7 @@ int nnc_op_status(int32_t *status_out) {
     if (!status_out) return NNC_ERR_INVALID_ARG;
     int words[2];
     const int zero[2] = {0, 0};
+    if (cudaDeviceSynchronize() != cudaSuccess) return NNC_ERR_CUDA;   // the copies wait for the default stream alone
     if (cudaMemcpyFromSymbol(words, g_op_status, sizeof words) != cudaSuccess) return NNC_ERR_CUDA;
     if (cudaMemcpyToSymbol(g_op_status, zero, sizeof zero) != cudaSuccess) return NNC_ERR_CUDA;
     *status_out = words[0] | words[1];

@@ -64,3 +64,22 @@ print("done")
 def test_codes_and_the_bit_of_bad_addresses_leave_one_another(planting_lib):
     r = subprocess.run([sys.executable, "-c", _CHILD], capture_output=True, text=True, timeout=300, env={**os.environ, "NNC_LIBRARY": planting_lib})
     assert r.returncode == 0 and "done" in r.stdout, r.stdout + r.stderr
+
+
+@pytest.mark.gpu
+def test_the_status_waits_for_every_stream():
+    """Streams that do not synchronise with the default one included."""
+    import torch
+    from paper_2512_21571_b200 import binding as nnc
+    cache = nnc.PagedKV.empty(1, 16, 1, 64, torch.bfloat16, 1, 1)
+    pos = torch.zeros(1, dtype=torch.int32, device="cuda")
+    nnc.op_kv_read_paged(cache, pos)
+    assert nnc.op_status() == 0x100
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)      # some 50 ms
+            nnc.op_kv_read_paged(cache, pos)
+        assert nnc.op_status() == 0x100
+    assert nnc.op_status() == 0
