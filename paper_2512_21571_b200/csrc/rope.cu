@@ -274,7 +274,6 @@ cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, i
     p.abreast = (int)abreast;
     const bool many = n > 1 && n_tokens >= 4ll * abreast * m * lc.sm_count;
     long long tokens = abreast * (many ? m : 1);
-    if (n == 1) tokens = 1;
     p.tokens_per_cta = (int)tokens;
     const dim3 grid((unsigned)((n_tokens + tokens - 1) / tokens)), block((unsigned)((threads + 31) / 32 * 32));
     const int smem = (int)(tokens * half * sizeof(float2));
