@@ -306,8 +306,9 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
         for (int u = 0; u < S::kSub; ++u) {
             const int pb = p0 + 16 * u;
             if (pb >= ahead.r.end) break;
-            const bool there = (unsigned)pages[u] < (unsigned)p.c.n_pages;
+            const bool there = (unsigned)pages[u] < (unsigned)p.c.n_pages && NNC_BC(ahead.b < p.batch && ahead.head < p.c.n_kv && stage < S::kStages, 3202);
             const long long row = there ? paged_row(p.c, pages[u], ahead.head, pb & ((1 << p.c.page_shift) - 1)) : 0;
+            if (!NNC_BC(row >= 0 && row + 16 <= paged_rows(p.c), 3203)) continue;
             const char *ks = p.c.k + row * ROW + lane * 16, *vs = p.c.v + row * ROW + lane * 16;   // 16 rows are one run of bytes
             if (there && pb >= ahead.r.start && pb + 16 <= ahead.r.end) {
 #pragma unroll
@@ -683,6 +684,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
                 for (int i = 0; i < S::kTilesD; ++i) all_sums += (o[nt][i][0] + o[nt][i][1]) + (o[nt][i][2] + o[nt][i][3]);
         }
         bool odd = !(fabsf(all_sums) < INFINITY);
+        if (!NNC_BC(now.b < p.batch && now.head < p.c.n_kv && heads_here > 0 && (chunk * (8 * NT)) + heads_here <= p.group, 3205)) return;
         if (!whole && !NNC_BC((size_t)(2 * (chunk * gridDim.x + cta) + 2) * S::kSlotFloats <= p.part_floats, 3201)) return;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -830,7 +832,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
         // tickets: [0, max) for an item's first (or only) group, [max, 2 max) for its later ones (their first CTA may start another
         // item's first group), [2 max, 3 max) for the groups' results
         uint32_t *ticket = tickets + (group ? kPagedMaxCtas : 0) + g_lo;
-        s.last = take_ticket(ticket, expected);
+        s.last = NNC_BC(g_lo >= 0 && chunk * (int)gridDim.x + g_lo < kPagedMaxCtas && s.c_hi < (int)gridDim.x, 3204) && take_ticket(ticket, expected);
     }
     __syncthreads();
     // The rows to be joined come into the ring's memory, all of them requested at once (a loop of copies and a loop of sums: this
@@ -859,6 +861,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
             }
             copy_commit();
             const int fit = kWarps * S::kStages * S::kStage / (cols * 16);   // pieces that the ring holds at a time (10 at least)
+            if (!NNC_BC(n > 0 && n <= S::kMaxJoin && fit > 0 && c0 + (n - 1) * apart <= c_hi, 3206)) break;
             for (int lo = 0; lo < n; lo += fit) {
                 const int hi = min(lo + fit, n);
                 for (int col = tid; col < cols; col += kWarps * 32) {

@@ -202,6 +202,7 @@ __global__ void __launch_bounds__(256) kv_rows_kernel(const RowsParams p) {
             if (lane == 0 && h[i] == 0) paged_complain(p.c);
         }
         at[i] = live[i] ? paged_row(p.c, page[i], h[i], n[i] & ((1 << p.c.page_shift) - 1)) : 0;
+        live[i] = live[i] && NNC_BC(at[i] >= 0 && at[i] < paged_rows(p.c) && h[i] < p.c.n_kv, 3301);
     }
     if constexpr (WRITE) {
 #pragma unroll

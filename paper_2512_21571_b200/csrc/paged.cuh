@@ -34,6 +34,9 @@ __device__ __forceinline__ long long paged_row(const PagedView &c, int page, int
     return (((long long)page * c.n_kv + head) << c.page_shift) + slot;
 }
 
+// rows of the pool
+__device__ __forceinline__ long long paged_rows(const PagedView &c) { return ((long long)c.n_pages * c.n_kv) << c.page_shift; }
+
 // 2^(byte - 127): a row's scale (byte 0 is 2^-127, a subnormal; 255 stands for no number)
 __device__ __forceinline__ float scale_from_byte(uint32_t byte) {
     return byte == 0u ? __uint_as_float(0x00400000u) : byte == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte << 23);

@@ -20,7 +20,7 @@ struct RopeParams {
     const int32_t *pos;
     const double *freq;
     long long x_row, x_head, y_row, y_head;   // elements
-    int n_tokens, n_heads, rot, tokens_per_cta, units;   // units: work items per head
+    int n_tokens, n_heads, head_dim, rot, tokens_per_cta, units;   // units: work items per head
     int abreast;                                         // vector form: tokens that a CTA's threads take at once
     float amplitude;
     bool inverse;
@@ -137,6 +137,7 @@ __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             if (first + m * p.abreast >= tokens) break;
+            if (!NNC_BC(h < p.n_heads && at_a >= 0 && at_a + N <= p.head_dim && at_b + N <= p.head_dim && t0 + first + m * p.abreast < p.n_tokens, 3401)) break;
             const char *x = p.x + (x_at + (long long)(m * p.abreast) * p.x_row) * el;
             a[m].load(x + at_a * el);
             if (u < rot_units) b[m].load(x + at_b * el);
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(512) rope_kernel(const RopeParams p) {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             const int t = first + m * p.abreast;
-            if (t >= tokens) break;
+            if (t >= tokens || !NNC_BC(t < p.tokens_per_cta && at_b + N <= p.head_dim, 3402)) break;
             char *y = p.y + (y_at + (long long)(m * p.abreast) * p.y_row) * el;
             if (u < rot_units) {
                 float fa[N], fb[N];
@@ -205,6 +206,7 @@ __global__ void __launch_bounds__(512) rope_plain_kernel(const RopeParams p) {
     __syncthreads();
     for (int i = threadIdx.x; i < tokens * per_token; i += blockDim.x) {
         const int t = i / per_token, r = i - t * per_token, h = r / p.units, u = r - h * p.units;
+        if (!NNC_BC(h < p.n_heads && (u < half || p.rot + u - half < p.head_dim) && t0 + t < p.n_tokens, 3403)) continue;
         const typename E::raw *x = reinterpret_cast<const typename E::raw *>(p.x) + (long long)(t0 + t) * p.x_row + h * p.x_head;
         typename E::raw *y = reinterpret_cast<typename E::raw *>(p.y) + (long long)(t0 + t) * p.y_row + h * p.y_head;
         if (u >= half) {
@@ -249,7 +251,7 @@ cudaError_t launch_rope(const LaunchCtx &lc, const void *x, void *y, int type, i
     RopeParams p;
     p.x = (const char *)x; p.y = (char *)y; p.pos = positions; p.freq = freq;
     p.x_row = x_row; p.x_head = x_head; p.y_row = y_row; p.y_head = y_head;
-    p.n_tokens = n_tokens; p.n_heads = n_heads; p.rot = rotary_dim;
+    p.n_tokens = n_tokens; p.n_heads = n_heads; p.head_dim = head_dim; p.rot = rotary_dim;
     p.amplitude = amplitude; p.inverse = inverse;
     const bool copy_rest = x != y && rotary_dim < head_dim;
     // the largest piece of n elements that pairs, what passes through, pointers and strides are all whole multiples of (16-byte
