@@ -324,7 +324,7 @@ int nnc_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, doub
  * head_dim <= 1024), in pairs (i, i + rotary_dim / 2), or (2i, 2i + 1) with interleaved != 0; the others are copied.
  *   y_a = amplitude * (x_a cos - x_b sin),  y_b = amplitude * (x_b cos + x_a sin),  angle = position * freq[i]
  * inverse != 0 turns the other way: given the gradient with respect to y it is the gradient with respect to x.  The
- * angle is reduced in 64 bits, the arithmetic is fp32, one rounding to `type` at the end.  y may be x itself (with the
+ * angle is reduced in two doubles (2^-28 turns at any position), the arithmetic is fp32, one rounding to `type` at the end.  y may be x itself (with the
  * same strides); other overlaps of x and y, and rows of y that overlap each other, are not allowed.  n_tokens or n_heads of 0 is a call that
  * does nothing. */
 int nnc_op_rope(const void *x, void *y, int32_t type, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
