@@ -11,18 +11,18 @@
 //   - A warp owns 4 KB of key rows and as much of value rows of every tile and runs its own ring of shared-memory stages, filled by
 //     16-byte asynchronous copies that run ahead across heads and sequences; no barrier in the steady state.  Rows outside the
 //     attended range are filled with zeros instead of being read, so nothing stored there can reach a product.
-//   - Two or three CTAs per SM: three (168 registers, rings of two stages) where the products' operands fit without spilling.  61
-//     E4M3 sequences of up to 9000 positions: 112 us with two, 101.5 us with three; two operands of 128-element heads spill
-//     there and are slower (58.5 -> 64.7 us for 32 x 8192, 2 heads, 16 queries each).
+//   - Two or three CTAs per SM: three (168 registers, rings of two stages, up to 20 bytes spilled) where that is faster.  32 x 8192, codes,
+//     4 query heads of 128 elements per KV head: 114.6 us with two, 99.1 with three; 16 heads of 64: bf16 128.7 and 115.4, but codes
+//     98.0 and 100.7 (48 bytes spilled); two operands of 128 elements need 255 registers as it is.
 //   - Both products run on the warp-level tensor-core path in transposed form: S^T = K Q^T and O^T = V^T P^T, so 16
 //     positions (16 head-dimension elements) fill the 16-row operand and 8 query heads are the 8-column operand: the tensor pipe is
-//     busy 13 % of the time at 95 % of the measured copy bandwidth.  A tcgen05 tile would have 128 rows for the same 8 columns,
+//     busy 17 % of the time at 94 % of the measured copy bandwidth.  A tcgen05 tile would have 128 rows for the same 8 columns,
 //     for more of a pipe that does not limit.
 //   - E4M3 codes are fp16 values exactly; key scales multiply the scores, value scales (powers of two) are added to the
 //     exponents of the probabilities that weigh the codes, so no code is ever multiplied by a scale.  Those weights have a running
 //     maximum of their own, over the rows that are not all zeros: the softmax's sum is taken of the probabilities themselves, whose reach
-//     has nothing to do with the values'.  (Looking for rows of zeros: 32 x 8192 with bf16 results 92.9 -> 95.5 us.)  (The warp-level product of
-//     8-bit operands is built from fp16 ones on this machine, at more instructions than these conversions: measured, 147 -> 179 us.)
+//     has nothing to do with the values'.  (Looking for rows of zeros: 32 x 8192 with heads of 128 97.3 -> 99.1 us, of 64 63.0 -> 67.4.  The
+//     warp-level product of 8-bit operands took longer than these conversions and fp16 products: 147 -> 179 us on a ragged batch.)
 // Numerics: scores, maxima, sums and outputs are fp32.  Queries enter exactly (16-bit types) or as three bf16 or two fp16 terms, and
 // probabilities as three bf16 or two fp16 terms whatever the results' type: 24 and 22 bits, so that the only rounding a caller
 // sees is the result's.  (One term less for 16-bit results moved them by up to 2^-18, bf16 results of codes by 2^-12, and took, 32 x 8192 with 4 and 16
@@ -57,7 +57,7 @@ struct PagedAttnParams {
 
 template <int D, int NT, int KV, int TYPE>
 struct Shape {
-    static constexpr int kCtas = (NT == 1 && (TYPE != NNC_F32 || KV != NNC_BF16)) || (NT == 2 && D == 64 && TYPE != NNC_F32) ? 3 : 2;   // resident per SM
+    static constexpr int kCtas = (NT == 1 && (TYPE != NNC_F32 || KV != NNC_BF16)) || (NT == 2 && D == 64 && TYPE != NNC_F32 && KV != NNC_E4M3) ? 3 : 2;   // resident per SM
     static constexpr int kBytes = KV == NNC_E4M3 ? 1 : 2;
     static constexpr int kRow = D * kBytes;                  // bytes of a row
     static constexpr int kPB = 4096 / kRow;                  // positions of a warp's block: 4 KB of keys, as many of values
@@ -492,20 +492,29 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
         }
         const uint32_t here = present >> (stage * S::kSub) & ((1u << S::kSub) - 1u);
         const bool full = p0 >= now.r.start && p0 + PB <= now.r.end && here == (1u << S::kSub) - 1u;
+        // A row of zeros has no exponent: whatever its scale says, it must not set the maximum for the others.  Two pieces a row tell an
+        // ordinary row (are there any bits but signs?); only where some have none there the others are looked at.
+        uint32_t filled[S::kSub];   // a bit a row
+        if constexpr (CODES) {
+            const char *rows = scales - S::kData + PB * ROW;
+            auto any_in = [&](int u, int piece) {   // of pieces `piece` and `piece` + 1
+                const uint4 x = *reinterpret_cast<const uint4 *>(rows + swizzled<ROW>(16 * u + (lane & 15), piece + (lane >> 4)));
+                const uint32_t votes = __ballot_sync(0xffffffffu, ((x.x | x.y | x.z | x.w) & 0x7f7f7f7fu) != 0u);
+                return (votes | votes >> 16) & 0xffffu;
+            };
+            uint32_t all_rows = 0xffffu;
+#pragma unroll
+            for (int u = 0; u < S::kSub; ++u) all_rows &= filled[u] = any_in(u, 0);
+            if (all_rows != 0xffffu) {
+#pragma unroll 1
+                for (int piece = 2; piece < kPieces; piece += 2)
+#pragma unroll
+                    for (int u = 0; u < S::kSub; ++u) filled[u] |= any_in(u, piece);
+            }
+        }
         float ev[S::kSub][2];   // exponents of the value rows
 #pragma unroll
         for (int u = 0; u < S::kSub; ++u) {
-            // a row of zeros has no exponent: whatever its scale says, it must not set the maximum for the others (a vote on each
-            // 16-byte piece: are there any bits but signs?)
-            uint32_t filled[kSteps];
-            if constexpr (CODES) {
-                const char *rows = scales - S::kData + PB * ROW;
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(rows + swizzled<ROW>(16 * u + r0 + i * kRowsPerStep, c0));
-                    filled[i] = __ballot_sync(0xffffffffu, ((x.x | x.y | x.z | x.w) & 0x7f7f7f7fu) != 0u);
-                }
-            }
 #pragma unroll
             for (int r = 0; r < 2; ++r) {   // rows g8 and g8 + 8
                 float ks = 1.f;
@@ -513,9 +522,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
                     const uint32_t bk = (uint8_t)scales[16 * u + g8 + 8 * r], bv = (uint8_t)scales[PB + 16 * u + g8 + 8 * r];
                     ks = __uint_as_float(bk << 23);
                     ev[u][r] = __uint_as_float(0x4b000000u | bv) - 8388735.f;   // bv - 127: 2^23 + bv as fp32, no conversion
-                    constexpr int kPer8 = 8 / kRowsPerStep;   // steps for 8 rows: 2 or 1
-                    const uint32_t votes = kPer8 > 1 && g8 >= kRowsPerStep ? filled[r * kPer8 + kPer8 - 1] : filled[r * kPer8];
-                    if (!(votes & ((1u << kPieces) - 1u) << (g8 % kRowsPerStep * kPieces))) ev[u][r] = -INFINITY;
+                    if (!(filled[u] >> (g8 + 8 * r) & 1u)) ev[u][r] = -INFINITY;
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -552,9 +559,11 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                if constexpr (CODES) {
-                    const float m_new = fmaxf(m_run[nt][e], top_of(nt, e)), ref = m_new == -INFINITY ? 0.f : m_new;
-                    float sum = 0.f;
+                if constexpr (CODES) {   // a lane's positions have a maximum of their own, until the piece ends
+                    float m_new = m_run[nt][e], sum = 0.f;
+#pragma unroll
+                    for (int u = 0; u < S::kSub; ++u) m_new = fmaxf(m_new, fmaxf(s[u][nt][e], s[u][nt][2 + e]));
+                    const float ref = m_new == -INFINITY ? 0.f : m_new;
 #pragma unroll
                     for (int u = 0; u < S::kSub; ++u)
 #pragma unroll
@@ -690,14 +699,19 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float l = l_run[nt][e];
+                float l = l_run[nt][e], m = m_run[nt][e];
+                if constexpr (CODES) {
+#pragma unroll
+                    for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                    l *= m_run[nt][e] == -INFINITY ? 1.f : exp2f(m_run[nt][e] - m);   // (no positions: l is 0)
+                }
                 l += __shfl_xor_sync(0xffffffffu, l, 4);
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 if (g8 == 0) {
                     float *const ml = sh.ml[warp][2 * t4 + e];
-                    ml[0] = (CODES ? mv_run[nt][e] : m_run[nt][e]) - kLift;
-                    ml[1] = CODES ? m_run[nt][e] : ml[0];
+                    ml[0] = (CODES ? mv_run[nt][e] : m) - kLift;
+                    ml[1] = CODES ? m : ml[0];
                     ml[2] = l;
                 }
             }
