@@ -1008,9 +1008,9 @@ cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_page
     p.group = n_q_heads / cache.n_kv_heads;
     p.scale_log2 = scale * 1.4426950408889634f;
     // Query heads in groups of 8.  Two groups as two operands of one CTA share every key and value fragment: 32 x 8192 E4M3 of 64
-    // elements, 16 heads: 45.5 us against 55.6 with a CTA each.  Not with an odd number of groups, where half of the last pair would be
-    // empty (64 x 8192, 17 heads: 89.7 us in pairs, 76 apart), and not where few (sequence, head)s share the whole GPU, whose
-    // joins are half as large apart (one of 131072, 16 heads: 32.7 and 25.7 us).
+    // elements, 8 KV heads of 16 query heads: 98 us against 120 with a CTA each.  Not with an odd number of groups, where half of the last
+    // pair would be empty (64 x 8192 bf16, 17 heads: 99.9 us in pairs, 90.0 apart), and not where few (sequence, head)s share the whole
+    // GPU, whose joins are half as large apart (one of 131072, 16 heads: 31.8 and 26.9 us).
     const int eights = (p.group + 7) / 8;
     const bool two = eights % 2 == 0 && (long long)batch * cache.n_kv_heads >= 16;
     p.chunks = two ? eights / 2 : eights;
