@@ -390,6 +390,42 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
                              int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
                              void *scratch, size_t scratch_bytes, void *cuda_stream);
 
+/* ---- long caches: pages chosen by a score --------------------------------------------------------------------
+ * A decoding step that reads part of a long cache: for every page the lowest and the highest of its keys, element by element
+ * (nnc_op_page_bounds, after rows were written), the most that a query's product with a key between them can be (nnc_op_score_pages), the
+ * pages of the highest scores (nnc_op_select_pages), and the attention over them (nnc_op_attn_selected_paged). */
+
+/* bounds: 16-byte aligned, [n_pages][n_kv_heads][2][head_dim] of the cache's type (NNC_BF16 for an NNC_E4M3 cache, which holds its scaled codes
+ * exactly): lowest, then highest.  Sets them for every page of sequences 0 .. batch - 1 (batch <= n_seqs) that holds a position in
+ * [first[b], lens[b]), from all positions of that page below lens[b]; other pages' bounds stay.  lens, first: int32 [batch]; first NULL: 0.
+ * NaN where a key is NaN.  Sequences that share such a page give it the same bounds if both have all of it, which shared pages want
+ * anyway.  A length beyond the table's reach counts as the longest the table holds, a page out of range is left out; both set the
+ * status word. */
+int nnc_op_page_bounds(const nnc_paged_kv *cache, void *bounds, const int32_t *lens, const int32_t *first, int32_t batch, void *cuda_stream);
+
+/* scores: fp32 [batch][n_kv_heads][pages_per_seq]: for page n of sequence b the largest, over the query heads of the KV head, of
+ * sum_i max(q_i lowest_i, q_i highest_i): no key of the page has a larger product with any of these queries.  -infinity for pages that hold no
+ * position below lens[b] and for pages out of range.  A page whose bounds are not all finite scores an infinity or NaN.  q as
+ * for nnc_op_attn_decode_paged.  Types other than the bounds' enter as sums of their terms (24 bits, or 22 in fp16); sums
+ * are fp32.  n_q_heads / n_kv_heads at most 128. */
+int nnc_op_score_pages(const void *q, const nnc_paged_kv *cache, const void *bounds, const int32_t *lens, float *scores, int32_t type,
+                       int32_t batch, int32_t n_q_heads, int64_t q_stride, void *cuda_stream);
+
+/* Of the P pages that hold positions below lens[b] (at most n_columns) the n of the highest scores, for each KV head: scores fp32
+ * [batch][n_kv_heads][n_columns].  The first `first` and the last `last` pages (first + last <= n) are always among them; NaN is above every
+ * number; among equal scores the lowest pages.  pages: int32 [batch][n_kv_heads][n], in ascending order, -1 behind the last; counts: int32
+ * [batch][n_kv_heads], min(n, P).  page_size as in the cache. */
+int nnc_op_select_pages(const float *scores, const int32_t *lens, int32_t *pages, int32_t *counts, int32_t batch, int32_t n_kv_heads,
+                        int32_t n_columns, int32_t page_size, int32_t n, int32_t first, int32_t last, void *cuda_stream);
+
+/* nnc_op_attn_decode_paged over listed pages: the query heads of KV head h of sequence b attend to the positions below lens[b] of the pages
+ * pages[b][h][0 .. counts[b][h] - 1] (numbers within the sequence, in any order, none twice; int32 [batch][n_kv_heads][list_len], counts
+ * above list_len count as list_len).  A page without such a position adds nothing; one outside [0, pages_per_seq) adds nothing and
+ * sets the status word.  Everything else, the scratch among it, is as there. */
+int nnc_op_attn_selected_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, const int32_t *pages, const int32_t *counts,
+                               int32_t list_len, void *out, float *lse, int32_t type, int32_t batch, int32_t n_q_heads, int64_t q_stride,
+                               int64_t out_stride, float scale, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -106,6 +106,14 @@ EXPORTS = {
     "nnc_op_attn_decode_paged": (C.c_int, [C.c_void_p, C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
                                            C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_float, C.c_int32, C.c_void_p,
                                            C.c_size_t, C.c_void_p]),
+    "nnc_op_page_bounds": (C.c_int, [C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "nnc_op_score_pages": (C.c_int, [C.c_void_p, C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                     C.c_int32, C.c_int64, C.c_void_p]),
+    "nnc_op_select_pages": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                      C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
+    "nnc_op_attn_selected_paged": (C.c_int, [C.c_void_p, C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                             C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_float,
+                                             C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 for _name, (_res, _args) in EXPORTS.items():
     _fn = getattr(lib, _name)
@@ -442,7 +450,8 @@ except ImportError as e:
     _calls = _Missing(e)
 else:
     _calls.bind(*(C.cast(getattr(lib, n), C.c_void_p).value for n in
-                  ("nnc_op_rope", "nnc_op_kv_write_paged", "nnc_op_kv_read_paged", "nnc_op_attn_decode_paged")), NncError)
+                  ("nnc_op_rope", "nnc_op_kv_write_paged", "nnc_op_kv_read_paged", "nnc_op_attn_decode_paged", "nnc_op_page_bounds",
+                   "nnc_op_score_pages", "nnc_op_select_pages", "nnc_op_attn_selected_paged")), NncError)
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp_turns": 3, "ramp_index": 4}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
@@ -566,3 +575,37 @@ def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, sc
     sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  out: None, q itself, or a tensor of q's
     shape and type that q does not overlap.  Returns out, or (out, lse)."""
     return _calls.attn(cache.address, cache.index, q, lens, scale, window, scratch, out, want_lse)
+
+
+# ---- long caches: pages chosen by a score ------------------------------------------------------------------------
+
+def page_bounds(cache: PagedKV) -> torch.Tensor:
+    """Bounds for op_page_bounds and op_score_pages, to be made once beside the cache: zeros."""
+    return torch.zeros(cache.n_pages, cache.n_kv_heads, 2, cache.head_dim, device=cache.device,
+                       dtype=torch.float16 if cache.dtype is torch.float16 else torch.bfloat16)
+
+
+def op_page_bounds(cache: PagedKV, bounds: torch.Tensor, lens: torch.Tensor, first: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nnc_op_page_bounds: sets `bounds` (page_bounds) of every page that holds a position in [first[b], lens[b]) of sequence b, and
+    returns it.  To be called after rows were written, with the positions of the first of them (None: all)."""
+    return _calls.page_bounds(cache.address, cache.index, bounds, lens, first)
+
+
+def op_score_pages(q: torch.Tensor, cache: PagedKV, bounds: torch.Tensor, lens: torch.Tensor) -> torch.Tensor:
+    """nnc_op_score_pages: float32 [batch][n_kv_heads][pages_per_seq], the most that a product of a KV head's queries with a key
+    between a page's bounds can be."""
+    return _calls.score_pages(cache.address, cache.index, q, bounds, lens)
+
+
+def op_select_pages(scores: torch.Tensor, lens: torch.Tensor, page_size: int, n: int, first: int = 1, last: int = 1):
+    """nnc_op_select_pages: (pages int32 [batch][n_kv_heads][n], counts int32 [batch][n_kv_heads]): the n pages of the highest scores in
+    ascending order, the first `first` and the last `last` of a sequence always among them."""
+    return _calls.select_pages(scores, lens, page_size, n, first, last)
+
+
+def op_attn_selected_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, pages: torch.Tensor, counts: torch.Tensor,
+                           scale: Optional[float] = None, scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                           want_lse: bool = False):
+    """nnc_op_attn_selected_paged: op_attn_decode_paged over the first counts[b][h] of pages[b][h] for the queries of KV head h.  Scratch and
+    out as there."""
+    return _calls.attn_selected(cache.address, cache.index, q, lens, pages, counts, scale, scratch, out, want_lse)

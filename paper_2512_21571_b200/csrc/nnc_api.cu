@@ -1039,24 +1039,88 @@ int nnc_op_kv_read_paged(const nnc_paged_kv *cache, void *k, void *v, int32_t ty
     return kv_rows_paged(cache, false, k, v, type, n_tokens, row_stride, head_stride, pos, seq, cuda_stream);
 }
 
-int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, void *out, float *lse, int32_t type,
-                             int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
-                             void *scratch, size_t scratch_bytes, void *cuda_stream) {
-    if (!paged_ok(cache) || batch < 0 || batch > cache->n_seqs || window < 0) return NNC_ERR_INVALID_ARG;
+// what the attentions over a paged cache and the scores of its pages ask of their queries
+static int paged_queries_ok(const nnc_paged_kv *cache, int32_t type, int32_t batch, int32_t n_q_heads) {
+    if (!paged_ok(cache) || batch < 0 || batch > cache->n_seqs) return NNC_ERR_INVALID_ARG;
     if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads) return NNC_ERR_INVALID_ARG;
     if (n_q_heads / cache->n_kv_heads > 65535 * 8) return NNC_ERR_CAPACITY;   // rows of the grid
     if (type != NNC_F32 && type != NNC_BF16 && type != NNC_F16) return NNC_ERR_INVALID_ARG;
     if (cache->type != NNC_E4M3 && type != NNC_F32 && type != cache->type) return NNC_ERR_INVALID_ARG;
+    return NNC_OK;
+}
+
+static bool paged_rows_aligned(const void *p, int32_t type, int64_t stride) {
+    return p && !((uintptr_t)p & 15) && stride * (type == NNC_F32 ? 4 : 2) % 16 == 0;
+}
+
+int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, void *out, float *lse, int32_t type,
+                             int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
+                             void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    if (window < 0) return NNC_ERR_INVALID_ARG;
+    if (int rc = paged_queries_ok(cache, type, batch, n_q_heads); rc != NNC_OK) return rc;
     if (batch == 0) return NNC_OK;
-    if (!q || !lens || !out || !scratch) return NNC_ERR_INVALID_ARG;
-    const int64_t el = type == NNC_F32 ? 4 : 2;
-    if ((((uintptr_t)q | (uintptr_t)out) & 15) || (q_stride * el) % 16 || (out_stride * el) % 16) return NNC_ERR_INVALID_ARG;
+    if (!lens || !scratch || !paged_rows_aligned(q, type, q_stride) || !paged_rows_aligned(out, type, out_stride)) return NNC_ERR_INVALID_ARG;
     if (((uintptr_t)lens | (uintptr_t)lse) & 3) return NNC_ERR_INVALID_ARG;
     if (((uintptr_t)scratch & 255) || scratch_bytes < NNC_ATTN_PAGED_SCRATCH_BYTES) return NNC_ERR_WORKSPACE;
     LaunchCtx lc;
     if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
     cudaError_t e = launch_attn_paged(lc, q, *cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, window, scratch,
                                       scratch_bytes);
+    if (e == cudaErrorInvalidValue) return NNC_ERR_CAPACITY;
+    return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+int nnc_op_page_bounds(const nnc_paged_kv *cache, void *bounds, const int32_t *lens, const int32_t *first, int32_t batch, void *cuda_stream) {
+    if (!paged_ok(cache) || batch < 0 || batch > cache->n_seqs) return NNC_ERR_INVALID_ARG;
+    if (batch == 0) return NNC_OK;
+    if (!bounds || ((uintptr_t)bounds & 15) || !lens || (((uintptr_t)lens | (uintptr_t)first) & 3)) return NNC_ERR_INVALID_ARG;
+    if (batch > 65535) return NNC_ERR_CAPACITY;   // rows of the grid
+    LaunchCtx lc;
+    if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    return launch_page_bounds(lc, *cache, bounds, lens, first, batch) == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+int nnc_op_score_pages(const void *q, const nnc_paged_kv *cache, const void *bounds, const int32_t *lens, float *scores, int32_t type,
+                       int32_t batch, int32_t n_q_heads, int64_t q_stride, void *cuda_stream) {
+    if (int rc = paged_queries_ok(cache, type, batch, n_q_heads); rc != NNC_OK) return rc;
+    if (n_q_heads / cache->n_kv_heads > kMaxScoredGroup) return NNC_ERR_CAPACITY;
+    if (batch == 0) return NNC_OK;
+    if (!bounds || ((uintptr_t)bounds & 15) || !lens || !scores || !paged_rows_aligned(q, type, q_stride)) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)lens | (uintptr_t)scores) & 3) return NNC_ERR_INVALID_ARG;
+    LaunchCtx lc;
+    if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    cudaError_t e = launch_score_pages(lc, q, *cache, bounds, lens, scores, type, batch, n_q_heads, q_stride);
+    if (e == cudaErrorInvalidValue) return NNC_ERR_CAPACITY;
+    return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+int nnc_op_select_pages(const float *scores, const int32_t *lens, int32_t *pages, int32_t *counts, int32_t batch, int32_t n_kv_heads,
+                        int32_t n_columns, int32_t page_size, int32_t n, int32_t first, int32_t last, void *cuda_stream) {
+    if (batch < 0 || n_kv_heads <= 0 || n_columns <= 0 || n <= 0 || first < 0 || last < 0 || (int64_t)first + last > n) return NNC_ERR_INVALID_ARG;
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return NNC_ERR_INVALID_ARG;
+    if (batch == 0) return NNC_OK;
+    if (!scores || !lens || !pages || !counts) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)scores | (uintptr_t)lens | (uintptr_t)pages | (uintptr_t)counts) & 3) return NNC_ERR_INVALID_ARG;
+    if ((int64_t)batch * n_kv_heads > 0x7fffffff || n_columns > 0x7fffffff - 1024 || n > 0x7fffffff - 1024) return NNC_ERR_CAPACITY;
+    LaunchCtx lc;
+    if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    return launch_select_pages(lc, scores, lens, pages, counts, batch, n_kv_heads, n_columns, page_size, n, first, last) == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
+int nnc_op_attn_selected_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, const int32_t *pages, const int32_t *counts,
+                               int32_t list_len, void *out, float *lse, int32_t type, int32_t batch, int32_t n_q_heads, int64_t q_stride,
+                               int64_t out_stride, float scale, void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    if (int rc = paged_queries_ok(cache, type, batch, n_q_heads); rc != NNC_OK) return rc;
+    if (list_len <= 0) return NNC_ERR_INVALID_ARG;
+    if ((int64_t)list_len * cache->page_size > 0x7fffffff - 1024) return NNC_ERR_CAPACITY;   // positions in a list are 32-bit numbers
+    if (batch == 0) return NNC_OK;
+    if (!lens || !pages || !counts || !scratch || !paged_rows_aligned(q, type, q_stride) || !paged_rows_aligned(out, type, out_stride)) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)lens | (uintptr_t)pages | (uintptr_t)counts | (uintptr_t)lse) & 3) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)scratch & 255) || scratch_bytes < NNC_ATTN_PAGED_SCRATCH_BYTES) return NNC_ERR_WORKSPACE;
+    LaunchCtx lc;
+    if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    cudaError_t e = launch_attn_selected(lc, q, *cache, lens, pages, counts, list_len, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale,
+                                         scratch, scratch_bytes);
     if (e == cudaErrorInvalidValue) return NNC_ERR_CAPACITY;
     return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
 }

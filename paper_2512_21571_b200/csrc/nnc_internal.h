@@ -139,6 +139,16 @@ constexpr int kPagedMaxCtas = NNC_ATTN_PAGED_TICKET_BYTES / 12;   // three ticke
 cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, void *out, float *lse,
                               int type, int batch, int n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int window,
                               void *scratch, size_t scratch_bytes);
+cudaError_t launch_attn_selected(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const int32_t *pages,
+                                 const int32_t *counts, int list_len, void *out, float *lse, int type, int batch, int n_q_heads,
+                                 int64_t q_stride, int64_t out_stride, float scale, void *scratch, size_t scratch_bytes);
+// pages.cu
+constexpr int kMaxScoredGroup = 128;   // query heads per KV head: their terms are held in shared memory
+cudaError_t launch_page_bounds(const LaunchCtx &lc, const nnc_paged_kv &cache, void *bounds, const int32_t *lens, const int32_t *first, int batch);
+cudaError_t launch_score_pages(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const void *bounds, const int32_t *lens, float *scores,
+                               int type, int batch, int n_q_heads, int64_t q_stride);
+cudaError_t launch_select_pages(const LaunchCtx &lc, const float *scores, const int32_t *lens, int32_t *pages, int32_t *counts, int batch, int n_kv,
+                                int columns, int page_size, int n, int first, int last);
 
 // ---- GEMM (gemm_tc.cu) --------------------------------------------------------------------------------
 enum GemmEpi { kEpiStoreF32 = 0, kEpiStoreBf16 = 1, kEpiAccumF32 = 2, kEpiSwigluBf16 = 3 };

@@ -26,6 +26,10 @@ decltype(&nnc_op_rope) call_rope;
 decltype(&nnc_op_kv_write_paged) call_write;
 decltype(&nnc_op_kv_read_paged) call_read;
 decltype(&nnc_op_attn_decode_paged) call_attn;
+decltype(&nnc_op_page_bounds) call_bounds;
+decltype(&nnc_op_score_pages) call_score;
+decltype(&nnc_op_select_pages) call_select;
+decltype(&nnc_op_attn_selected_paged) call_selected;
 PyObject *error_class;   // NncError(status, detail)
 
 struct Refused {};   // a Python error is set
@@ -313,48 +317,159 @@ PyObject *kv_read(PyObject *const *a) {
     return pair(k, v);
 }
 
+// contiguous int32 numbers, one for every element of `shape`
+const int32_t *indices_of(const at::Tensor &t, at::IntArrayRef shape, int device, const char *what) {
+    if (t.scalar_type() != at::kInt || t.sizes() != shape || !t.is_contiguous() || !t.is_cuda() || t.get_device() != device) {
+        PyErr_Format(PyExc_ValueError, "%s on the call's CUDA device", what);
+        throw Refused();
+    }
+    return static_cast<const int32_t *>(t.data_ptr());
+}
+
+int32_t whole(PyObject *o, long long least, const char *refusal) {
+    const long long n = PyLong_AsLongLong(o);
+    if (n == -1 && PyErr_Occurred()) throw Refused();
+    if (n < least || n > INT32_MAX) refuse(refusal);
+    return static_cast<int32_t>(n);
+}
+
+// What the attentions of one token per sequence have in common: queries, scale, results, scratch.
+struct Attention {
+    const nnc_paged_kv &c;
+    int device;
+    const at::Tensor &q;
+    Rows in, to;
+    at::Tensor out, lse, scratch;
+    PyObject *given;   // out, or None
+    bool want_lse;
+    float scale;
+
+    Attention(PyObject *cache, PyObject *index, PyObject *queries, PyObject *scale_or_none, PyObject *out_or_none, PyObject *want)
+        : c(cache_of(cache)), device((int)PyLong_AsLong(index)), q(tensor(queries, "q")), in(rows_of(q, device, "q")), to(in), given(out_or_none) {
+        if (in.d != c.head_dim || in.head != in.d) refuse("q: [batch][n_q_heads][head_dim] of the cache's head_dim, heads next to each other");
+        scale = scale_or_none == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(in.d))) : number(scale_or_none);
+        to.row = in.heads * in.d;
+        if (given == Py_None) {
+            out = at::empty({in.tokens, in.heads, in.d}, q.options());
+        } else {
+            out = tensor(given, "out");
+            to = rows_of(out, device, "out");
+            writable(out);
+            if (!to.like(in) || to.head != in.d || !disjoint(out)) refuse("out: q's shape and type, heads next to each other, no rows that overlap");
+            apart_or_same(region_of(out, to), region_of(q, in), "out: q itself, or memory that q has no part of");
+            for (const void *pool : {c.k, c.v})
+                if (meet(region_of(out, to), pool_of(c, pool))) refuse("out: memory that the cache has no part of");
+        }
+        want_lse = truth(want);
+        if (want_lse) lse = at::empty({in.tokens, in.heads}, q.options().dtype(at::kFloat));
+    }
+
+    // scratch of the caller's, or of the call's own, whose first `zeros` bytes have to be zero
+    void take_scratch(PyObject *o, int64_t bytes, int64_t zeros, const char *refusal) {
+        if (o == Py_None) {
+            scratch = at::empty({bytes}, q.options().dtype(at::kByte));
+            scratch.narrow(0, 0, zeros).zero_();
+        } else {
+            scratch = tensor(o, "scratch");
+            if (!scratch.is_cuda() || scratch.get_device() != device || !scratch.is_contiguous()) refuse(refusal);
+        }
+    }
+    float *lse_at() const { return want_lse ? static_cast<float *>(lse.data_ptr()) : nullptr; }
+    PyObject *result() const {
+        if (given != Py_None) written(out);
+        return want_lse ? pair(out, lse) : THPVariable_Wrap(out);
+    }
+};
+constexpr const char *kPagedScratch = "scratch: a contiguous tensor on the call's CUDA device (attn_paged_scratch)";
+
 // attn(cache, device, q, lens, scale or None, window, scratch or None, out or None, want_lse)
 PyObject *attn(PyObject *const *a) {
+    Attention x(a[0], a[1], a[2], a[4], a[7], a[8]);
+    const int32_t *at_lens = index_of(tensor(a[3], "lens"), x.in.tokens, x.device, "lens");
+    const int32_t window = whole(a[5], 0, "window: 0 or a number of positions");
+    x.take_scratch(a[6], NNC_ATTN_PAGED_SCRATCH_BYTES, NNC_ATTN_PAGED_TICKET_BYTES, kPagedScratch);
+    launch(x.device, "nnc_op_attn_decode_paged", [&](void *stream) {
+        return call_attn(x.q.data_ptr(), &x.c, at_lens, x.out.data_ptr(), x.lse_at(), x.in.type, (int32_t)x.in.tokens, (int32_t)x.in.heads, x.in.row, x.to.row,
+                         x.scale, window, x.scratch.data_ptr(), x.scratch.nbytes(), stream);
+    });
+    return x.result();
+}
+
+// attn_selected(cache, device, q, lens, pages, counts, scale or None, scratch or None, out or None, want_lse)
+PyObject *attn_selected(PyObject *const *a) {
+    Attention x(a[0], a[1], a[2], a[6], a[8], a[9]);
+    const int32_t *at_lens = index_of(tensor(a[3], "lens"), x.in.tokens, x.device, "lens");
+    const at::Tensor &pages = tensor(a[4], "pages"), &counts = tensor(a[5], "counts");
+    const int64_t list_len = pages.dim() == 3 ? pages.size(2) : 0;
+    if (list_len < 1 || list_len > INT32_MAX) refuse("pages: contiguous int32 [batch][n_kv_heads][entries]");
+    const int32_t *at_pages = indices_of(pages, {x.in.tokens, x.c.n_kv_heads, list_len}, x.device, "pages: contiguous int32 [batch][n_kv_heads][entries]");
+    const int32_t *at_counts = indices_of(counts, {x.in.tokens, x.c.n_kv_heads}, x.device, "counts: contiguous int32 [batch][n_kv_heads]");
+    x.take_scratch(a[7], NNC_ATTN_PAGED_SCRATCH_BYTES, NNC_ATTN_PAGED_TICKET_BYTES, kPagedScratch);
+    launch(x.device, "nnc_op_attn_selected_paged", [&](void *stream) {
+        return call_selected(x.q.data_ptr(), &x.c, at_lens, at_pages, at_counts, (int32_t)list_len, x.out.data_ptr(), x.lse_at(), x.in.type, (int32_t)x.in.tokens,
+                             (int32_t)x.in.heads, x.in.row, x.to.row, x.scale, x.scratch.data_ptr(), x.scratch.nbytes(), stream);
+    });
+    return x.result();
+}
+
+// a cache's bounds: [n_pages][n_kv_heads][2][head_dim]
+const at::Tensor &bounds_of(PyObject *o, const nnc_paged_kv &c, int device) {
+    const at::Tensor &t = tensor(o, "bounds");
+    const at::ScalarType type = c.type == NNC_F16 ? at::kHalf : at::kBFloat16;
+    if (t.scalar_type() != type || t.sizes() != at::IntArrayRef({c.n_pages, c.n_kv_heads, 2, c.head_dim}) || !t.is_contiguous() || !t.is_cuda() || t.get_device() != device)
+        refuse("bounds: contiguous [n_pages][n_kv_heads][2][head_dim] of the cache's type (bfloat16 for float8_e4m3fn) on the cache's device (page_bounds)");
+    return t;
+}
+
+// page_bounds(cache, device, bounds, lens, first or None)
+PyObject *page_bounds(PyObject *const *a) {
     const nnc_paged_kv &c = cache_of(a[0]);
     const int device = (int)PyLong_AsLong(a[1]);
-    const at::Tensor &q = tensor(a[2], "q"), &lens = tensor(a[3], "lens");
+    const at::Tensor &bounds = bounds_of(a[2], c, device), &lens = tensor(a[3], "lens");
+    writable(bounds);
+    const int64_t batch = lens.dim() == 1 ? lens.size(0) : 0;
+    if (batch > INT32_MAX) refuse("sizes: 32-bit numbers");
+    const int32_t *at_lens = index_of(lens, batch, device, "lens"), *at_first = a[4] == Py_None ? nullptr : index_of(tensor(a[4], "first"), batch, device, "first");
+    const Region whole_bounds = {reinterpret_cast<int64_t>(bounds.data_ptr()), (int64_t)bounds.nbytes(), {{0, 1}, {0, 1}}};
+    for (const void *pool : {c.k, c.v})
+        if (meet(whole_bounds, pool_of(c, pool))) refuse("bounds: memory that the cache has no part of");
+    launch(device, "nnc_op_page_bounds", [&](void *stream) { return call_bounds(&c, bounds.data_ptr(), at_lens, at_first, (int32_t)batch, stream); });
+    written(bounds);
+    Py_INCREF(a[2]);
+    return a[2];
+}
+
+// score_pages(cache, device, q, bounds, lens)
+PyObject *score_pages(PyObject *const *a) {
+    const nnc_paged_kv &c = cache_of(a[0]);
+    const int device = (int)PyLong_AsLong(a[1]);
+    const at::Tensor &q = tensor(a[2], "q"), &bounds = bounds_of(a[3], c, device);
     const Rows in = rows_of(q, device, "q");
     if (in.d != c.head_dim || in.head != in.d) refuse("q: [batch][n_q_heads][head_dim] of the cache's head_dim, heads next to each other");
-    const int32_t *at_lens = index_of(lens, in.tokens, device, "lens");
-    const float scale = a[4] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(in.d))) : number(a[4]);
-    const long long window = PyLong_AsLongLong(a[5]);
-    if (window == -1 && PyErr_Occurred()) throw Refused();
-    if (window < 0 || window > INT32_MAX) refuse("window: 0 or a number of positions");
-    at::Tensor out, lse, scratch;
-    Rows to = in;
-    to.row = in.heads * in.d;
-    if (a[7] == Py_None) {
-        out = at::empty({in.tokens, in.heads, in.d}, q.options());
-    } else {
-        out = tensor(a[7], "out");
-        to = rows_of(out, device, "out");
-        writable(out);
-        if (!to.like(in) || to.head != in.d || !disjoint(out)) refuse("out: q's shape and type, heads next to each other, no rows that overlap");
-        apart_or_same(region_of(out, to), region_of(q, in), "out: q itself, or memory that q has no part of");
-        for (const void *pool : {c.k, c.v})
-            if (meet(region_of(out, to), pool_of(c, pool))) refuse("out: memory that the cache has no part of");
-    }
-    const bool want_lse = truth(a[8]);
-    if (want_lse) lse = at::empty({in.tokens, in.heads}, q.options().dtype(at::kFloat));
-    if (a[6] == Py_None) {   // the tickets alone have to be zero
-        scratch = at::empty({(int64_t)NNC_ATTN_PAGED_SCRATCH_BYTES}, q.options().dtype(at::kByte));
-        scratch.narrow(0, 0, NNC_ATTN_PAGED_TICKET_BYTES).zero_();
-    } else {
-        scratch = tensor(a[6], "scratch");
-        if (!scratch.is_cuda() || scratch.get_device() != device || !scratch.is_contiguous()) refuse("scratch: a contiguous tensor on the call's CUDA device (attn_paged_scratch)");
-    }
-    launch(device, "nnc_op_attn_decode_paged", [&](void *stream) {
-        return call_attn(q.data_ptr(), &c, at_lens, out.data_ptr(), want_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, in.type, (int32_t)in.tokens,
-                         (int32_t)in.heads, in.row, to.row, scale, (int32_t)window, scratch.data_ptr(), scratch.nbytes(), stream);
+    const int32_t *at_lens = index_of(tensor(a[4], "lens"), in.tokens, device, "lens");
+    at::Tensor scores = at::empty({in.tokens, c.n_kv_heads, c.pages_per_seq}, q.options().dtype(at::kFloat));
+    launch(device, "nnc_op_score_pages", [&](void *stream) {
+        return call_score(q.data_ptr(), &c, bounds.data_ptr(), at_lens, static_cast<float *>(scores.data_ptr()), in.type, (int32_t)in.tokens, (int32_t)in.heads, in.row, stream);
     });
-    if (a[7] != Py_None) written(out);
-    if (want_lse) return pair(out, lse);
-    return THPVariable_Wrap(out);
+    return THPVariable_Wrap(scores);
+}
+
+// select_pages(scores, lens, page_size, n, first, last)
+PyObject *select_pages(PyObject *const *a) {
+    const at::Tensor &scores = tensor(a[0], "scores"), &lens = tensor(a[1], "lens");
+    if (scores.scalar_type() != at::kFloat || scores.dim() != 3 || !scores.is_contiguous() || !scores.is_cuda()) refuse("scores: contiguous float32 [batch][n_kv_heads][pages] on a CUDA device");
+    const int device = static_cast<int>(scores.get_device());
+    const int64_t batch = scores.size(0), heads = scores.size(1), columns = scores.size(2);
+    if (batch > INT32_MAX || heads > INT32_MAX || columns > INT32_MAX) refuse("sizes: 32-bit numbers");
+    const int32_t *at_lens = index_of(lens, batch, device, "lens");
+    const int32_t page_size = whole(a[2], 1, "page_size: a cache's"), n = whole(a[3], 1, "n: a number of pages");
+    const int32_t first = whole(a[4], 0, "first, last: numbers of pages"), last = whole(a[5], 0, "first, last: numbers of pages");
+    at::Tensor pages = at::empty({batch, heads, n}, scores.options().dtype(at::kInt)), counts = at::empty({batch, heads}, scores.options().dtype(at::kInt));
+    launch(device, "nnc_op_select_pages", [&](void *stream) {
+        return call_select(static_cast<const float *>(scores.data_ptr()), at_lens, static_cast<int32_t *>(pages.data_ptr()), static_cast<int32_t *>(counts.data_ptr()),
+                           (int32_t)batch, (int32_t)heads, (int32_t)columns, page_size, n, first, last, stream);
+    });
+    return pair(pages, counts);
 }
 
 template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -371,10 +486,10 @@ template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, 
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of the four entry points, NncError)
+// bind(addresses of the entry points, NncError)
 PyObject *bind(PyObject *const *a) {
-    void *p[4];
-    for (int i = 0; i < 4; ++i) {
+    void *p[8];
+    for (int i = 0; i < 8; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) refuse("bind: addresses");
     }
@@ -382,14 +497,19 @@ PyObject *bind(PyObject *const *a) {
     call_write = reinterpret_cast<decltype(call_write)>(p[1]);
     call_read = reinterpret_cast<decltype(call_read)>(p[2]);
     call_attn = reinterpret_cast<decltype(call_attn)>(p[3]);
+    call_bounds = reinterpret_cast<decltype(call_bounds)>(p[4]);
+    call_score = reinterpret_cast<decltype(call_score)>(p[5]);
+    call_select = reinterpret_cast<decltype(call_select)>(p[6]);
+    call_selected = reinterpret_cast<decltype(call_selected)>(p[7]);
     Py_XDECREF(error_class);
-    Py_INCREF(a[4]);
-    error_class = a[4];
+    Py_INCREF(a[8]);
+    error_class = a[8];
     Py_RETURN_NONE;
 }
 
 #define NNC_ENTRY(name, n) {#name, (PyCFunction)(void *)entry<name, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {NNC_ENTRY(bind, 5), NNC_ENTRY(rope, 7), NNC_ENTRY(kv_write, 6), NNC_ENTRY(kv_read, 7), NNC_ENTRY(attn, 9), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {NNC_ENTRY(bind, 9), NNC_ENTRY(rope, 7), NNC_ENTRY(kv_write, 6), NNC_ENTRY(kv_read, 7), NNC_ENTRY(attn, 9),
+                         NNC_ENTRY(page_bounds, 5), NNC_ENTRY(score_pages, 5), NNC_ENTRY(select_pages, 6), NNC_ENTRY(attn_selected, 10), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
