@@ -390,6 +390,21 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
                              int32_t batch, int32_t n_q_heads, int64_t q_stride, int64_t out_stride, float scale, int32_t window,
                              void *scratch, size_t scratch_bytes, void *cuda_stream);
 
+/* The same where groups of sequences share their first positions (one system prompt, one document): the shared rows are read once for all
+ * sequences of a group, not once for each.  Group g is the sequences starts[g] .. starts[g + 1] - 1 (int32 [n_groups + 1], not
+ * descending, within 0 .. batch); its sequences have positions 0 .. shared[g] - 1 in common (int32 [n_groups]), which are read
+ * through the page table of the group's first sequence, whole pages of them (what is left of the last page counts as each sequence's own).
+ * The cache holds all of them, whatever the sequences' lengths; a shorter sequence attends to its first lens[b].  Sequences of
+ * no group, and of groups with shared[g] below a page, attend to their own rows alone.  A `starts` that descends or leaves 0 .. batch
+ * and a shared[g] outside 0 .. the table's reach are cut to what is allowed and set the status word.  1 <= n_groups <= batch.
+ *   q, out, lens, lse, scale, strides: as there, without a window.  fp32 queries and results are computed sequence by sequence.
+ * scratch: DEVICE, 256-byte aligned, nnc_attn_prefix_scratch_bytes(batch, n_q_heads, head_dim); its first NNC_ATTN_PAGED_TICKET_BYTES as
+ * there.  Three launches. */
+size_t nnc_attn_prefix_scratch_bytes(int32_t batch, int32_t n_q_heads, int32_t head_dim);
+int nnc_op_attn_prefix_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, const int32_t *starts, const int32_t *shared,
+                             int32_t n_groups, void *out, float *lse, int32_t type, int32_t batch, int32_t n_q_heads, int64_t q_stride,
+                             int64_t out_stride, float scale, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
 /* ---- long caches: pages chosen by a score --------------------------------------------------------------------
  * A decoding step that reads part of a long cache: for every page the lowest and the highest of its keys, element by element
  * (nnc_op_page_bounds, after rows were written), the most that a query's product with a key between them can be (nnc_op_score_pages), the

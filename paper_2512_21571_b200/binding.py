@@ -114,6 +114,10 @@ EXPORTS = {
     "nnc_op_attn_selected_paged": (C.c_int, [C.c_void_p, C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
                                              C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_float,
                                              C.c_void_p, C.c_size_t, C.c_void_p]),
+    "nnc_attn_prefix_scratch_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "nnc_op_attn_prefix_paged": (C.c_int, [C.c_void_p, C.POINTER(nnc_paged_kv), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                           C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, C.c_float,
+                                           C.c_void_p, C.c_size_t, C.c_void_p]),
 }
 for _name, (_res, _args) in EXPORTS.items():
     _fn = getattr(lib, _name)
@@ -451,11 +455,13 @@ except ImportError as e:
 else:
     _calls.bind(*(C.cast(getattr(lib, n), C.c_void_p).value for n in
                   ("nnc_op_rope", "nnc_op_kv_write_paged", "nnc_op_kv_read_paged", "nnc_op_attn_decode_paged", "nnc_op_page_bounds",
-                   "nnc_op_score_pages", "nnc_op_select_pages", "nnc_op_attn_selected_paged")), NncError)
+                   "nnc_op_score_pages", "nnc_op_select_pages", "nnc_op_attn_selected_paged", "nnc_op_attn_prefix_paged",
+                   "nnc_attn_prefix_scratch_bytes")), NncError)
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp_turns": 3, "ramp_index": 4}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
 ATTN_PAGED_SCRATCH_BYTES = 16 << 20
+ATTN_PAGED_TICKET_BYTES = 8192
 
 
 def _device(t: torch.Tensor, what: str) -> int:
@@ -575,6 +581,25 @@ def op_attn_decode_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, sc
     sequence, the last `window` of them if window > 0.  scale: 1 / sqrt(head_dim) if None.  out: None, q itself, or a tensor of q's
     shape and type that q does not overlap.  Returns out, or (out, lse)."""
     return _calls.attn(cache.address, cache.index, q, lens, scale, window, scratch, out, want_lse)
+
+
+def attn_prefix_scratch(batch: int, n_q_heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A scratch buffer for op_attn_prefix_paged on up to `batch` sequences, to be made once and kept; calls that share one must not overlap."""
+    nbytes = lib.nnc_attn_prefix_scratch_bytes(batch, n_q_heads, head_dim)
+    if nbytes == 0:
+        raise ValueError("batch, n_q_heads, head_dim: sizes that op_attn_prefix_paged takes")
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    scratch[:ATTN_PAGED_TICKET_BYTES].zero_()
+    return scratch
+
+
+def op_attn_prefix_paged(q: torch.Tensor, cache: PagedKV, lens: torch.Tensor, starts: torch.Tensor, shared: torch.Tensor,
+                         scale: Optional[float] = None, scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                         want_lse: bool = False):
+    """nnc_op_attn_prefix_paged: op_attn_decode_paged (without a window) where sequences starts[g] .. starts[g + 1] - 1 have their first
+    shared[g] positions in common, whose rows are read once for all of them.  int32 starts [groups + 1], shared [groups]; scratch:
+    attn_prefix_scratch, or None; scale and out as there.  Returns out, or (out, lse)."""
+    return _calls.attn_prefix(cache.address, cache.index, q, lens, starts, shared, scale, scratch, out, want_lse)
 
 
 # ---- long caches: pages chosen by a score ------------------------------------------------------------------------

@@ -1,0 +1,72 @@
+// What the kernels of the attention behind a shared prefix have in common: groups of sequences, the list of tiles, scratch.
+#pragma once
+#include "paged.cuh"
+
+namespace nnc {
+
+constexpr int kPrefixRows = 128;       // query rows of a tile: (sequence of the group, query head of the KV head)
+constexpr int kPrefixStep = 64;        // positions of a step
+constexpr int kPrefixFixed = 2;        // places in the list for what it costs to begin and to end a tile, in steps
+constexpr int kPrefixMaxCtas = 320;
+
+struct PrefixGroups {
+    const int32_t *starts, *shared;
+    int n_groups, batch;
+};
+
+// where a group's tiles stand in the list
+struct PrefixPlan {
+    long long base;                    // first place
+    int b0, rows, tiles, steps;        // first sequence, query rows and tiles per KV head, steps of a tile (0: no prefix)
+    int prefix, unused;                // positions
+};
+struct PrefixHead {
+    long long share;                   // places of a CTA
+    long long unused;
+};
+
+// positions of a group that its sequences share: whole pages
+__device__ __forceinline__ int prefix_of(const PagedView &c, const PrefixGroups &s, int g) {
+    return min(max(s.shared[g], 0), c.pages_per_seq << c.page_shift) >> c.page_shift << c.page_shift;
+}
+
+// the group of a sequence, or -1 (whatever `starts` holds, the answer lies in range)
+__device__ __forceinline__ int group_of(const PrefixGroups &s, int b) {
+    int lo = -1, hi = s.n_groups;      // starts[lo] <= b < starts[hi], where these exist
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s.starts[mid] <= b) lo = mid;
+        else hi = mid;
+    }
+    return lo >= 0 && b < s.starts[lo + 1] ? lo : -1;
+}
+
+__device__ __forceinline__ PrefixPlan plan_of(const PagedView &c, const PrefixGroups &s, int g, int group) {
+    PrefixPlan p;
+    p.b0 = min(max(s.starts[g], 0), s.batch);
+    p.rows = max(min(max(s.starts[g + 1], 0), s.batch) - p.b0, 0) * group;
+    p.tiles = (p.rows + kPrefixRows - 1) / kPrefixRows;
+    p.prefix = prefix_of(c, s, g);
+    p.steps = p.rows ? (p.prefix + kPrefixStep - 1) / kPrefixStep : 0;
+    p.base = 0;
+    p.unused = 0;
+    return p;
+}
+__device__ __forceinline__ long long places_of(const PagedView &c, const PrefixPlan &p) {
+    return p.steps ? (long long)c.n_kv * p.tiles * (p.steps + kPrefixFixed) : 0;
+}
+
+// Partial results: a row for every query row of a (tile, CTA) pair that occurs.  Pairs in the list's order move on by a tile's rows or by
+// a CTA, so row (rows of earlier tiles) + 128 CTA is a pair's own.
+struct PrefixScratch {
+    PrefixHead *head;
+    PrefixPlan *plan;                  // [n_groups]
+    float2 *ml;                        // [rows]: reference in log2 units, sum
+    float *o;                          // [rows][D]
+    float *tail_lse, *tail;            // [batch][n_q] and [batch][n_q][D]: what lies behind the prefix
+};
+
+cudaError_t launch_attn_tail(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const PrefixGroups &groups, float *out,
+                             float *lse, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes);
+
+}  // namespace nnc

@@ -1070,6 +1070,29 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
     return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
 }
 
+size_t nnc_attn_prefix_scratch_bytes(int32_t batch, int32_t n_q_heads, int32_t head_dim) {
+    if (batch < 0 || n_q_heads <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+    return attn_prefix_scratch_bytes(batch, n_q_heads, head_dim);
+}
+
+int nnc_op_attn_prefix_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, const int32_t *starts, const int32_t *shared,
+                             int32_t n_groups, void *out, float *lse, int32_t type, int32_t batch, int32_t n_q_heads, int64_t q_stride,
+                             int64_t out_stride, float scale, void *scratch, size_t scratch_bytes, void *cuda_stream) {
+    if (int rc = paged_queries_ok(cache, type, batch, n_q_heads); rc != NNC_OK) return rc;
+    if (batch == 0) return NNC_OK;
+    if (n_groups < 1 || n_groups > batch) return NNC_ERR_INVALID_ARG;
+    if (!lens || !starts || !shared || !scratch || !paged_rows_aligned(q, type, q_stride) || !paged_rows_aligned(out, type, out_stride)) return NNC_ERR_INVALID_ARG;
+    if (((uintptr_t)lens | (uintptr_t)starts | (uintptr_t)shared | (uintptr_t)lse) & 3) return NNC_ERR_INVALID_ARG;
+    // rows of a pool are the 32-bit coordinates of a tensor map; a CTA a row of the results
+    if ((int64_t)cache->n_pages * cache->n_kv_heads * cache->page_size > 0x7fffff00 || (int64_t)batch * n_q_heads > 0x7fffffff) return NNC_ERR_CAPACITY;
+    if (((uintptr_t)scratch & 255) || scratch_bytes < attn_prefix_scratch_bytes(batch, n_q_heads, cache->head_dim)) return NNC_ERR_WORKSPACE;
+    LaunchCtx lc;
+    if (paged_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
+    cudaError_t e = launch_attn_prefix(lc, q, *cache, lens, starts, shared, n_groups, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, scratch);
+    if (e == cudaErrorInvalidValue) return NNC_ERR_CAPACITY;
+    return e == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;
+}
+
 int nnc_op_page_bounds(const nnc_paged_kv *cache, void *bounds, const int32_t *lens, const int32_t *first, int32_t batch, void *cuda_stream) {
     if (!paged_ok(cache) || batch < 0 || batch > cache->n_seqs) return NNC_ERR_INVALID_ARG;
     if (batch == 0) return NNC_OK;

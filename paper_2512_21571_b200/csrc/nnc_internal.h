@@ -142,6 +142,11 @@ cudaError_t launch_attn_paged(const LaunchCtx &lc, const void *q, const nnc_page
 cudaError_t launch_attn_selected(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const int32_t *pages,
                                  const int32_t *counts, int list_len, void *out, float *lse, int type, int batch, int n_q_heads,
                                  int64_t q_stride, int64_t out_stride, float scale, void *scratch, size_t scratch_bytes);
+// attn_prefix.cu
+size_t attn_prefix_scratch_bytes(int batch, int n_q_heads, int head_dim);
+cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const int32_t *starts,
+                               const int32_t *shared, int n_groups, void *out, float *lse, int type, int batch, int n_q_heads, int64_t q_stride,
+                               int64_t out_stride, float scale, void *scratch);
 // pages.cu
 constexpr int kMaxScoredGroup = 128;   // query heads per KV head: their terms are held in shared memory
 cudaError_t launch_page_bounds(const LaunchCtx &lc, const nnc_paged_kv &cache, void *bounds, const int32_t *lens, const int32_t *first, int batch);

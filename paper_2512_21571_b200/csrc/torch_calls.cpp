@@ -30,6 +30,8 @@ decltype(&nnc_op_page_bounds) call_bounds;
 decltype(&nnc_op_score_pages) call_score;
 decltype(&nnc_op_select_pages) call_select;
 decltype(&nnc_op_attn_selected_paged) call_selected;
+decltype(&nnc_op_attn_prefix_paged) call_prefix;
+decltype(&nnc_attn_prefix_scratch_bytes) prefix_scratch_bytes;
 PyObject *error_class;   // NncError(status, detail)
 
 struct Refused {};   // a Python error is set
@@ -412,6 +414,23 @@ PyObject *attn_selected(PyObject *const *a) {
     return x.result();
 }
 
+// attn_prefix(cache, device, q, lens, starts, shared, scale or None, scratch or None, out or None, want_lse)
+PyObject *attn_prefix(PyObject *const *a) {
+    Attention x(a[0], a[1], a[2], a[6], a[8], a[9]);
+    const int32_t *at_lens = index_of(tensor(a[3], "lens"), x.in.tokens, x.device, "lens");
+    const at::Tensor &starts = tensor(a[4], "starts"), &shared = tensor(a[5], "shared");
+    const int64_t groups = shared.dim() == 1 ? shared.size(0) : -1;
+    if (groups < 0 || groups > x.in.tokens || (groups == 0 && x.in.tokens > 0)) refuse("shared: contiguous int32 numbers, one a group, at most one group a sequence");
+    const int32_t *at_starts = index_of(starts, groups + 1, x.device, "starts"), *at_shared = index_of(shared, groups, x.device, "shared");
+    x.take_scratch(a[7], (int64_t)prefix_scratch_bytes((int32_t)x.in.tokens, (int32_t)x.in.heads, (int32_t)x.in.d), NNC_ATTN_PAGED_TICKET_BYTES,
+                   "scratch: a contiguous tensor on the call's CUDA device (attn_prefix_scratch)");
+    launch(x.device, "nnc_op_attn_prefix_paged", [&](void *stream) {
+        return call_prefix(x.q.data_ptr(), &x.c, at_lens, at_starts, at_shared, (int32_t)groups, x.out.data_ptr(), x.lse_at(), x.in.type, (int32_t)x.in.tokens,
+                           (int32_t)x.in.heads, x.in.row, x.to.row, x.scale, x.scratch.data_ptr(), x.scratch.nbytes(), stream);
+    });
+    return x.result();
+}
+
 // a cache's bounds: [n_pages][n_kv_heads][2][head_dim]
 const at::Tensor &bounds_of(PyObject *o, const nnc_paged_kv &c, int device) {
     const at::Tensor &t = tensor(o, "bounds");
@@ -488,8 +507,8 @@ template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, 
 
 // bind(addresses of the entry points, NncError)
 PyObject *bind(PyObject *const *a) {
-    void *p[8];
-    for (int i = 0; i < 8; ++i) {
+    void *p[10];
+    for (int i = 0; i < 10; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) refuse("bind: addresses");
     }
@@ -501,15 +520,17 @@ PyObject *bind(PyObject *const *a) {
     call_score = reinterpret_cast<decltype(call_score)>(p[5]);
     call_select = reinterpret_cast<decltype(call_select)>(p[6]);
     call_selected = reinterpret_cast<decltype(call_selected)>(p[7]);
+    call_prefix = reinterpret_cast<decltype(call_prefix)>(p[8]);
+    prefix_scratch_bytes = reinterpret_cast<decltype(prefix_scratch_bytes)>(p[9]);
     Py_XDECREF(error_class);
-    Py_INCREF(a[8]);
-    error_class = a[8];
+    Py_INCREF(a[10]);
+    error_class = a[10];
     Py_RETURN_NONE;
 }
 
 #define NNC_ENTRY(name, n) {#name, (PyCFunction)(void *)entry<name, n>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {NNC_ENTRY(bind, 9), NNC_ENTRY(rope, 7), NNC_ENTRY(kv_write, 6), NNC_ENTRY(kv_read, 7), NNC_ENTRY(attn, 9),
-                         NNC_ENTRY(page_bounds, 5), NNC_ENTRY(score_pages, 5), NNC_ENTRY(select_pages, 6), NNC_ENTRY(attn_selected, 10), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {NNC_ENTRY(bind, 11), NNC_ENTRY(rope, 7), NNC_ENTRY(kv_write, 6), NNC_ENTRY(kv_read, 7), NNC_ENTRY(attn, 9),
+                         NNC_ENTRY(page_bounds, 5), NNC_ENTRY(score_pages, 5), NNC_ENTRY(select_pages, 6), NNC_ENTRY(attn_selected, 10), NNC_ENTRY(attn_prefix, 10), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

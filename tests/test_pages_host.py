@@ -56,3 +56,20 @@ def test_attention_calls_that_are_refused_and_empty_ones(nnc):
     assert call(nbytes=(16 << 20) - 1) == WORKSPACE and call(scratch=P + 128) == WORKSPACE
     assert call(list_len=1 << 26) == CAPACITY
     assert call(batch=0) == 0 and call(batch=0, q=None, out=None, lens=None, pages=None, scratch=None) == 0
+
+
+def test_prefix_calls_that_are_refused_and_empty_ones(nnc):
+    nbytes = nnc.lib.nnc_attn_prefix_scratch_bytes(4, 8, 128)
+    assert nbytes > 16 << 20 and nnc.lib.nnc_attn_prefix_scratch_bytes(0, 8, 128) > 0
+    assert [nnc.lib.nnc_attn_prefix_scratch_bytes(*x) for x in ((-1, 8, 128), (4, 0, 128), (4, 8, 96))] == [0, 0, 0]
+    good = dict(q=P, cache=C.byref(_cache(nnc)), lens=P, starts=P, shared=P, n_groups=2, out=P, lse=None, type=1, batch=4, nq=8, qs=1024, os=1024, scale=1.0,
+                scratch=P, nbytes=nbytes)
+    call = lambda **kw: nnc.lib.nnc_op_attn_prefix_paged(*{**good, **kw}.values(), None)
+    codes, half = C.byref(_cache(nnc, type=3, k_scale=P, v_scale=P)), C.byref(_cache(nnc, type=2))
+    for bad in (dict(q=None), dict(cache=None), dict(lens=None), dict(starts=None), dict(shared=None), dict(out=None), dict(scratch=None), dict(type=2), dict(type=3),
+                dict(cache=half), dict(cache=codes, type=3), dict(batch=-1), dict(batch=5), dict(nq=0), dict(nq=7), dict(n_groups=0), dict(n_groups=5), dict(n_groups=-1),
+                dict(q=P + 8), dict(out=P + 8), dict(qs=1023), dict(os=4), dict(type=0, qs=1022), dict(lens=P + 2), dict(starts=P + 2), dict(shared=P + 1), dict(lse=P + 1)):
+        assert call(**bad) == INVALID, bad
+    assert call(nbytes=nbytes - 1) == WORKSPACE and call(scratch=P + 128) == WORKSPACE
+    assert call(cache=C.byref(_cache(nnc, n_pages=1 << 24))) == CAPACITY
+    assert call(batch=0) == 0 and call(batch=0, q=None, out=None, lens=None, starts=None, scratch=None) == 0
