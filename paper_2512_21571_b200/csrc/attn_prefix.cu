@@ -42,11 +42,10 @@ struct PrefixParams {
     PagedView c;
     PrefixGroups groups;
     PrefixScratch s;
-    const char *q;
     const int32_t *lens;
-    long long q_stride, part_rows;
-    int group, n_q, box;                // query heads per KV head, in all; positions of a TMA box
-    uint32_t flip;                      // sign bits of two queries where the scale is negative
+    long long part_rows;
+    int group, per_tile, n_q, box;      // query heads per KV head; sequences of a tile; query heads in all; positions of a TMA box
+    uint32_t flip;                      // the sign bit of the scores where the scale is negative
     float scale_log2;                   // |scale| in log2 units
     int *wait_status;
 };
@@ -61,7 +60,7 @@ struct Step {
 // the first group from g on that has a prefix
 __device__ __forceinline__ void find_group(const PrefixParams &p, Step &at) {
     for (at.plan.steps = 0; at.g < p.groups.n_groups; ++at.g) {
-        at.plan = plan_of(p.c, p.groups, at.g, p.group);
+        at.plan = plan_of(p.c, p.groups, at.g, p.per_tile);
         if (at.plan.steps) return;
     }
 }
@@ -78,6 +77,17 @@ __device__ __forceinline__ void advance(const PrefixParams &p, Step &at) {
     find_group(p, at);
 }
 
+// two floats to nearest even, the first in the low half: one instruction
+__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ void store16(float4 *dst, const uint32_t *v) {
+    *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 __device__ __forceinline__ float top3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -87,7 +97,7 @@ __device__ __forceinline__ float top3(float a, float b, float c) {
 // BF: bf16 caches, otherwise fp16; queries are of the cache's type
 template <int D, bool BF>
 __global__ void __launch_bounds__(kThreads, 2)
-attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PrefixParams p) {
+attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PrefixParams p) {
     typedef Tiles<D> T;
     // fp16 probabilities are scaled by 2^6, so that small ones keep their bits (at most 2^8 by the lazy maximum: below 2^15; sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 6.f;
@@ -110,7 +120,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     volatile int *abort_flag = &abort_s;
     if (tid == 0) {
         abort_s = 0;
-        mbar_init(q_ready, kSoftmaxRows);
+        mbar_init(q_ready, 1);
         for (int st = 0; st < 2; ++st) {
             mbar_init(k_full(st), 1); mbar_init(v_full(st), 1); mbar_init(s_full(st), 1);
             mbar_init(p_full(st), kSoftmaxRows); mbar_init(pv_done(st), 1);
@@ -127,7 +137,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     // ---- the list: its length, and where this CTA's share begins ----
     const int per = (p.groups.n_groups + kThreads - 1) / kThreads, g_lo = min(tid * per, p.groups.n_groups), g_hi = min(g_lo + per, p.groups.n_groups);
     long long mine = 0;
-    for (int g = g_lo; g < g_hi; ++g) mine += places_of(p.c, plan_of(p.c, p.groups, g, p.group));
+    for (int g = g_lo; g < g_hi; ++g) mine += places_of(p.c, plan_of(p.c, p.groups, g, p.per_tile));
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -148,7 +158,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (tid == 0) p.s.head->share = share;
         long long at = before;
         for (int g = g_lo; g < g_hi; ++g) {
-            PrefixPlan plan = plan_of(p.c, p.groups, g, p.group);
+            PrefixPlan plan = plan_of(p.c, p.groups, g, p.per_tile);
             plan.base = at;
             at += places_of(p.c, plan);
             p.s.plan[g] = plan;
@@ -160,7 +170,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         long long rest = t0 - before;
         int g = g_lo;
         for (; g < g_hi; ++g) {
-            const long long n = places_of(p.c, plan_of(p.c, p.groups, g, p.group));
+            const long long n = places_of(p.c, plan_of(p.c, p.groups, g, p.per_tile));
             if (rest < n) break;
             rest -= n;
         }
@@ -173,7 +183,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     at.index = t1;
     if (t0 < t1) {
         at.g = first_g;
-        at.plan = plan_of(p.c, p.groups, at.g, p.group);
+        at.plan = plan_of(p.c, p.groups, at.g, p.per_tile);
         const int per_tile = at.plan.steps + kPrefixFixed;
         const long long item = first_rest / per_tile;
         at.step = (int)(first_rest - item * per_tile);
@@ -188,41 +198,66 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
     }
     auto more = [&]() { return at.index < t1 && at.g < p.groups.n_groups; };
 
-    if (warp == 0) {
-        if (lane == 0) {   // ---------------- TMA producer ----------------
-            Step next = at;                              // K runs one step ahead of V
-            const long long absent = paged_rows(p.c);    // a row outside the tensor: zeros
-            auto load = [&](const Step &x, uint32_t dst, const CUtensorMap *map, uint32_t bar) {
-                mbar_expect_tx(bar, T::kKV);
-                for (int r = 0; r < kPrefixStep; r += p.box) {
-                    const int pos = x.step * kPrefixStep + r;
-                    long long row = absent;
-                    if (pos < x.plan.prefix) {
-                        const int page = p.c.table[(long long)x.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
-                        if ((unsigned)page < (unsigned)p.c.n_pages) row = paged_row(p.c, page, x.head, pos & ((1 << p.c.page_shift) - 1));
-                        else paged_complain(p.c);
-                    }
-                    if (!NNC_BC(row >= 0 && row <= 0x7fffffffll, 3601)) row = absent;
-#pragma unroll
-                    for (int h = 0; h < T::kHalves; ++h) tma_load_2d(dst + h * T::kSlabKV + r * 128, map, bar, 64 * h, (int)row);
-                }
-            };
-            auto more_k = [&]() { return next.index < t1 && next.g < p.groups.n_groups; };
-            // A stage's K tile is free as soon as the S of the step that read it is complete: K_{j+1} is requested when S_{j-1} is
-            // complete, V_j when O += P_{j-2} V_{j-2} is.
-            int k = 0;
-            for (; k < 2 && more_k(); ++k) { load(next, k_tile(k & 1), &map_k, k_full(k & 1)); advance(p, next); }
-            for (int j = 0; more(); ++j) {
-                if (j >= 1 && more_k()) {
-                    if (!mbar_wait(s_full((j - 1) & 1), (uint32_t)(((j - 1) >> 1) & 1), abort_flag, p.wait_status, 41)) break;
-                    load(next, k_tile(k & 1), &map_k, k_full(k & 1));
-                    advance(p, next);
-                    ++k;
-                }
-                if (j >= 2 && !mbar_wait(pv_done(j & 1), (uint32_t)(((j - 2) >> 1) & 1), abort_flag, p.wait_status, 42)) break;
-                load(at, v_tile(j & 1), &map_v, v_full(j & 1));
-                advance(p, at);
+    if (warp == 0) {   // ---------------- TMA producer: a lane a box ----------------
+        // Lane: kind (K or V), box of the step's positions, half of the head's elements.  Rows are looked up a step before K needs them, and V
+        // takes K's.
+        const int half = lane & 1, r = (lane >> 1 & 3) * p.box;
+        const bool loads = lane < 16 && half < T::kHalves && r < kPrefixStep, is_v = lane >= 8;
+        const int absent = (int)min(paged_rows(p.c), 0x7fffffffll);   // a row outside the tensor: zeros
+        Step far = at;                                                // the step whose rows are looked up next
+        auto look = [&]() {
+            if (!(far.index < t1 && far.g < p.groups.n_groups)) return absent;
+            const int pos = far.step * kPrefixStep + r;
+            int page = -1;
+            if (loads && pos < far.plan.prefix) {
+                page = p.c.table[(long long)far.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
+                if ((unsigned)page >= (unsigned)p.c.n_pages) { page = -1; if (!is_v && half == 0) paged_complain(p.c); }
             }
+            const long long row = page < 0 ? absent : paged_row(p.c, page, far.head, pos & ((1 << p.c.page_shift) - 1));
+            advance(p, far);
+            return NNC_BC(row >= 0 && row <= absent, 3601) ? (int)row : absent;
+        };
+        // The box of stage `st` for this kind; the other kind's lanes look on
+        auto load = [&](bool v, int st, int row) {
+            const uint32_t bar = v ? v_full(st) : k_full(st);
+            if (lane == 0) mbar_expect_tx(bar, T::kKV);
+            __syncwarp();
+            if (loads && is_v == v) tma_load_2d((v ? v_tile(st) : k_tile(st)) + half * T::kSlabKV + r * 128, v ? &map_v : &map_k, bar, 64 * half, row);
+        };
+        auto load_queries = [&](const Step &x) {   // [sequence][query head of the KV head][64]: a row of the tile after the other
+            if (lane == 0) mbar_expect_tx(q_ready, (uint32_t)(T::kHalves * p.per_tile * p.group * 128));
+            __syncwarp();
+            if (lane < T::kHalves) tma_load_3d(q_tile + lane * T::kQSlab, &map_q, q_ready, 64 * lane, x.head * p.group, x.plan.b0 + x.tile * p.per_tile);
+        };
+        long long steps = 0;   // of this share
+        for (Step s = at; s.index < t1 && s.g < p.groups.n_groups;) {   // a tile's at a time
+            const long long n = min((long long)(s.plan.steps - s.step), t1 - s.index);
+            steps += n;
+            s.index += n - 1;
+            s.step += (int)n - 1;
+            advance(p, s);
+        }
+        // A stage's K tile is free as soon as the S of the step that read it is complete: K_{j+1} is requested when S_{j-1} is
+        // complete, V_j when O += P_{j-2} V_{j-2} is.
+        int row0 = look(), row1 = look(), row2 = absent;   // of steps j, j + 1, j + 2
+        if (steps > 0) {
+            load_queries(at);
+            load(false, 0, row0);
+        }
+        if (steps > 1) load(false, 1, row1);
+        for (long long j = 0; j < steps; ++j) {
+            const int st = (int)(j & 1);
+            row2 = look();
+            if (j >= 1) {
+                if (!__all_sync(0xffffffffu, mbar_wait(s_full(st ^ 1), (uint32_t)(((j - 1) >> 1) & 1), abort_flag, p.wait_status, 41))) break;
+                advance(p, at);
+                if (at.step == 0) load_queries(at);   // a new tile's: the last one's have been multiplied for the last time
+                if (j + 1 < steps) load(false, st ^ 1, row1);
+            }
+            if (j >= 2 && !__all_sync(0xffffffffu, mbar_wait(pv_done(st), (uint32_t)(((j - 2) >> 1) & 1), abort_flag, p.wait_status, 42))) break;
+            load(true, st, row0);
+            row0 = row1;
+            row1 = row2;
         }
     } else if (warp == 1) {
         if (lane == 0) {   // ---------------- MMA issuer ----------------
@@ -254,8 +289,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             bool ok = !more() || issue_qk(0);
             bool begins = true;
             for (int j = 0; ok && more(); ++j) {
-                // (a tile's first product waits for its queries, which come after the last probabilities of the tile before it)
-                const bool early = next.step != 0;
+                const bool early = next.step != 0;   // a tile's first product waits for its queries: behind the last product of the tile before it
                 if (early && more_qk() && !issue_qk(j + 1)) break;
                 const int st = j & 1, u = j >> 1;
                 if (!mbar_wait(p_full(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 46)) break;
@@ -278,29 +312,14 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const int quarter = warp & 3, r = quarter * 32 + lane;   // the quarter of tensor memory's lanes that this warp may touch
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, to = tmem_base + lane_addr + kColO;
         bool ok = true, begins = true;
-        int limit = 0;                                           // positions that this thread's query attends to
         long long out_row = -1;                                  // among the results
         bool idle = false;                                       // no query of this warp counts
         float m_used = -INFINITY, l = 0.f;
-        // a tile's queries to shared memory, K-major under the 128-byte swizzle (16-byte chunk index XOR row % 8)
-        auto take_queries = [&]() {
-            const int row = at.tile * kPrefixRows + r;
-            const bool valid = row < at.plan.rows;
-            const int b = at.plan.b0 + (valid ? row / p.group : 0), h = at.head * p.group + (valid ? row % p.group : 0);
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (b * p.q_stride + (long long)h * D) * 2);
-            uint4 x[D / 8];
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) x[i] = valid ? src[i] : make_uint4(0u, 0u, 0u, 0u);
-            limit = valid ? min(at.plan.prefix, p.lens[b]) : at.plan.prefix;
-            out_row = valid ? (long long)at.plan.b0 * p.n_q + (long long)at.head * at.plan.rows + row + kPrefixRows * cta : -1;
-            idle = at.tile * kPrefixRows + quarter * 32 >= at.plan.rows;
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) {
-                const uint32_t dst = q_tile + (uint32_t)((i >> 3) * T::kQSlab + r * 128 + (((i & 7) ^ (r & 7)) << 4));
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(x[i].x ^ p.flip), "r"(x[i].y ^ p.flip), "r"(x[i].z ^ p.flip), "r"(x[i].w ^ p.flip) : "memory");
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // generic-proxy writes, async-proxy (MMA) reads
-            mbar_arrive(q_ready);
+        auto begin_tile = [&]() {
+            const int member = r / p.group, nth = at.tile * p.per_tile + member;
+            const bool valid = member < p.per_tile && nth < at.plan.members && takes_prefix(at.plan.prefix, p.lens[at.plan.b0 + nth]);
+            out_row = valid ? (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + (r - member * p.group) + kPrefixRows * cta : -1;
+            idle = !__any_sync(0xffffffffu, valid);
         };
         // pages that the pool does not have: a lane's 16 positions of a step, looked up a step ahead
         auto has_page = [&](const Step &x) {
@@ -310,7 +329,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         bool has = true;
         if (more()) {
             has = has_page(at);
-            take_queries();
+            begin_tile();
         }
         for (int j = 0; more(); ++j) {
             const int st = j & 1, u = j >> 1, p0 = at.step * kPrefixStep;
@@ -325,7 +344,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             if (idle) {   // (its rows of P are whatever the scores' bits are, and nobody's)
                 mbar_arrive(p_full(st));
                 at = next;
-                if (ends && !last) take_queries();
+                if (ends && !last) begin_tile();
                 continue;
             }
             const uint32_t ts = tmem_base + lane_addr + kColS + (uint32_t)st * kPrefixStep;
@@ -333,12 +352,16 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             tmem_ld32_nowait(ts, sv[0]);
             tmem_ld32_nowait(ts + 32u, sv[1]);
             tmem_wait_ld();
-            if (__any_sync(0xffffffffu, p0 + kPrefixStep > limit) || there != 0xfu) {
+            if (p.flip) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) { sv[0][e] ^= p.flip; sv[1][e] ^= p.flip; }
+            }
+            if (p0 + kPrefixStep > at.plan.prefix || there != 0xfu) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
-                        if (p0 + 32 * c + e >= limit || !(there >> (2 * c + e / 16) & 1u)) sv[c][e] = 0xff800000u;   // -infinity
+                        if (p0 + 32 * c + e >= at.plan.prefix || !(there >> (2 * c + e / 16) & 1u)) sv[c][e] = 0xff800000u;   // -infinity
             }
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -352,7 +375,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 m_used = m_step;
             } else {
                 // the maximum that O refers to moves only when a step passes it by 2^8
-                const bool need = m_step > m_used + kLazyMax;
+                const bool need = out_row >= 0 && m_step > m_used + kLazyMax;
                 if (__any_sync(0xffffffffu, need)) {
                     ok = __all_sync(0xffffffffu, mbar_wait(pv_done((j - 1) & 1), (uint32_t)(((j - 1) >> 1) & 1), abort_flag, p.wait_status, 49));
                     if (!ok) break;
@@ -384,9 +407,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                     const float2 w = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                     sum[e & 1] = __fadd2_rn(sum[e & 1], w);
                     if constexpr (BF) {
-                        hi[e] = pack_bf16x2(w.x, w.y);
-                        const float2 rest = __fadd2_rn(w, make_float2(-bf16_lo(hi[e]), -bf16_hi(hi[e])));
-                        lo[e] = pack_bf16x2(rest.x, rest.y);
+                        hi[e] = round_bf16x2(w.x, w.y);
+                        lo[e] = round_bf16x2(w.x - bf16_lo(hi[e]), w.y - bf16_hi(hi[e]));
                     } else {
                         const __half2 a = __floats2half2_rn(w.x, w.y);
                         const float2 f = __half22float2(a);
@@ -405,9 +427,9 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             at = next;
             begins = ends;
             if (!ends && !last) continue;
-            // ---- the share's part of a tile is done; the next tile's queries are on their way while its last product runs ----
+            // ---- the share's part of a tile is done ----
             const long long row = out_row;
-            if (!last) take_queries();
+            if (!last) begin_tile();
             ok = __all_sync(0xffffffffu, mbar_wait(pv_done(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 50));
             if (!ok) break;
             tc_fence_after();
@@ -418,9 +440,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
                 uint32_t t[32];
                 tmem_ld32(to + 32u * c, t);
                 if (!store) continue;
-                uint4 *dst = reinterpret_cast<uint4 *>(p.s.o + row * D + 32 * c);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e] = make_uint4(t[4 * e], t[4 * e + 1], t[4 * e + 2], t[4 * e + 3]);
+                for (int e = 0; e < 8; ++e) store16(p.s.o + (8 * c + e) * p.part_rows + row, t + 4 * e);
             }
             tc_fence_before();
             m_used = -INFINITY;
@@ -441,9 +462,14 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemColumns) : "memory");
 }
 
-// ---- joining: a CTA a (sequence, query head) ----------------------------------------------------------------------------------
+// ---- joining: a CTA a (sequence, KV head) -------------------------------------------------------------------------------------
+//
+// Its query heads' rows are neighbours in every piece.  A thread takes four elements of a row, of every kth piece where rows are few; the
+// weights of up to kJoinPieces pieces are computed first, by a warp a row.
 
-constexpr int kJoinWarps = 4;
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 8;           // query heads at a time
+constexpr int kJoinPieces = kPrefixMaxCtas;
 
 struct JoinParams {
     PagedView c;
@@ -453,111 +479,133 @@ struct JoinParams {
     char *out;
     float *lse;
     long long out_stride, part_rows;
-    int group, n_q;
+    int group, per_tile, n_q;
 };
 
-template <int D, bool BF, bool FINITE>   // BF: results are bf16, otherwise fp16; FINITE: codes, which hold no infinities
-__global__ void __launch_bounds__(kJoinWarps * 32) attn_prefix_join_kernel(const JoinParams p) {
-    constexpr int kOwn = D / 32;   // elements of a lane
-    __shared__ float part[kJoinWarps][D + 2];
+template <int D, bool BF>   // BF: results (and the cache) are bf16, otherwise fp16
+__global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const JoinParams p) {
+    constexpr int kPieces4 = D / 4;                                // of a row
+    __shared__ float wgt[kJoinRows][kJoinPieces + 1];              // of every piece, then of the tail
+    __shared__ float2 tot[kJoinRows];                              // reference, sum
+    __shared__ float4 sums[kJoinThreads];
+    __shared__ uint32_t odd_bits[D];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int b = blockIdx.x / p.n_q, qh = blockIdx.x - b * p.n_q, head = qh / p.group;
-    const long long row = (long long)b * p.n_q + qh;
+    const int b = blockIdx.x / p.c.n_kv, head = blockIdx.x - b * p.c.n_kv;
     const int g = group_of(p.groups, b);
-    long long c_lo = 0, first_row = 0;
-    int n = 0;
+    long long first_row = 0;
+    int n = 0, b0 = 0, prefix = 0;
     if (g >= 0) {
         const PrefixPlan plan = p.s.plan[g];
-        if (plan.steps) {
-            const int r = (b - plan.b0) * p.group + qh - head * p.group;
-            const long long lo = plan.base + ((long long)head * plan.tiles + r / kPrefixRows) * (plan.steps + kPrefixFixed), share = p.s.head->share;
-            c_lo = lo / share;
+        if (plan.steps && takes_prefix(plan.prefix, p.lens[b])) {
+            b0 = plan.b0;
+            prefix = plan.prefix;
+            const long long lo = plan.base + ((long long)head * plan.tiles + (b - b0) / p.per_tile) * (plan.steps + kPrefixFixed), share = p.s.head->share;
+            const long long c_lo = lo / share;
             n = (int)((lo + plan.steps - 1) / share - c_lo) + 1;
-            first_row = (long long)plan.b0 * p.n_q + (long long)head * plan.rows + r + kPrefixRows * c_lo;
-            if (!NNC_BC(first_row >= 0 && first_row + (long long)kPrefixRows * (n - 1) < p.part_rows, 3603)) n = 0;
+            first_row = (long long)b0 * p.n_q + ((long long)head * plan.members + b - b0) * p.group + kPrefixRows * c_lo;
+            if (!NNC_BC(first_row >= 0 && n <= kJoinPieces && first_row + (long long)kPrefixRows * (n - 1) + p.group <= p.part_rows, 3603)) n = 0;
         }
     }
-    // a warp's pieces: c_lo + warp, c_lo + warp + kJoinWarps, ..; warp 0 begins with the tail
-    float m = -INFINITY, l = 0.f, o[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) o[i] = 0.f;
-    auto add = [&](float m2, float l2, const float (&x)[kOwn]) {
-        if (m2 == -INFINITY) return;
-        const float top = fmaxf(m, m2), a = exp2f(m - top), w = exp2f(m2 - top);
-        m = top;
-        l = fmaf(l, a, l2 * w);
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) o[i] = fmaf(o[i], a, x[i] * w);
-    };
-    auto fetch = [&](float (&x)[kOwn], const float *src) {
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) x[i] = src[lane * kOwn + i];
-    };
-    if (warp == 0) {
-        float x[kOwn];
-        fetch(x, p.s.tail + row * D);
-        add(p.s.tail_lse[row] * 1.4426950408889634f, 1.f, x);
-    }
-    constexpr int kAhead = 4;   // pieces whose rows are on their way at a time
-    for (int i0 = warp; i0 < n; i0 += kAhead * kJoinWarps) {
-        float2 ml[kAhead];
-        float x[kAhead][kOwn];
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const int i = i0 + a * kJoinWarps;
-            if (i >= n) continue;
-            ml[a] = p.s.ml[first_row + (long long)kPrefixRows * i];
-            fetch(x[a], p.s.o + (first_row + (long long)kPrefixRows * i) * D);
+    for (int h0 = 0; h0 < p.group; h0 += kJoinRows) {
+        const int rows = min(kJoinRows, p.group - h0);
+        const long long q_row = (long long)b * p.n_q + (long long)head * p.group + h0;
+        if (warp < rows) {
+            const float tail = p.s.tail_lse[q_row + warp] * 1.4426950408889634f;   // the tail's sum is 1 at this reference
+            float top = tail;
+            for (int i = lane; i < n; i += 32) top = fmaxf(top, p.s.ml[first_row + h0 + warp + (long long)kPrefixRows * i].x);
+            top = warp_max(top);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
+            for (int i = lane; i < n; i += 32) {
+                const float2 ml = p.s.ml[first_row + h0 + warp + (long long)kPrefixRows * i];
+                const float w = exp2f(ml.x - ref);
+                wgt[warp][i] = w;
+                sum = fmaf(w, ml.y, sum);
+            }
+            sum = warp_sum(sum);
+            const float w = exp2f(tail - ref);
+            if (lane == 0) {
+                wgt[warp][n] = w;
+                tot[warp] = make_float2(ref, sum + w);
+                if (p.lse) p.lse[q_row + warp] = sum + w == 0.f ? -INFINITY : (ref + log2f(sum + w)) * kLn2;
+            }
         }
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (i0 + a * kJoinWarps < n) add(ml[a].x, ml[a].y, x[a]);
-    }
-    if (lane == 0) { part[warp][D] = m; part[warp][D + 1] = l; }
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) part[warp][lane * kOwn + i] = o[i];
-    __syncthreads();
-    float M = -INFINITY, L = 0.f, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, part[w][D]);
-    const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) {
-        const float a = exp2f(part[w][D] - ref);
-        L = fmaf(part[w][D + 1], a, L);
-        if (tid < D) sum = fmaf(part[w][tid], a, sum);
-    }
-    if constexpr (!FINITE) {
-        // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs, or
-        // NaN, leave no number); a weight of 0 made NaN of it.  So where a sum is no number the rows are looked through again.
-        if (__syncthreads_or(tid < D && !(fabsf(sum) < INFINITY))) {
-            uint32_t bits = 0;
-            const float behind = tid < D ? p.s.tail[row * D + tid] : 0.f;
-            if (!(fabsf(behind) < INFINITY)) bits = behind != behind ? 4u : behind > 0.f ? 1u : 2u;
-            const int end = g < 0 ? 0 : min(prefix_of(p.c, p.groups, g), p.lens[b]);
-            const int b0 = g < 0 ? 0 : p.s.plan[g].b0;
-            if (n > 0 && tid < D) {
-#pragma unroll 4
-                for (int pos = 0; pos < end; ++pos) {
-                    const int page = p.c.table[(long long)b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
-                    if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
-                    constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
-                    const uint32_t x = reinterpret_cast<const uint16_t *>(p.c.v)[paged_row(p.c, page, head, pos & ((1 << p.c.page_shift) - 1)) * D + tid], size = x & 0x7fffu;
-                    if (size >= kInf) bits |= size > kInf ? 4u : x == size ? 1u : 2u;
+        __syncthreads();
+        // thread: element group c4 of row h, pieces k, k + apart, ..
+        const int items = rows * kPieces4, apart = kJoinThreads / items;
+        {
+            const int item = tid % items, k = tid / items;
+            const bool mine = k < apart;
+            const int h = mine ? item % rows : 0, c4 = mine ? item / rows : 0;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (mine) {
+                const float4 *src = p.s.o + c4 * p.part_rows + first_row + h0 + h;
+#pragma unroll 8
+                for (int i = k; i < n; i += apart) {
+                    const float w = wgt[h][i];
+                    const float4 v = src[(long long)kPrefixRows * i];
+                    sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
+                }
+                if (k == 0) {
+                    const float w = wgt[h][n];
+                    const float4 v = *reinterpret_cast<const float4 *>(p.s.tail + (q_row + h) * D + 4 * c4);
+                    sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
                 }
             }
-            if (bits) sum = bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
+            if (apart > 1) {
+                sums[tid] = sum;
+                __syncthreads();
+                if (mine && k == 0)
+                    for (int j = 1; j < apart; ++j) {
+                        const float4 v = sums[item + j * items];
+                        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+                    }
+            }
+            const bool store = mine && k == 0;
+            // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs,
+            // or NaN, leave no number); a weight of 0 made NaN of it.  So where a sum is no number the rows are looked through again.
+            if (__syncthreads_or(store && !(fabsf((sum.x + sum.y) + (sum.z + sum.w)) < INFINITY))) {
+                if (tid < D) {
+                    uint32_t bits = 0;
+                    const int end = n > 0 ? prefix : 0;
+#pragma unroll 4
+                    for (int pos = 0; pos < end; ++pos) {
+                        const int page = p.c.table[(long long)b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
+                        if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
+                        constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+                        const uint32_t x = reinterpret_cast<const uint16_t *>(p.c.v)[paged_row(p.c, page, head, pos & ((1 << p.c.page_shift) - 1)) * D + tid], size = x & 0x7fffu;
+                        if (size >= kInf) bits |= size > kInf ? 4u : x == size ? 1u : 2u;
+                    }
+                    odd_bits[tid] = bits;
+                }
+                __syncthreads();
+                if (store) {
+                    float *const s[4] = {&sum.x, &sum.y, &sum.z, &sum.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t bits = odd_bits[4 * c4 + e];
+                        const float behind = p.s.tail[(q_row + h) * D + 4 * c4 + e];
+                        if (!(fabsf(behind) < INFINITY)) bits |= behind != behind ? 4u : behind > 0.f ? 1u : 2u;
+                        if (bits) *s[e] = bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
+                    }
+                }
+            }
+            if (store) {
+                const float L = tot[h].y, inv = L == 0.f ? 0.f : 1.f / L;
+                const long long at = b * p.out_stride + ((long long)head * p.group + h0 + h) * D + 4 * c4;
+                uint2 v;
+                if constexpr (BF) v = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
+                else {
+                    const __half2 lo = __floats2half2_rn(sum.x * inv, sum.y * inv), hi = __floats2half2_rn(sum.z * inv, sum.w * inv);
+                    v = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+                }
+                *reinterpret_cast<uint2 *>(p.out + at * 2) = v;
+            }
         }
+        __syncthreads();
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    if (tid < D) {
-        const long long at = b * p.out_stride + (long long)qh * D + tid;
-        if constexpr (BF) reinterpret_cast<uint16_t *>(p.out)[at] = f32_to_bf16_bits(sum * inv);
-        else reinterpret_cast<__half *>(p.out)[at] = __float2half_rn(sum * inv);
-    }
-    if (p.lse && tid == 0) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -570,7 +618,7 @@ PrefixScratch carve(char *at, int batch, int n_q, int d, long long part_rows, si
     s.head = (PrefixHead *)take(sizeof(PrefixHead));
     s.plan = (PrefixPlan *)take(sizeof(PrefixPlan) * batch);
     s.ml = (float2 *)take(8 * part_rows);
-    s.o = (float *)take(4 * part_rows * d);
+    s.o = (float4 *)take(4 * part_rows * d);
     s.tail_lse = (float *)take(4ll * batch * n_q);
     s.tail = (float *)take(4ll * batch * n_q * d);
     if (bytes) *bytes = used;
@@ -588,17 +636,27 @@ bool make_pool_map(CUtensorMap *map, const nnc_paged_kv &c, const void *pool, in
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF> cudaError_t launch_prefix_of(const LaunchCtx &lc, const CUtensorMap &mk, const CUtensorMap &mv, const PrefixParams &p) {
+// the queries: [sequence][head][element], in boxes of a tile's
+bool make_query_map(CUtensorMap *map, const void *q, bool bf, int d, int n_q, int batch, int64_t stride, int group, int per_tile) {
+    EncodeTiledFn enc = get_encode();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)n_q, (cuuint64_t)batch}, strides[2] = {(cuuint64_t)d * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t boxes[3] = {64, (cuuint32_t)group, (cuuint32_t)per_tile}, one[3] = {1, 1, 1};
+    return enc(map, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(q), dims, strides, boxes, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool BF> cudaError_t launch_prefix_of(const LaunchCtx &lc, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const PrefixParams &p) {
     static unsigned long long raised = 0;
     auto kern = attn_prefix_kernel<D, BF>;
     if (cudaError_t e = ensure_dynamic_smem(kern, Tiles<D>::kSmem, &raised); e != cudaSuccess) return e;
     const int ctas = 2 * lc.sm_count < kPrefixMaxCtas ? 2 * lc.sm_count : kPrefixMaxCtas;
-    return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)Tiles<D>::kSmem, mk, mv, p);
+    return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)Tiles<D>::kSmem, mq, mk, mv, p);
 }
 
-template <int D> cudaError_t launch_join_of(const LaunchCtx &lc, const JoinParams &p, bool bf, long long rows) {
-    return bf ? launch(lc, attn_prefix_join_kernel<D, true, false>, dim3((unsigned)rows), dim3(kJoinWarps * 32), p)
-              : launch(lc, attn_prefix_join_kernel<D, false, false>, dim3((unsigned)rows), dim3(kJoinWarps * 32), p);
+template <int D> cudaError_t launch_join_of(const LaunchCtx &lc, const JoinParams &p, bool bf, long long ctas) {
+    return bf ? launch(lc, attn_prefix_join_kernel<D, true>, dim3((unsigned)ctas), dim3(kJoinThreads), p)
+              : launch(lc, attn_prefix_join_kernel<D, false>, dim3((unsigned)ctas), dim3(kJoinThreads), p);
 }
 
 }  // namespace
@@ -612,39 +670,41 @@ size_t attn_prefix_scratch_bytes(int batch, int n_q_heads, int head_dim) {
 cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const int32_t *starts,
                                const int32_t *shared, int n_groups, void *out, float *lse, int type, int batch, int n_q_heads, int64_t q_stride,
                                int64_t out_stride, float scale, void *scratch) {
-    // fp32 and codes: every sequence's own rows, the shared ones among them
-    if (type == NNC_F32 || cache.type == NNC_E4M3)
+    // Every sequence's own rows, the shared ones among them: fp32 and codes; more query heads than a tile has rows, which share rows among
+    // themselves; queries whose rows overlap, which a tensor map does not describe.
+    if (type == NNC_F32 || cache.type == NNC_E4M3 || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim))
         return launch_attn_paged(lc, q, cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, 0, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     const int d = cache.head_dim, group = n_q_heads / cache.n_kv_heads;
     const bool bf = cache.type == NNC_BF16;
-    const long long rows = (long long)batch * n_q_heads;
     const PrefixScratch s = carve((char *)scratch + NNC_ATTN_PAGED_SCRATCH_BYTES, batch, n_q_heads, d, part_rows_of(batch, n_q_heads), nullptr);
     const PrefixGroups groups{starts, shared, n_groups, batch};
     PrefixParams p = {};
     p.c = paged_view(cache, lc.status);
     p.groups = groups;
     p.s = s;
-    p.q = (const char *)q; p.lens = lens; p.q_stride = q_stride;
+    p.lens = lens;
     p.part_rows = part_rows_of(batch, n_q_heads);
-    p.group = group; p.n_q = n_q_heads;
+    p.group = group; p.per_tile = kPrefixRows / group; p.n_q = n_q_heads;
     p.box = cache.page_size < kPrefixStep ? cache.page_size : kPrefixStep;
-    p.flip = scale < 0.f ? 0x80008000u : 0u;
+    p.flip = scale < 0.f ? 0x80000000u : 0u;
     p.scale_log2 = fabsf(scale) * 1.4426950408889634f;
     if (p.scale_log2 == 0.f) p.scale_log2 = 1e-45f;   // (0 times the -infinity of a masked score would be no number)
     p.wait_status = lc.status - 1;                    // the tensor-core kernels' word lies before the paged-cache kernels'
-    CUtensorMap mk, mv;
+    CUtensorMap mq, mk, mv;
+    if (!make_query_map(&mq, q, bf, d, n_q_heads, batch, batch > 1 ? q_stride : (int64_t)n_q_heads * d, group, p.per_tile)) return cudaErrorUnknown;
     if (!make_pool_map(&mk, cache, cache.k, p.box) || !make_pool_map(&mv, cache, cache.v, p.box)) return cudaErrorUnknown;
     LaunchCtx early = lc;
     early.pdl = true;
-    cudaError_t e = d == 64 ? (bf ? launch_prefix_of<64, true>(early, mk, mv, p) : launch_prefix_of<64, false>(early, mk, mv, p))
-                            : (bf ? launch_prefix_of<128, true>(early, mk, mv, p) : launch_prefix_of<128, false>(early, mk, mv, p));
+    cudaError_t e = d == 64 ? (bf ? launch_prefix_of<64, true>(early, mq, mk, mv, p) : launch_prefix_of<64, false>(early, mq, mk, mv, p))
+                            : (bf ? launch_prefix_of<128, true>(early, mq, mk, mv, p) : launch_prefix_of<128, false>(early, mq, mk, mv, p));
     if (e != cudaSuccess) return e;
     e = launch_attn_tail(lc, q, cache, lens, groups, s.tail, s.tail_lse, type, n_q_heads, q_stride, scale, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     if (e != cudaSuccess) return e;
     JoinParams j = {};
     j.c = p.c; j.groups = groups; j.s = s; j.lens = lens;
-    j.out = (char *)out; j.lse = lse; j.out_stride = out_stride; j.part_rows = p.part_rows; j.group = group; j.n_q = n_q_heads;
-    return d == 64 ? launch_join_of<64>(early, j, bf, rows) : launch_join_of<128>(early, j, bf, rows);
+    j.out = (char *)out; j.lse = lse; j.out_stride = out_stride; j.part_rows = p.part_rows; j.group = group; j.per_tile = p.per_tile; j.n_q = n_q_heads;
+    const long long ctas = (long long)batch * cache.n_kv_heads;
+    return d == 64 ? launch_join_of<64>(early, j, bf, ctas) : launch_join_of<128>(early, j, bf, ctas);
 }
 
 }  // namespace nnc

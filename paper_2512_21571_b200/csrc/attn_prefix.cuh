@@ -4,7 +4,7 @@
 
 namespace nnc {
 
-constexpr int kPrefixRows = 128;       // query rows of a tile: (sequence of the group, query head of the KV head)
+constexpr int kPrefixRows = 128;       // query rows of a tile, at most: as many sequences' as fit, all query heads of the KV head each
 constexpr int kPrefixStep = 64;        // positions of a step
 constexpr int kPrefixFixed = 2;        // places in the list for what it costs to begin and to end a tile, in steps
 constexpr int kPrefixMaxCtas = 320;
@@ -17,7 +17,7 @@ struct PrefixGroups {
 // where a group's tiles stand in the list
 struct PrefixPlan {
     long long base;                    // first place
-    int b0, rows, tiles, steps;        // first sequence, query rows and tiles per KV head, steps of a tile (0: no prefix)
+    int b0, members, tiles, steps;     // first sequence, sequences, tiles per KV head, steps of a tile (0: no prefix)
     int prefix, unused;                // positions
 };
 struct PrefixHead {
@@ -30,6 +30,10 @@ __device__ __forceinline__ int prefix_of(const PagedView &c, const PrefixGroups 
     return min(max(s.shared[g], 0), c.pages_per_seq << c.page_shift) >> c.page_shift << c.page_shift;
 }
 
+// A sequence that ends inside its group's prefix reads its own rows alone: so every query that meets the shared rows attends to all of
+// them, and nothing behind a sequence's end is multiplied by its weights of 0 (which makes NaN of infinities).
+__device__ __forceinline__ bool takes_prefix(int prefix, int len) { return len >= prefix; }
+
 // the group of a sequence, or -1 (whatever `starts` holds, the answer lies in range)
 __device__ __forceinline__ int group_of(const PrefixGroups &s, int b) {
     int lo = -1, hi = s.n_groups;      // starts[lo] <= b < starts[hi], where these exist
@@ -41,13 +45,13 @@ __device__ __forceinline__ int group_of(const PrefixGroups &s, int b) {
     return lo >= 0 && b < s.starts[lo + 1] ? lo : -1;
 }
 
-__device__ __forceinline__ PrefixPlan plan_of(const PagedView &c, const PrefixGroups &s, int g, int group) {
+__device__ __forceinline__ PrefixPlan plan_of(const PagedView &c, const PrefixGroups &s, int g, int per_tile) {   // per_tile: sequences
     PrefixPlan p;
     p.b0 = min(max(s.starts[g], 0), s.batch);
-    p.rows = max(min(max(s.starts[g + 1], 0), s.batch) - p.b0, 0) * group;
-    p.tiles = (p.rows + kPrefixRows - 1) / kPrefixRows;
+    p.members = max(min(max(s.starts[g + 1], 0), s.batch) - p.b0, 0);
+    p.tiles = (p.members + per_tile - 1) / per_tile;
     p.prefix = prefix_of(c, s, g);
-    p.steps = p.rows ? (p.prefix + kPrefixStep - 1) / kPrefixStep : 0;
+    p.steps = p.members ? (p.prefix + kPrefixStep - 1) / kPrefixStep : 0;
     p.base = 0;
     p.unused = 0;
     return p;
@@ -62,7 +66,7 @@ struct PrefixScratch {
     PrefixHead *head;
     PrefixPlan *plan;                  // [n_groups]
     float2 *ml;                        // [rows]: reference in log2 units, sum
-    float *o;                          // [rows][D]
+    float4 *o;                         // [D / 4][rows]: neighbouring threads hold neighbouring rows
     float *tail_lse, *tail;            // [batch][n_q] and [batch][n_q][D]: what lies behind the prefix
 };
 

@@ -12,7 +12,7 @@ struct TailRows {
     template <int TILE> static __device__ __forceinline__ Reach reach(const PagedAttnParams &p, int b, int) {
         const PrefixGroups groups{p.starts, p.shared, p.n_groups, p.batch};
         const int len = length_of(p, p.lens[b]), g = group_of(groups, b);
-        const int start = g < 0 ? 0 : prefix_of(p.c, groups, g);
+        const int prefix = g < 0 ? 0 : prefix_of(p.c, groups, g), start = takes_prefix(prefix, p.lens[b]) ? prefix : 0;
         return start < len ? reach_between<TILE>(start, len) : Reach{len, len, 0, len};
     }
     static __device__ __forceinline__ int page(const PagedAttnParams &p, const Place &at, int pos, int &) {

@@ -187,6 +187,31 @@ def test_infinite_keys_and_values(nnc, kv):
         assert (ls[0].double() - torch.logsumexp(torch.einsum("gd,nd->gn", q[b].double(), kk[0]) / 8, -1)).abs()[rows].max() < 2.0 ** -16
 
 
+@pytest.mark.parametrize("kv", [BF16, F16], ids=str)
+def test_shared_rows_behind_a_sequence_s_end_do_not_reach_it(nnc, kv):
+    """NaN and infinities in shared rows past a shorter sequence's length, in one CTA's share and in several."""
+    for shared, lens_of in ((128, [140, 40, 127, 0, 128]), (8192, [8200, 8191, 70])):
+        cache, lens, starts, groups, held = _grouped(nnc, kv, [(shared, lens_of)], 16, 2, 64, 2)
+        last = cache.page_table[0, shared // 16 - 1].long()
+        cache.v[last, :, 15, 3], cache.v[last, :, 15, 4], cache.k[last, :, 15, 0] = math.inf, math.nan, math.nan
+        q = _randn(_gen(4), len(lens), 6, 64, dtype=kv)
+        out, lse = nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(groups), want_lse=True)
+        short = [b for b, n in enumerate(lens) if n < shared]
+        _check_attention(out[short], lse[short], q[short], [[t[b] for b in short] for t in held], [lens[b] for b in short], 0.125, 0, kv)
+        assert out[[b for b in range(len(lens)) if b not in short]].isnan().all()
+
+
+def test_query_rows_that_overlap_and_groups_of_many_heads(nnc):
+    cache, lens, starts, shared, held = _grouped(nnc, BF16, [(64, [70, 64, 80])], 16, 2, 64, 2)
+    one = _randn(_gen(2), 1, 4, 64, dtype=BF16)
+    out, lse = nnc.op_attn_prefix_paged(one.expand(3, 4, 64), cache, _ints(lens), _ints(starts), _ints(shared), want_lse=True)
+    _check_attention(out, lse, one.expand(3, 4, 64), held, lens, 0.125, 0, BF16)
+    for group in (127, 128, 129):
+        q = _randn(_gen(3), 3, 2 * group, 64, dtype=BF16)
+        out, lse = nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(shared), want_lse=True)
+        _check_attention(out, lse, q, held, lens, 0.125, 0, BF16)
+
+
 def test_pages_lengths_and_groups_out_of_range(nnc):
     cache, lens, starts, shared, held = _grouped(nnc, BF16, [(96, [100, 99]), (48, [60, 50])], 16, 2, 64, 2)
     q = _randn(_gen(2), 4, 4, 64, dtype=BF16)
