@@ -12,8 +12,11 @@
 // fills one tile, by the exponentials where it fills several.
 //   - The list of (group, KV head, tile, step of 64 positions) is cut into one contiguous share per CTA; the groups' lengths live on the
 //     device, so every CTA adds up the list itself.  A share may begin and end inside a tile.
-//   - Two CTAs of 192 threads per SM: TMA producer, MMA issuer, four softmax warps with a query row per thread, as in attn_prefill_f16.cu:
-//     two score buffers, so that the products of the next step run while the softmax works on this one.
+//   - One CTA of 384 threads per SM: a warp that fetches K (and Q), one that fetches V, one that issues S = Q K^T, one that issues O += P V (a
+//     single warp's instructions for two of these take longer than the step), and two teams of four softmax warps with a query row per thread, which take turns
+//     at the steps.  Four score buffers in tensor memory, so that scores run two steps ahead (with two, a step's scores wait for the product of
+//     the step before it).  Each team has an output accumulator and a running maximum of its own; they are joined where a share's part of a
+//     tile ends.
 //   - Queries enter exactly.  Probabilities are two terms of the cache's type (bf16: 16 bits, fp16: 22), written over the scores they
 //     come from: one bf16 term alone would add an error of the size of the result's own rounding.  fp32 queries and results would need three
 //     terms and shorter sums; they go through the kernel that reads every sequence's rows.
@@ -26,16 +29,22 @@ namespace nnc {
 
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kThreads = 384, kSoftmaxThreads = 256;
 constexpr int kSoftmaxRows = 128;
-constexpr uint32_t kColS = 0, kColO = 128, kTmemColumns = 256;   // score buffers at columns 0 and 64
+constexpr int kScoreBuffers = 4;
+constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then two accumulators of 128 columns
 constexpr float kLn2 = 0.69314718055994530942f;
 
 template <int D> struct Tiles {
     static constexpr int kHalves = D / 64;                        // slabs of 64 elements
     static constexpr int kQSlab = kPrefixRows * 128, kQ = kHalves * kQSlab;
     static constexpr int kSlabKV = kPrefixStep * 128, kKV = kHalves * kSlabKV;
-    static constexpr int kSmem = kQ + 4 * kKV + 1024 /*alignment*/ + 128 /*barriers*/;
+    // of K and of V.  At most kScoreBuffers: the producer takes a stage as free by the barriers of its step's score buffer, which then cannot move on
+    // by more than one phase before it has looked
+    static constexpr int kStages = 4;
+    static_assert(kStages <= kScoreBuffers, "");
+    static constexpr int kBars = kQ + 2 * kStages * kKV;
+    static constexpr int kSmem = kBars + 1024 /*alignment*/ + 256 /*barriers*/;   // more than half of an SM's: one CTA there
 };
 
 struct PrefixParams {
@@ -77,6 +86,13 @@ __device__ __forceinline__ void advance(const PrefixParams &p, Step &at) {
     find_group(p, at);
 }
 
+__device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+
 // two floats to nearest even, the first in the low half: one instruction
 __device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
     uint32_t r;
@@ -94,11 +110,26 @@ __device__ __forceinline__ float top3(float a, float b, float c) {
     return d;
 }
 
+// The products are issued by warp-wide code in which one lane's instruction counts: what they address then lies in uniform registers.  (Inside a
+// branch that one lane takes, every operand is moved there first: 85 to 115 cycles an instruction instead of .. .)
+__device__ __forceinline__ void mma_ss(bool one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)one) : "memory");
+}
+__device__ __forceinline__ void mma_ts(bool one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {   // the first operand in tensor memory
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)one) : "memory");
+}
+__device__ __forceinline__ void mma_commit(bool one, uint32_t bar) {
+    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"((uint32_t)one) : "memory");
+}
+
 // BF: bf16 caches, otherwise fp16; queries are of the cache's type
 template <int D, bool BF>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 1)
 attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PrefixParams p) {
     typedef Tiles<D> T;
+    constexpr int NS = T::kStages;
     // fp16 probabilities are scaled by 2^6, so that small ones keep their bits (at most 2^8 by the lazy maximum: below 2^15; sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 6.f;
     extern __shared__ uint8_t smem_raw[];
@@ -106,25 +137,25 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t q_tile = base;
     auto k_tile = [&](int st) { return base + (uint32_t)(T::kQ + st * 2 * T::kKV); };
     auto v_tile = [&](int st) { return k_tile(st) + (uint32_t)T::kKV; };
-    const uint32_t bars = base + (uint32_t)(T::kQ + 4 * T::kKV);
-    const uint32_t q_ready = bars;
-    auto k_full = [&](int st) { return bars + 8u * (1 + st); };
-    auto v_full = [&](int st) { return bars + 8u * (3 + st); };
-    auto s_full = [&](int st) { return bars + 8u * (5 + st); };
-    auto p_full = [&](int st) { return bars + 8u * (7 + st); };
-    auto pv_done = [&](int st) { return bars + 8u * (9 + st); };
+    const uint32_t q_ready = base + (uint32_t)T::kBars;
+    auto k_full = [&](int st) { return q_ready + 8u * (1 + st); };
+    auto v_full = [&](int st) { return q_ready + 8u * (1 + NS + st); };
+    auto s_full = [&](int j) { return q_ready + 8u * (1 + 2 * NS + j % kScoreBuffers); };                           // by step
+    auto p_full = [&](int j) { return q_ready + 8u * (1 + 2 * NS + kScoreBuffers + j % kScoreBuffers); };
+    auto pv_done = [&](int j) { return q_ready + 8u * (1 + 2 * NS + 2 * kScoreBuffers + j % kScoreBuffers); };
+    auto turn = [&](int j) { return (uint32_t)(j / kScoreBuffers & 1); };                                            // their parity
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s, first_g;
     __shared__ long long first_rest, sums[kThreads / 32];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    __shared__ float2 ml_s[2][kPrefixRows];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     volatile int *abort_flag = &abort_s;
     if (tid == 0) {
         abort_s = 0;
         mbar_init(q_ready, 1);
-        for (int st = 0; st < 2; ++st) {
-            mbar_init(k_full(st), 1); mbar_init(v_full(st), 1); mbar_init(s_full(st), 1);
-            mbar_init(p_full(st), kSoftmaxRows); mbar_init(pv_done(st), 1);
-        }
+        for (int st = 0; st < NS; ++st) { mbar_init(k_full(st), 1); mbar_init(v_full(st), 1); }
+        for (int j = 0; j < kScoreBuffers; ++j) { mbar_init(s_full(j), 1); mbar_init(p_full(j), kSoftmaxRows); mbar_init(pv_done(j), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -154,8 +185,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     before += incl - mine;
     const long long share = max((total + gridDim.x - 1) / gridDim.x, 1ll), cta = blockIdx.x;
     const long long t0 = cta * share, t1 = min(t0 + share, total);
-    if (cta == 0) {   // for the joining kernel
-        if (tid == 0) p.s.head->share = share;
+    if (cta == gridDim.x - 1) {   // for the joining kernel; the last share is the shortest
         long long at = before;
         for (int g = g_lo; g < g_hi; ++g) {
             PrefixPlan plan = plan_of(p.c, p.groups, g, p.per_tile);
@@ -178,7 +208,25 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         first_rest = rest;
     }
     __syncthreads();
-    const uint32_t tmem_base = tmem_base_s;
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, tmem_base_s, 0);
+    if (cta == gridDim.x - 1)
+        for (int b = tid; b < p.groups.batch; b += kThreads) {
+            PrefixOf of = {};
+            const int g = group_of(p.groups, b);
+            if (g >= 0) {
+                const PrefixPlan plan = p.s.plan[g];
+                const int nth = b - plan.b0;
+                of.per_head = plan.tiles * (plan.steps + kPrefixFixed);
+                of.first = plan.base + (long long)(nth / p.per_tile) * (plan.steps + kPrefixFixed);
+                of.rows_per_head = plan.members * p.group;
+                of.row = (long long)plan.b0 * p.n_q + (long long)nth * p.group;
+                of.steps = takes_prefix(plan.prefix, p.lens[b]) ? plan.steps : 0;
+                of.prefix = plan.prefix;
+                of.b0 = plan.b0;
+                of.share = share;
+            }
+            p.s.of[b] = of;
+        }
     Step at = {};
     at.index = t1;
     if (t0 < t1) {
@@ -198,254 +246,280 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     }
     auto more = [&]() { return at.index < t1 && at.g < p.groups.n_groups; };
 
-    if (warp == 0) {   // ---------------- TMA producer: a lane a box ----------------
-        // Lane: kind (K or V), box of the step's positions, half of the head's elements.  Rows are looked up a step before K needs them, and V
-        // takes K's.
-        const int half = lane & 1, r = (lane >> 1 & 3) * p.box;
-        const bool loads = lane < 16 && half < T::kHalves && r < kPrefixStep, is_v = lane >= 8;
+    long long all = 0;   // steps of this share
+    for (Step s = at; s.index < t1 && s.g < p.groups.n_groups;) {   // a tile's at a time
+        const long long n = min((long long)(s.plan.steps - s.step), t1 - s.index);
+        all += n;
+        s.index += n - 1;
+        s.step += (int)n - 1;
+        advance(p, s);
+    }
+    const int steps = __shfl_sync(0xffffffffu, (int)min(all, 0x7fffffffll), 0);
+
+    // how many steps this share has of the tile where `x` stands, which then moves to the next tile
+    auto part = [&](Step &x) -> int {
+        const int n = __shfl_sync(0xffffffffu, (int)min((long long)(x.plan.steps - x.step), t1 - x.index), 0);
+        x.index += n - 1;
+        x.step += n - 1;
+        advance(p, x);
+        return n;
+    };
+    auto wait = [&](uint32_t bar, uint32_t parity, int code) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.wait_status, code)); };
+
+    if (warp <= 1) {   // ---------------- TMA producers, a lane a box: keys and queries; values ----------------
+        const bool v = warp == 1;
+        const int half = lane & 1, r = (lane >> 1) * p.box;           // this lane's half of the head's elements, first position of a step
+        const bool loads = half < T::kHalves && r < kPrefixStep;
+        const uint32_t to = (v ? v_tile(0) : k_tile(0)) + (uint32_t)(half * T::kSlabKV + r * 128);
+        const CUtensorMap *const map = v ? &map_v : &map_k;
         const int absent = (int)min(paged_rows(p.c), 0x7fffffffll);   // a row outside the tensor: zeros
-        Step far = at;                                                // the step whose rows are looked up next
-        auto look = [&]() {
-            if (!(far.index < t1 && far.g < p.groups.n_groups)) return absent;
-            const int pos = far.step * kPrefixStep + r;
-            int page = -1;
-            if (loads && pos < far.plan.prefix) {
-                page = p.c.table[(long long)far.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
-                if ((unsigned)page >= (unsigned)p.c.n_pages) { page = -1; if (!is_v && half == 0) paged_complain(p.c); }
-            }
-            const long long row = page < 0 ? absent : paged_row(p.c, page, far.head, pos & ((1 << p.c.page_shift) - 1));
-            advance(p, far);
-            return NNC_BC(row >= 0 && row <= absent, 3601) ? (int)row : absent;
-        };
-        // The box of stage `st` for this kind; the other kind's lanes look on
-        auto load = [&](bool v, int st, int row) {
-            const uint32_t bar = v ? v_full(st) : k_full(st);
-            if (lane == 0) mbar_expect_tx(bar, T::kKV);
-            __syncwarp();
-            if (loads && is_v == v) tma_load_2d((v ? v_tile(st) : k_tile(st)) + half * T::kSlabKV + r * 128, v ? &map_v : &map_k, bar, 64 * half, row);
-        };
+        const int page_rows = p.c.n_kv << p.c.page_shift, page_mask = (1 << p.c.page_shift) - 1;
         auto load_queries = [&](const Step &x) {   // [sequence][query head of the KV head][64]: a row of the tile after the other
             if (lane == 0) mbar_expect_tx(q_ready, (uint32_t)(T::kHalves * p.per_tile * p.group * 128));
             __syncwarp();
             if (lane < T::kHalves) tma_load_3d(q_tile + lane * T::kQSlab, &map_q, q_ready, 64 * lane, x.head * p.group, x.plan.b0 + x.tile * p.per_tile);
         };
-        long long steps = 0;   // of this share
-        for (Step s = at; s.index < t1 && s.g < p.groups.n_groups;) {   // a tile's at a time
-            const long long n = min((long long)(s.plan.steps - s.step), t1 - s.index);
-            steps += n;
-            s.index += n - 1;
-            s.step += (int)n - 1;
-            advance(p, s);
+        Step tile_q = at;
+        int begins_q = 0;   // the step where the next tile to load the queries of begins
+        if (steps > 0 && !v) {
+            load_queries(tile_q);
+            begins_q = part(tile_q);
         }
-        // A stage's K tile is free as soon as the S of the step that read it is complete: K_{j+1} is requested when S_{j-1} is
-        // complete, V_j when O += P_{j-2} V_{j-2} is.
-        int row0 = look(), row1 = look(), row2 = absent;   // of steps j, j + 1, j + 2
-        if (steps > 0) {
-            load_queries(at);
-            load(false, 0, row0);
-        }
-        if (steps > 1) load(false, 1, row1);
-        for (long long j = 0; j < steps; ++j) {
-            const int st = (int)(j & 1);
-            row2 = look();
-            if (j >= 1) {
-                if (!__all_sync(0xffffffffu, mbar_wait(s_full(st ^ 1), (uint32_t)(((j - 1) >> 1) & 1), abort_flag, p.wait_status, 41))) break;
-                advance(p, at);
-                if (at.step == 0) load_queries(at);   // a new tile's: the last one's have been multiplied for the last time
-                if (j + 1 < steps) load(false, st ^ 1, row1);
-            }
-            if (j >= 2 && !__all_sync(0xffffffffu, mbar_wait(pv_done(st), (uint32_t)(((j - 2) >> 1) & 1), abort_flag, p.wait_status, 42))) break;
-            load(true, st, row0);
-            row0 = row1;
-            row1 = row2;
-        }
-    } else if (warp == 1) {
-        if (lane == 0) {   // ---------------- MMA issuer ----------------
-            constexpr uint32_t idesc_qk = make_idesc(kPrefixStep, !BF, false), idesc_pv = make_idesc(D, !BF, true);
-            const uint64_t dq = make_smem_desc(q_tile);
-            const uint64_t dk[2] = {make_smem_desc(k_tile(0)), make_smem_desc(k_tile(1))};
-            const uint64_t dv[2] = {make_smem_desc_mn(v_tile(0), T::kSlabKV), make_smem_desc_mn(v_tile(1), T::kSlabKV)};
-            int pieces = 0;
-            Step next = at;
-            auto issue_qk = [&](int j) -> bool {
-                const int st = j & 1, u = j >> 1;
-                if (j == 0 || next.step == 0) {   // a new tile's queries
-                    if (!mbar_wait(q_ready, (uint32_t)(pieces & 1), abort_flag, p.wait_status, 43)) return false;
-                    ++pieces;
+        // A stage is free when the product that reads it is complete: the scores of its step for K, the output's for V.  Queries are replaced when
+        // the tile's last scores are complete; so the keys' warp goes on looking until there is no tile left.
+        int left = 0, pos = 0, head_rows = 0, end = 0, page = 0;
+        const int32_t *table = p.c.table;
+        for (int j = 0, st = 0; j < steps || (!v && begins_q < steps); ++j) {
+            if (j >= NS) {
+                const int done = j - NS;
+                if (!wait(v ? pv_done(done) : s_full(done), turn(done), v ? 42 : 41)) break;
+                if (!v && done + 1 == begins_q && begins_q < steps) {
+                    load_queries(tile_q);
+                    begins_q += part(tile_q);
                 }
-                if (!mbar_wait(k_full(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 44)) return false;
-                // the score buffer holds P_{j-2} until O += P_{j-2} V_{j-2} has completed
-                if (j >= 2 && !mbar_wait(pv_done(st), (uint32_t)((u - 1) & 1), abort_flag, p.wait_status, 45)) return false;
+                if (j >= steps) continue;
+            }
+            if (left == 0) {   // this share's part of another tile
+                table = p.c.table + (long long)at.plan.b0 * p.c.pages_per_seq;
+                pos = at.step * kPrefixStep + r;
+                end = loads ? at.plan.prefix : 0;
+                head_rows = at.head << p.c.page_shift;
+                if (pos < end) page = table[pos >> p.c.page_shift];
+                left = part(at);
+            }
+            int row = absent;
+            if (pos < end) {
+                if ((unsigned)page < (unsigned)p.c.n_pages) row = page * page_rows + head_rows + (pos & page_mask);   // (the host has seen that rows are 32-bit numbers)
+                else if (!v && half == 0) paged_complain(p.c);
+            }
+            if (!NNC_BC(row >= 0 && row <= absent, 3601)) row = absent;
+            const uint32_t bar = v ? v_full(st) : k_full(st);
+            if (lane == 0) mbar_expect_tx(bar, T::kKV);
+            __syncwarp();
+            if (loads) tma_load_2d(to + (uint32_t)(st * 2 * T::kKV), map, bar, 64 * half, row);
+            pos += kPrefixStep;
+            --left;
+            if (left > 0 && pos < end) page = table[pos >> p.c.page_shift];   // on its way while this warp waits for the next stage
+            if (++st == NS) st = 0;
+        }
+    } else if (warp <= 3) {   // ---------------- MMA issuers: scores; outputs ----------------
+        const bool one = lane == 0;
+        auto stage = [&](uint64_t desc, int st) { return desc + (uint64_t)((st * 2 * T::kKV) >> 4); };
+        int st = 0, turn_st = 0;
+        if (warp == 2) {
+            constexpr uint32_t idesc = make_idesc(kPrefixStep, !BF, false);
+            const uint64_t dq = make_smem_desc(q_tile), dk = make_smem_desc(k_tile(0));
+            for (int j = 0, left = 0, tiles = 0; j < steps; ++j) {
+                if (left == 0) {   // a new tile's queries
+                    left = part(at);
+                    if (!wait(q_ready, (uint32_t)(tiles & 1), 43)) break;
+                    ++tiles;
+                }
+                --left;
+                if (!wait(k_full(st), (uint32_t)turn_st, 44)) break;
+                // the score buffer holds the probabilities of the step that had it before until their product is complete
+                if (j >= kScoreBuffers && !wait(pv_done(j), turn(j) ^ 1u, 45)) break;
                 tc_fence_after();
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)     // 16 elements per instruction
-                    umma_bf16(tmem_base + kColS + (uint32_t)st * kPrefixStep, dq + (uint64_t)(((ks >> 2) * T::kQSlab + (ks & 3) * 32) >> 4),
-                              dk[st] + (uint64_t)(((ks >> 2) * T::kSlabKV + (ks & 3) * 32) >> 4), idesc_qk, ks != 0);
-                umma_commit(s_full(st));
-                advance(p, next);
-                return true;
-            };
-            auto more_qk = [&]() { return next.index < t1 && next.g < p.groups.n_groups; };
-            bool ok = !more() || issue_qk(0);
-            bool begins = true;
-            for (int j = 0; ok && more(); ++j) {
-                const bool early = next.step != 0;   // a tile's first product waits for its queries: behind the last product of the tile before it
-                if (early && more_qk() && !issue_qk(j + 1)) break;
-                const int st = j & 1, u = j >> 1;
-                if (!mbar_wait(p_full(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 46)) break;
-                if (!mbar_wait(v_full(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 47)) break;
+                    mma_ss(one, tmem_base + kColS + (uint32_t)(j % kScoreBuffers * kPrefixStep), dq + (uint64_t)(((ks >> 2) * T::kQSlab + (ks & 3) * 32) >> 4),
+                           stage(dk, st) + (uint64_t)(((ks >> 2) * T::kSlabKV + (ks & 3) * 32) >> 4), idesc, ks != 0);
+                mma_commit(one, s_full(j));
+                if (++st == NS) { st = 0; turn_st ^= 1; }
+            }
+        } else {
+            constexpr uint32_t idesc = make_idesc(D, !BF, true);
+            const uint64_t dv = make_smem_desc_mn(v_tile(0), T::kSlabKV);
+            for (int j = 0, left = 0, nth = 0; j < steps; ++j) {
+                if (left == 0) { left = part(at); nth = 0; }
+                const bool begins = nth < 2;   // the accumulator of this step's team is empty
+                --left;
+                ++nth;
+                if (!wait(v_full(st), (uint32_t)turn_st, 47)) break;
+                if (!wait(p_full(j), turn(j), 46)) break;
                 tc_fence_after();
-                const uint32_t pa = tmem_base + kColS + (uint32_t)st * kPrefixStep;   // two positions per column: first terms, then second ones
+                const uint32_t pa = tmem_base + kColS + (uint32_t)(j % kScoreBuffers * kPrefixStep);   // two positions per column: first terms, then second ones
 #pragma unroll
                 for (int term = 0; term < 2; ++term)
 #pragma unroll
                     for (int ks = 0; ks < kPrefixStep / 16; ++ks)
-                        umma_bf16_ts(tmem_base + kColO, pa + (uint32_t)(term * 32 + ks * 8), dv[st] + (uint64_t)(ks * (2048 >> 4)), idesc_pv,
-                                     !begins || term != 0 || ks != 0);
-                umma_commit(pv_done(st));
-                begins = at.step + 1 == at.plan.steps;
-                advance(p, at);
-                if (!early && more_qk() && !issue_qk(j + 1)) break;
+                        mma_ts(one, tmem_base + kColO + (uint32_t)(j & 1) * 128u, pa + (uint32_t)(term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
+                               !begins || term != 0 || ks != 0);
+                mma_commit(one, pv_done(j));
+                if (++st == NS) { st = 0; turn_st ^= 1; }
             }
         }
     } else {   // ---------------- softmax: a query row per thread ----------------
-        const int quarter = warp & 3, r = quarter * 32 + lane;   // the quarter of tensor memory's lanes that this warp may touch
-        const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, to = tmem_base + lane_addr + kColO;
-        bool ok = true, begins = true;
-        long long out_row = -1;                                  // among the results
-        bool idle = false;                                       // no query of this warp counts
-        float m_used = -INFINITY, l = 0.f;
-        auto begin_tile = [&]() {
-            const int member = r / p.group, nth = at.tile * p.per_tile + member;
+        const int team = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;   // quarter: of tensor memory's lanes, which this warp may touch
+        const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, to = tmem_base + lane_addr + kColO + (uint32_t)team * 128u;
+        const int member = r / p.group, head_row = r - member * p.group;
+        bool ok = true;
+        // Where a wait gave up, a warp still comes to the barriers below, once for every part of a tile, so that no other waits there for it
+        for (int j0 = 0; j0 < steps;) {
+            const int n = (int)min((long long)(at.plan.steps - at.step), t1 - at.index), s0 = at.step;   // this share's part of a tile: steps j0 .. j0 + n - 1
+            const int nth = at.tile * p.per_tile + member;
             const bool valid = member < p.per_tile && nth < at.plan.members && takes_prefix(at.plan.prefix, p.lens[at.plan.b0 + nth]);
-            out_row = valid ? (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + (r - member * p.group) + kPrefixRows * cta : -1;
-            idle = !__any_sync(0xffffffffu, valid);
-        };
-        // pages that the pool does not have: a lane's 16 positions of a step, looked up a step ahead
-        auto has_page = [&](const Step &x) {
-            const int pos = x.step * kPrefixStep + 16 * (lane & 3);
-            return pos >= x.plan.prefix || (unsigned)p.c.table[(long long)x.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)] < (unsigned)p.c.n_pages;
-        };
-        bool has = true;
-        if (more()) {
-            has = has_page(at);
-            begin_tile();
-        }
-        for (int j = 0; more(); ++j) {
-            const int st = j & 1, u = j >> 1, p0 = at.step * kPrefixStep;
-            ok = __all_sync(0xffffffffu, mbar_wait(s_full(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 48));
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t there = __ballot_sync(0xffffffffu, has) & 0xfu;   // per 16 positions
-            Step next = at;
-            advance(p, next);
-            const bool last = next.index >= t1 || next.g >= p.groups.n_groups, ends = at.step + 1 == at.plan.steps;
-            if (!last) has = has_page(next);
-            if (idle) {   // (its rows of P are whatever the scores' bits are, and nobody's)
-                mbar_arrive(p_full(st));
-                at = next;
-                if (ends && !last) begin_tile();
-                continue;
-            }
-            const uint32_t ts = tmem_base + lane_addr + kColS + (uint32_t)st * kPrefixStep;
-            uint32_t sv[2][32];
-            tmem_ld32_nowait(ts, sv[0]);
-            tmem_ld32_nowait(ts + 32u, sv[1]);
-            tmem_wait_ld();
-            if (p.flip) {
+            const bool idle = !__any_sync(0xffffffffu, valid);   // no query of this warp counts
+            // pages that the pool does not have: a lane's 16 positions of a step, looked up a step ahead
+            auto has_page = [&](int i) {
+                const int pos = (s0 + i) * kPrefixStep + 16 * (lane & 3);
+                return i >= n || pos >= at.plan.prefix || (unsigned)p.c.table[(long long)at.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)] < (unsigned)p.c.n_pages;
+            };
+            const int first = (j0 ^ team) & 1;   // this team's first step
+            bool has = has_page(first);
+            float m_used = -INFINITY, l = 0.f, ref = 0.f;
+            // The first time once without effect, while rows and queries are on their way, on the empty accumulator instead of scores: fetching the
+            // instructions of a step takes longer than the step
+            for (int i = j0 == 0 ? first - 2 : first; ok && i < n; i += 2) {
+                const int j = j0 + i, p0 = (s0 + i) * kPrefixStep;
+                const bool dry = i < first;
+                if (!dry) ok = __all_sync(0xffffffffu, mbar_wait(s_full(j), turn(j), abort_flag, p.wait_status, 48));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t there = __ballot_sync(0xffffffffu, has) & 0xfu;   // per 16 positions
+                if (!dry) has = has_page(i + 2);
+                if (idle) {   // (its rows of P are whatever the scores' bits are, and nobody's)
+                    if (!dry) mbar_arrive(p_full(j));
+                    continue;
+                }
+                const uint32_t ts = dry ? to : tmem_base + lane_addr + kColS + (uint32_t)(j % kScoreBuffers * kPrefixStep);
+                uint32_t sv[2][32];
+                tmem_ld32_nowait(ts, sv[0]);
+                tmem_ld32_nowait(ts + 32u, sv[1]);
+                tmem_wait_ld();
+                if (p.flip) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) { sv[0][e] ^= p.flip; sv[1][e] ^= p.flip; }
-            }
-            if (p0 + kPrefixStep > at.plan.prefix || there != 0xfu) {
+                    for (int e = 0; e < 32; ++e) { sv[0][e] ^= p.flip; sv[1][e] ^= p.flip; }
+                }
+                if (p0 + kPrefixStep > at.plan.prefix || there != 0xfu) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (p0 + 32 * c + e >= at.plan.prefix || !(there >> (2 * c + e / 16) & 1u)) sv[c][e] = 0xff800000u;   // -infinity
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (p0 + 32 * c + e >= at.plan.prefix || !(there >> (2 * c + e / 16) & 1u)) sv[c][e] = 0xff800000u;   // -infinity
-            }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    for (int e = 0; e < 32; e += 8)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 32; e += 8)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx[i] = top3(mx[i], __uint_as_float(sv[c][e + 2 * i]), __uint_as_float(sv[c][e + 2 * i + 1]));
-            const float m_step = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-            if (begins) {
-                m_used = m_step;
-            } else {
-                // the maximum that O refers to moves only when a step passes it by 2^8
-                const bool need = out_row >= 0 && m_step > m_used + kLazyMax;
-                if (__any_sync(0xffffffffu, need)) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(pv_done((j - 1) & 1), (uint32_t)(((j - 1) >> 1) & 1), abort_flag, p.wait_status, 49));
-                    if (!ok) break;
-                    tc_fence_after();
-                    const float m_new = need ? m_step : m_used;
-                    const float alpha = need ? ex2_approx(m_used - m_new) : 1.f;
+                        for (int x = 0; x < 4; ++x) mx[x] = top3(mx[x], __uint_as_float(sv[c][e + 2 * x]), __uint_as_float(sv[c][e + 2 * x + 1]));
+                const float m_step = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+                if (i <= first) {
+                    m_used = m_step;
+                    l = 0.f;
+                } else {
+                    // the maximum that O refers to moves only when a step passes it by 2^8
+                    const bool need = valid && m_step > m_used + kLazyMax;
+                    if (__any_sync(0xffffffffu, need)) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(pv_done(j - 2), turn(j - 2), abort_flag, p.wait_status, 49));
+                        if (!ok) break;
+                        tc_fence_after();
+                        const float m_new = need ? m_step : m_used;
+                        const float alpha = need ? ex2_approx(m_used - m_new) : 1.f;
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t t[32];
-                        tmem_ld32(to + 32u * c, t);
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t t[32];
+                            tmem_ld32(to + 32u * c, t);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) t[e] = __float_as_uint(__uint_as_float(t[e]) * alpha);
-                        tmem_st32(to + 32u * c, t);
-                    }
-                    tmem_wait_st();
-                    l *= alpha;
-                    m_used = m_new;
-                }
-            }
-            const float ref = (m_used == -INFINITY ? 0.f : m_used) - kLift;   // nothing attended so far: every weight is 0
-            const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), neg = make_float2(-ref, -ref);
-            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t hi[16], lo[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv[c][2 * e]), __uint_as_float(sv[c][2 * e + 1])), scale2, neg);
-                    const float2 w = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                    sum[e & 1] = __fadd2_rn(sum[e & 1], w);
-                    if constexpr (BF) {
-                        hi[e] = round_bf16x2(w.x, w.y);
-                        lo[e] = round_bf16x2(w.x - bf16_lo(hi[e]), w.y - bf16_hi(hi[e]));
-                    } else {
-                        const __half2 a = __floats2half2_rn(w.x, w.y);
-                        const float2 f = __half22float2(a);
-                        const __half2 b = __floats2half2_rn(w.x - f.x, w.y - f.y);
-                        hi[e] = *reinterpret_cast<const uint32_t *>(&a);
-                        lo[e] = *reinterpret_cast<const uint32_t *>(&b);
+                            for (int e = 0; e < 32; ++e) t[e] = __float_as_uint(__uint_as_float(t[e]) * alpha);
+                            tmem_st32(to + 32u * c, t);
+                        }
+                        tmem_wait_st();
+                        l *= alpha;
+                        m_used = m_new;
                     }
                 }
-                tmem_st16(ts + 16u * c, hi);
-                tmem_st16(ts + 32u + 16u * c, lo);
-            }
-            l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-            tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive(p_full(st));
-            at = next;
-            begins = ends;
-            if (!ends && !last) continue;
-            // ---- the share's part of a tile is done ----
-            const long long row = out_row;
-            if (!last) begin_tile();
-            ok = __all_sync(0xffffffffu, mbar_wait(pv_done(st), (uint32_t)(u & 1), abort_flag, p.wait_status, 50));
-            if (!ok) break;
-            tc_fence_after();
-            const bool store = row >= 0 && NNC_BC(row < p.part_rows, 3602);
-            if (store) p.s.ml[row] = make_float2(m_used == -INFINITY && l == 0.f ? -INFINITY : ref, l);
-#pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t t[32];
-                tmem_ld32(to + 32u * c, t);
-                if (!store) continue;
+                ref = (m_used == -INFINITY ? 0.f : m_used) - kLift;   // nothing attended so far: every weight is 0
+                const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), neg = make_float2(-ref, -ref);
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) store16(p.s.o + (8 * c + e) * p.part_rows + row, t + 4 * e);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv[c][2 * e]), __uint_as_float(sv[c][2 * e + 1])), scale2, neg);
+                        const float2 w = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        sum[e & 1] = __fadd2_rn(sum[e & 1], w);
+                        if constexpr (BF) {
+                            hi[e] = round_bf16x2(w.x, w.y);
+                            lo[e] = round_bf16x2(w.x - bf16_lo(hi[e]), w.y - bf16_hi(hi[e]));
+                        } else {
+                            const __half2 a = __floats2half2_rn(w.x, w.y);
+                            const float2 f = __half22float2(a);
+                            const __half2 b = __floats2half2_rn(w.x - f.x, w.y - f.y);
+                            hi[e] = *reinterpret_cast<const uint32_t *>(&a);
+                            lo[e] = *reinterpret_cast<const uint32_t *>(&b);
+                        }
+                    }
+                    tmem_st16(ts + 16u * c, hi);
+                    tmem_st16(ts + 32u + 16u * c, lo);
+                }
+                l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                tmem_wait_st();
+                tc_fence_before();
+                if (!dry) mbar_arrive(p_full(j));
             }
-            tc_fence_before();
-            m_used = -INFINITY;
-            l = 0.f;
+            // ---- the part is done: each team writes half of the columns of both accumulators' sum ----
+            if (first >= n) { m_used = -INFINITY; l = 0.f; }   // no step of this team's
+            ml_s[team][r] = make_float2(m_used == -INFINITY && l == 0.f ? -INFINITY : ref, l);
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+            const int last = j0 + n - 1;
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last), turn(last), abort_flag, p.wait_status, 50));
+            if (ok && n > 1) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last - 1), turn(last - 1), abort_flag, p.wait_status, 51));
+            if (ok && !idle) {
+                tc_fence_after();
+                const long long row = (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + head_row + kPrefixRows * cta;
+                const bool store = valid && NNC_BC(row < p.part_rows, 3602);
+                const float2 x = ml_s[team][r], y = ml_s[team ^ 1][r];
+                const float m = fmaxf(x.x, y.x), ref_all = m == -INFINITY ? 0.f : m;
+                const float a = exp2f(x.x - ref_all), b = exp2f(y.x - ref_all);
+                if (store && team == 0) p.s.ml[row] = make_float2(m, fmaf(a, x.y, b * y.y));
+                const bool mine = first < n, other = n > 1 || !mine;   // which of the accumulators hold anything
+                const uint32_t at_mine = to + (uint32_t)(team * (D / 2)), at_other = at_mine + (team ? -128u : 128u);
+                float4 *dst = p.s.o + (team * (D / 8)) * p.part_rows + row;
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {   // 16 columns at a time
+                    uint32_t u[16], v[16];
+                    tmem_ld16_nowait(at_mine + 16u * c, u);
+                    tmem_ld16_nowait(at_other + 16u * c, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        u[e] = __float_as_uint((mine ? a * __uint_as_float(u[e]) : 0.f) + (other ? b * __uint_as_float(v[e]) : 0.f));
+                    if (store) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store16(dst + (4 * c + e) * p.part_rows, u + 4 * e);
+                    }
+                }
+                tc_fence_before();
+            }
+            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");   // the accumulators and ml_s are free
+            j0 += n;
+            at.index += n - 1;
+            at.step += n - 1;
+            advance(p, at);
         }
     }
 
@@ -464,12 +538,10 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // ---- joining: a CTA a (sequence, KV head) -------------------------------------------------------------------------------------
 //
-// Its query heads' rows are neighbours in every piece.  A thread takes four elements of a row, of every kth piece where rows are few; the
-// weights of up to kJoinPieces pieces are computed first, by a warp a row.
+// Its query heads' rows are neighbours in every piece.  A thread takes four elements of a row of every kth piece, as a softmax of its own, and
+// those that share a row's elements are joined in shared memory: so what a CTA loads after its sequence's record depends on that alone.
 
-constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = 8;           // query heads at a time
-constexpr int kJoinPieces = kPrefixMaxCtas;
+constexpr int kJoinThreads = 512;
 
 struct JoinParams {
     PagedView c;
@@ -484,125 +556,109 @@ struct JoinParams {
 
 template <int D, bool BF>   // BF: results (and the cache) are bf16, otherwise fp16
 __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const JoinParams p) {
-    constexpr int kPieces4 = D / 4;                                // of a row
-    __shared__ float wgt[kJoinRows][kJoinPieces + 1];              // of every piece, then of the tail
-    __shared__ float2 tot[kJoinRows];                              // reference, sum
+    constexpr int kFours = D / 4, kRows = kJoinThreads / kFours;   // of a row; rows at a time
     __shared__ float4 sums[kJoinThreads];
+    __shared__ float2 mls[kJoinThreads];
     __shared__ uint32_t odd_bits[D];
     pdl_launch_dependents();
     pdl_wait();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int b = blockIdx.x / p.c.n_kv, head = blockIdx.x - b * p.c.n_kv;
-    const int g = group_of(p.groups, b);
+    const int tid = threadIdx.x, b = blockIdx.x / p.c.n_kv, head = blockIdx.x - b * p.c.n_kv;
+    const PrefixOf of = p.s.of[b];
     long long first_row = 0;
-    int n = 0, b0 = 0, prefix = 0;
-    if (g >= 0) {
-        const PrefixPlan plan = p.s.plan[g];
-        if (plan.steps && takes_prefix(plan.prefix, p.lens[b])) {
-            b0 = plan.b0;
-            prefix = plan.prefix;
-            const long long lo = plan.base + ((long long)head * plan.tiles + (b - b0) / p.per_tile) * (plan.steps + kPrefixFixed), share = p.s.head->share;
-            const long long c_lo = lo / share;
-            n = (int)((lo + plan.steps - 1) / share - c_lo) + 1;
-            first_row = (long long)b0 * p.n_q + ((long long)head * plan.members + b - b0) * p.group + kPrefixRows * c_lo;
-            if (!NNC_BC(first_row >= 0 && n <= kJoinPieces && first_row + (long long)kPrefixRows * (n - 1) + p.group <= p.part_rows, 3603)) n = 0;
-        }
+    int n = 0;
+    if (of.steps) {
+        const long long lo = of.first + (long long)head * of.per_head, c_lo = lo / of.share;
+        n = (int)((lo + of.steps - 1) / of.share - c_lo) + 1;
+        first_row = of.row + (long long)head * of.rows_per_head + kPrefixRows * c_lo;
+        if (!NNC_BC(first_row >= 0 && first_row + (long long)kPrefixRows * (n - 1) + p.group <= p.part_rows, 3603)) n = 0;
     }
-    for (int h0 = 0; h0 < p.group; h0 += kJoinRows) {
-        const int rows = min(kJoinRows, p.group - h0);
+    for (int h0 = 0; h0 < p.group; h0 += kRows) {
+        const int rows = min(kRows, p.group - h0);
         const long long q_row = (long long)b * p.n_q + (long long)head * p.group + h0;
-        if (warp < rows) {
-            const float tail = p.s.tail_lse[q_row + warp] * 1.4426950408889634f;   // the tail's sum is 1 at this reference
-            float top = tail;
-            for (int i = lane; i < n; i += 32) top = fmaxf(top, p.s.ml[first_row + h0 + warp + (long long)kPrefixRows * i].x);
-            top = warp_max(top);
-            const float ref = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
-            for (int i = lane; i < n; i += 32) {
-                const float2 ml = p.s.ml[first_row + h0 + warp + (long long)kPrefixRows * i];
-                const float w = exp2f(ml.x - ref);
-                wgt[warp][i] = w;
-                sum = fmaf(w, ml.y, sum);
+        // thread: elements c4 of row h, pieces k, k + apart, ..
+        const int items = rows * kFours, apart = kJoinThreads / items, item = tid % items, k = tid / items, h = item % rows, c4 = item / rows;
+        const bool mine = k < apart;
+        float m = -INFINITY, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](float2 ml, float4 v) {
+            if (ml.x == -INFINITY) return;
+            const float top = fmaxf(m, ml.x), a = exp2f(m - top), w = exp2f(ml.x - top);
+            m = top;
+            l = fmaf(l, a, ml.y * w);
+            o.x = fmaf(o.x, a, v.x * w); o.y = fmaf(o.y, a, v.y * w); o.z = fmaf(o.z, a, v.z * w); o.w = fmaf(o.w, a, v.w * w);
+        };
+        if (mine) {
+            const float2 *ml = p.s.ml + first_row + h0 + h;
+            const float4 *src = p.s.o + c4 * p.part_rows + first_row + h0 + h;
+            constexpr int kAhead = 4;   // pieces on their way at a time
+            float2 tail_ml = make_float2(-INFINITY, 0.f);
+            float4 tail = o;
+            if (k == 0) {
+                tail_ml = make_float2(p.s.tail_lse[q_row + h] * 1.4426950408889634f, 1.f);
+                tail = *reinterpret_cast<const float4 *>(p.s.tail + (q_row + h) * D + 4 * c4);
             }
-            sum = warp_sum(sum);
-            const float w = exp2f(tail - ref);
-            if (lane == 0) {
-                wgt[warp][n] = w;
-                tot[warp] = make_float2(ref, sum + w);
-                if (p.lse) p.lse[q_row + warp] = sum + w == 0.f ? -INFINITY : (ref + log2f(sum + w)) * kLn2;
+            for (int i0 = k; i0 < n; i0 += kAhead * apart) {
+                float2 x[kAhead];
+                float4 v[kAhead];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+                    if (i0 + a * apart < n) {
+                        x[a] = ml[(long long)kPrefixRows * (i0 + a * apart)];
+                        v[a] = src[(long long)kPrefixRows * (i0 + a * apart)];
+                    }
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+                    if (i0 + a * apart < n) add(x[a], v[a]);
+            }
+            add(tail_ml, tail);
+        }
+        if (apart > 1) {
+            sums[tid] = o;
+            mls[tid] = make_float2(m, l);
+            __syncthreads();
+            if (mine && k == 0)
+                for (int j = 1; j < apart; ++j) add(mls[item + j * items], sums[item + j * items]);
+        }
+        const bool store = mine && k == 0;
+        // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs,
+        // or NaN, leave no number); a weight of 0 made NaN of it.  So where a sum is no number the rows are looked through again.
+        if (__syncthreads_or(store && !(fabsf((o.x + o.y) + (o.z + o.w)) < INFINITY))) {
+            if (tid < D) {
+                uint32_t bits = 0;
+                const int end = n > 0 ? of.prefix : 0;
+#pragma unroll 4
+                for (int pos = 0; pos < end; ++pos) {
+                    const int page = p.c.table[(long long)of.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
+                    if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
+                    constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+                    const uint32_t x = reinterpret_cast<const uint16_t *>(p.c.v)[paged_row(p.c, page, head, pos & ((1 << p.c.page_shift) - 1)) * D + tid], size = x & 0x7fffu;
+                    if (size >= kInf) bits |= size > kInf ? 4u : x == size ? 1u : 2u;
+                }
+                odd_bits[tid] = bits;
+            }
+            __syncthreads();
+            if (store) {
+                float *const s[4] = {&o.x, &o.y, &o.z, &o.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t bits = odd_bits[4 * c4 + e];
+                    const float behind = p.s.tail[(q_row + h) * D + 4 * c4 + e];
+                    if (!(fabsf(behind) < INFINITY)) bits |= behind != behind ? 4u : behind > 0.f ? 1u : 2u;
+                    if (bits) *s[e] = bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
+                }
             }
         }
-        __syncthreads();
-        // thread: element group c4 of row h, pieces k, k + apart, ..
-        const int items = rows * kPieces4, apart = kJoinThreads / items;
-        {
-            const int item = tid % items, k = tid / items;
-            const bool mine = k < apart;
-            const int h = mine ? item % rows : 0, c4 = mine ? item / rows : 0;
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (mine) {
-                const float4 *src = p.s.o + c4 * p.part_rows + first_row + h0 + h;
-#pragma unroll 8
-                for (int i = k; i < n; i += apart) {
-                    const float w = wgt[h][i];
-                    const float4 v = src[(long long)kPrefixRows * i];
-                    sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
-                }
-                if (k == 0) {
-                    const float w = wgt[h][n];
-                    const float4 v = *reinterpret_cast<const float4 *>(p.s.tail + (q_row + h) * D + 4 * c4);
-                    sum.x = fmaf(w, v.x, sum.x); sum.y = fmaf(w, v.y, sum.y); sum.z = fmaf(w, v.z, sum.z); sum.w = fmaf(w, v.w, sum.w);
-                }
+        if (store) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const long long at = b * p.out_stride + ((long long)head * p.group + h0 + h) * D + 4 * c4;
+            uint2 v;
+            if constexpr (BF) v = make_uint2(round_bf16x2(o.x * inv, o.y * inv), round_bf16x2(o.z * inv, o.w * inv));
+            else {
+                const __half2 lo = __floats2half2_rn(o.x * inv, o.y * inv), hi = __floats2half2_rn(o.z * inv, o.w * inv);
+                v = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
             }
-            if (apart > 1) {
-                sums[tid] = sum;
-                __syncthreads();
-                if (mine && k == 0)
-                    for (int j = 1; j < apart; ++j) {
-                        const float4 v = sums[item + j * items];
-                        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-                    }
-            }
-            const bool store = mine && k == 0;
-            // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs,
-            // or NaN, leave no number); a weight of 0 made NaN of it.  So where a sum is no number the rows are looked through again.
-            if (__syncthreads_or(store && !(fabsf((sum.x + sum.y) + (sum.z + sum.w)) < INFINITY))) {
-                if (tid < D) {
-                    uint32_t bits = 0;
-                    const int end = n > 0 ? prefix : 0;
-#pragma unroll 4
-                    for (int pos = 0; pos < end; ++pos) {
-                        const int page = p.c.table[(long long)b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
-                        if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
-                        constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
-                        const uint32_t x = reinterpret_cast<const uint16_t *>(p.c.v)[paged_row(p.c, page, head, pos & ((1 << p.c.page_shift) - 1)) * D + tid], size = x & 0x7fffu;
-                        if (size >= kInf) bits |= size > kInf ? 4u : x == size ? 1u : 2u;
-                    }
-                    odd_bits[tid] = bits;
-                }
-                __syncthreads();
-                if (store) {
-                    float *const s[4] = {&sum.x, &sum.y, &sum.z, &sum.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t bits = odd_bits[4 * c4 + e];
-                        const float behind = p.s.tail[(q_row + h) * D + 4 * c4 + e];
-                        if (!(fabsf(behind) < INFINITY)) bits |= behind != behind ? 4u : behind > 0.f ? 1u : 2u;
-                        if (bits) *s[e] = bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
-                    }
-                }
-            }
-            if (store) {
-                const float L = tot[h].y, inv = L == 0.f ? 0.f : 1.f / L;
-                const long long at = b * p.out_stride + ((long long)head * p.group + h0 + h) * D + 4 * c4;
-                uint2 v;
-                if constexpr (BF) v = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
-                else {
-                    const __half2 lo = __floats2half2_rn(sum.x * inv, sum.y * inv), hi = __floats2half2_rn(sum.z * inv, sum.w * inv);
-                    v = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-                }
-                *reinterpret_cast<uint2 *>(p.out + at * 2) = v;
-            }
+            *reinterpret_cast<uint2 *>(p.out + at * 2) = v;
+            if (p.lse && c4 == 0) p.lse[q_row + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
         }
         __syncthreads();
     }
@@ -615,8 +671,8 @@ PrefixScratch carve(char *at, int batch, int n_q, int d, long long part_rows, si
     size_t used = 0;
     auto take = [&](size_t n) { char *p = at + used; used += aligned(n); return p; };
     PrefixScratch s;
-    s.head = (PrefixHead *)take(sizeof(PrefixHead));
     s.plan = (PrefixPlan *)take(sizeof(PrefixPlan) * batch);
+    s.of = (PrefixOf *)take(sizeof(PrefixOf) * batch);
     s.ml = (float2 *)take(8 * part_rows);
     s.o = (float4 *)take(4 * part_rows * d);
     s.tail_lse = (float *)take(4ll * batch * n_q);
@@ -650,7 +706,7 @@ template <int D, bool BF> cudaError_t launch_prefix_of(const LaunchCtx &lc, cons
     static unsigned long long raised = 0;
     auto kern = attn_prefix_kernel<D, BF>;
     if (cudaError_t e = ensure_dynamic_smem(kern, Tiles<D>::kSmem, &raised); e != cudaSuccess) return e;
-    const int ctas = 2 * lc.sm_count < kPrefixMaxCtas ? 2 * lc.sm_count : kPrefixMaxCtas;
+    const int ctas = lc.sm_count < kPrefixMaxCtas ? lc.sm_count : kPrefixMaxCtas;
     return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)Tiles<D>::kSmem, mq, mk, mv, p);
 }
 

@@ -7,7 +7,7 @@ namespace nnc {
 constexpr int kPrefixRows = 128;       // query rows of a tile, at most: as many sequences' as fit, all query heads of the KV head each
 constexpr int kPrefixStep = 64;        // positions of a step
 constexpr int kPrefixFixed = 2;        // places in the list for what it costs to begin and to end a tile, in steps
-constexpr int kPrefixMaxCtas = 320;
+constexpr int kPrefixMaxCtas = 160;    // one per SM
 
 struct PrefixGroups {
     const int32_t *starts, *shared;
@@ -20,9 +20,12 @@ struct PrefixPlan {
     int b0, members, tiles, steps;     // first sequence, sequences, tiles per KV head, steps of a tile (0: no prefix)
     int prefix, unused;                // positions
 };
-struct PrefixHead {
+// what the joining kernel wants to know of a sequence
+struct PrefixOf {
+    long long first, row;              // first place of its tile of KV head 0, first row of its queries for KV head 0 (of CTA 0)
+    int per_head, rows_per_head;       // places and rows from one KV head to the next
+    int steps, prefix, b0, unused;     // steps 0: nothing from a prefix
     long long share;                   // places of a CTA
-    long long unused;
 };
 
 // positions of a group that its sequences share: whole pages
@@ -63,8 +66,8 @@ __device__ __forceinline__ long long places_of(const PagedView &c, const PrefixP
 // Partial results: a row for every query row of a (tile, CTA) pair that occurs.  Pairs in the list's order move on by a tile's rows or by
 // a CTA, so row (rows of earlier tiles) + 128 CTA is a pair's own.
 struct PrefixScratch {
-    PrefixHead *head;
     PrefixPlan *plan;                  // [n_groups]
+    PrefixOf *of;                      // [batch]
     float2 *ml;                        // [rows]: reference in log2 units, sum
     float4 *o;                         // [D / 4][rows]: neighbouring threads hold neighbouring rows
     float *tail_lse, *tail;            // [batch][n_q] and [batch][n_q][D]: what lies behind the prefix

@@ -332,3 +332,10 @@ def test_refusals_of_the_binding(nnc):
             refused()
         assert e.value.status == status
     assert torch.equal(call(scratch=nnc.attn_prefix_scratch(9, 4, 64)), call())      # a larger one will do
+
+
+@pytest.mark.parametrize("kv", [BF16, F16], ids=str)
+@pytest.mark.parametrize("heads,group,d,page,shared,members", [(2, 12, 64, 128, 65536, 48), (1, 128, 64, 64, 20000, 7), (4, 30, 128, 32, 9000, 25), (8, 1, 64, 16, 8192, 130)])
+def test_long_shares_of_several_tiles(nnc, kv, heads, group, d, page, shared, members):
+    """Dozens of steps a CTA, its share beginning and ending inside tiles: every ring wraps many times over."""
+    _check(nnc, kv, kv, [(shared, [shared // page * page + 1 + 3 * i for i in range(members)])], page, heads, group, d)
