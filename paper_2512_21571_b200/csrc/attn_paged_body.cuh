@@ -223,7 +223,7 @@ template <int TYPE> __device__ __forceinline__ void store_out(const PagedAttnPar
 
 // NT: groups of 8 query heads; TYPE: the queries' and (unless W wants them in 32 bits) the results'
 template <int D, int NT, int KV, int TYPE, typename W>
-__global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) attn_paged_kernel(const PagedAttnParams p) {
+__device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
     typedef Shape<D, NT, KV, TYPE> S;
     constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3;
     constexpr int OUT = W::kOutF32 ? NNC_F32 : TYPE;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
     extern __shared__ __align__(128) char smem[];
     __shared__ AttnShared sh;
     pdl_launch_dependents();
-    pdl_wait();   // lengths, tables, queries and rows may be the preceding kernel's
+    if constexpr (!W::kConcurrent) pdl_wait();   // lengths, tables, queries and rows may be the preceding kernel's
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     const int g8 = lane >> 2, t4 = lane & 3;
@@ -1002,6 +1002,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
             c0 = c_lo; apart = kJoinGroup; n = groups; final = true;
         }
     }
+}
+
+// W::kConcurrent: starts as the preceding kernel's CTAs leave, which let it start after that kernel's own predecessors had ended.  One CTA waits for
+// the whole of that kernel in the end, so that whoever waits for this one has waited for both.
+template <int D, int NT, int KV, int TYPE, typename W>
+__global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) attn_paged_kernel(const PagedAttnParams p) {
+    attn_paged_cta<D, NT, KV, TYPE, W>(p);
+    if constexpr (W::kConcurrent)
+        if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1) pdl_wait();
 }
 
 template <int D, int NT, int KV, int TYPE, typename W>

@@ -44,7 +44,8 @@ template <int D> struct Tiles {
     static constexpr int kStages = 4;
     static_assert(kStages <= kScoreBuffers, "");
     static constexpr int kBars = kQ + 2 * kStages * kKV;
-    static constexpr int kSmem = kBars + 1024 /*alignment*/ + 256 /*barriers*/;   // more than half of an SM's: one CTA there
+    // more than an SM has left beside it for a CTA of the tail, which would take turns with the softmax (171 us instead of 89 + 14)
+    static constexpr int kSmem = (kBars > 160 << 10 ? kBars : 160 << 10) + 1024 /*alignment*/ + 256 /*barriers*/;
 };
 
 struct PrefixParams {
@@ -163,8 +164,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(kTmemColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    pdl_launch_dependents();
     pdl_wait();   // groups, lengths, tables, queries and rows may be the preceding kernel's
+    pdl_launch_dependents();   // after that: the tail does not wait for this kernel, and what came before is done for it too
     // ---- the list: its length, and where this CTA's share begins ----
     const int per = (p.groups.n_groups + kThreads - 1) / kThreads, g_lo = min(tid * per, p.groups.n_groups), g_hi = min(g_lo + per, p.groups.n_groups);
     long long mine = 0;
@@ -541,7 +542,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // Its query heads' rows are neighbours in every piece.  A thread takes four elements of a row of every kth piece, as a softmax of its own, and
 // those that share a row's elements are joined in shared memory: so what a CTA loads after its sequence's record depends on that alone.
 
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 256;
 
 struct JoinParams {
     PagedView c;
@@ -590,7 +591,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
         if (mine) {
             const float2 *ml = p.s.ml + first_row + h0 + h;
             const float4 *src = p.s.o + c4 * p.part_rows + first_row + h0 + h;
-            constexpr int kAhead = 4;   // pieces on their way at a time
+            constexpr int kAhead = 8;   // pieces on their way at a time
             float2 tail_ml = make_float2(-INFINITY, 0.f);
             float4 tail = o;
             if (k == 0) {

@@ -8,7 +8,7 @@ namespace nnc {
 namespace {
 
 struct TailRows {
-    static constexpr bool kListed = false, kOutF32 = true, kTypeF32 = false;
+    static constexpr bool kListed = false, kOutF32 = true, kTypeF32 = false, kConcurrent = true;
     template <int TILE> static __device__ __forceinline__ Reach reach(const PagedAttnParams &p, int b, int) {
         const PrefixGroups groups{p.starts, p.shared, p.n_groups, p.batch};
         const int len = length_of(p, p.lens[b]), g = group_of(groups, b);
