@@ -286,10 +286,14 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const Sco
 
 // ---- selection ---------------------------------------------------------------------------------------------------------------
 //
-// A CTA a row.  Scores become whole numbers of the same order; four passes over 8 bits each find the n-th largest (a histogram, and the
-// bin that the n-th falls into), a fifth writes the indices of what is above it, and of as many of its equals as are missing, in order.
+// A CTA a row.  Scores become whole numbers of the same order, in registers (up to 8192 pages) or in shared memory.  A histogram of 2048 equal
+// parts of their range tells the part that the n-th largest lies in; that part is divided again, until all of it is wanted (scores of one
+// batch are spread well enough for one or two rounds) or its numbers are one.  Then the indices of what lies above, and of as many of the
+// equals as are missing, are written in order.  (By digits of 8 bits: 10.1 and 11.9 us for 8 rows of 4097 and 256 of 2049, as most scores have
+// the highest digit in common; bit by bit, with a vote each: 9.5 and 10.5.)
 
-constexpr int kSelectThreads = 512;
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectBins = 2048;
 
 struct SelectParams {
     const float *scores;
@@ -298,16 +302,27 @@ struct SelectParams {
     int n_kv, columns, page_shift, n, first, last, kept;   // kept: the row's numbers fit in shared memory
 };
 
+// ITEMS: numbers of a thread, in registers; 0: any number, in shared memory if p.kept, otherwise made again from the scores each time
+template <int ITEMS>
 __global__ void __launch_bounds__(kSelectThreads) select_pages_kernel(const SelectParams p) {
     extern __shared__ uint32_t row_keys[];
-    __shared__ uint32_t histogram[256];
-    __shared__ uint32_t chosen_bin, left;
-    __shared__ uint2 sums[kSelectThreads / 32];
+    constexpr int kChunks = ITEMS ? ITEMS : 16;                  // runs of kSelectThreads pages that are counted at a time
+    constexpr int kEach = (kChunks * kSelectWarps + 31) / 32;    // counts of a lane that adds them up
+    __shared__ uint32_t histogram[kSelectBins];
+    __shared__ uint2 sums[kEach * 32];                           // of a warp's pages of a run: above, equal; then of what came before
+    __shared__ uint2 all_sums;
+    __shared__ uint32_t most[kSelectWarps], least[kSelectWarps], found[3];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long row = blockIdx.x;
+    const float *const scores = p.scores + row * p.columns;
     const int len = p.lens[row / p.n_kv];
+    float early[ITEMS ? ITEMS : 1];                              // scores, on their way with the length
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        if (tid + j * kSelectThreads < p.columns) early[j] = scores[tid + j * kSelectThreads];
+    for (int i = tid; i < kSelectBins; i += kSelectThreads) histogram[i] = 0;
     const int pages = len <= 0 ? 0 : min((int)(((long long)len + (1 << p.page_shift) - 1) >> p.page_shift), p.columns);
     int32_t *const out = p.pages + row * p.n;
     const int count = min(pages, p.n);
@@ -317,69 +332,135 @@ __global__ void __launch_bounds__(kSelectThreads) select_pages_kernel(const Sele
         for (int i = tid; i < count; i += kSelectThreads) out[i] = i;
         return;
     }
-    const float *const scores = p.scores + row * p.columns;
-    auto key_of = [&](int i) -> uint32_t {
+    auto key_of = [&](int i, float score) -> uint32_t {
         if (i < p.first || i >= pages - p.last) return 0xffffffffu;
-        const float x = scores[i] + 0.f;   // (-0 is 0)
+        const float x = score + 0.f;       // (-0 is 0)
         if (x != x) return 0xfffffffeu;    // NaN: above every number
         const uint32_t u = __float_as_uint(x);
         return u & 0x80000000u ? ~u : u | 0x80000000u;
     };
-    if (p.kept)
-        for (int i = tid; i < pages; i += kSelectThreads) row_keys[i] = key_of(i);
-    auto key = [&](int i) { return p.kept ? row_keys[i] : key_of(i); };   // (a thread reads what it wrote itself)
-    uint32_t above = 0, need = p.n;   // above: the bits of the n-th largest that are known; need: how many of those that share them
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) histogram[i] = 0;
-        __syncthreads();
+    uint32_t mine[ITEMS ? ITEMS : 1], top = 0, low = 0xffffffffu;
+    auto widen = [&](uint32_t k) {   // the range of the scores; pages that are in anyway do not count
+        if (k != 0xffffffffu) { top = max(top, k); low = min(low, k); }
+    };
+    if constexpr (ITEMS > 0) {
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) {
+            const int i = tid + j * kSelectThreads;
+            mine[j] = i < pages ? key_of(i, early[j]) : 0u;      // (0 is less than any number's key)
+            if (i < pages) widen(mine[j]);
+        }
+    } else {
         for (int i = tid; i < pages; i += kSelectThreads) {
-            const uint32_t k = key(i);
-            if (shift == 24 || (k >> (shift + 8)) == (above >> (shift + 8))) atomicAdd(&histogram[k >> shift & 255u], 1u);
+            const uint32_t k = key_of(i, scores[i]);
+            if (p.kept) row_keys[i] = k;   // (a thread reads what it wrote itself)
+            widen(k);
+        }
+    }
+    auto each = [&](auto f) {   // this thread's keys; 0 for none
+        if constexpr (ITEMS > 0) {
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) f(mine[j]);
+        } else {
+            for (int i = tid; i < pages; i += kSelectThreads) f(p.kept ? row_keys[i] : key_of(i, scores[i]));
+        }
+    };
+    top = __reduce_max_sync(kAllLanes, top);
+    low = __reduce_min_sync(kAllLanes, low);
+    if (lane == 0) { most[warp] = top; least[warp] = low; }
+    __syncthreads();
+    top = __reduce_max_sync(kAllLanes, most[lane & (kSelectWarps - 1)]);
+    low = __reduce_min_sync(kAllLanes, least[lane & (kSelectWarps - 1)]);
+    // wanted: how many of the numbers in [low, low + span] (pages that are in anyway lie above: first + last <= n < pages)
+    uint32_t need = p.n - (p.first + p.last), span = top - low;
+    bool all = need == 0;            // all numbers from `low` on are wanted (with need == 0: none below the pages that are in anyway)
+    if (all) low = 0xffffffffu;
+#pragma unroll 1
+    while (!all && span > 0) {
+        const int shift = max(0, 21 - __clz(span));   // span >> shift < 2048
+        each([&](uint32_t k) {
+            if (k - low <= span && k != 0xffffffffu && k >= low) atomicAdd(&histogram[(k - low) >> shift], 1u);
+        });
+        __syncthreads();
+        // four parts a thread, the highest first
+        uint4 part = *reinterpret_cast<const uint4 *>(histogram + kSelectBins - 4 - 4 * tid);
+        const uint32_t n4[4] = {part.w, part.z, part.y, part.x}, sum = part.x + part.y + part.z + part.w;
+        uint32_t before = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(kAllLanes, before, o);
+            if (lane >= o) before += x;
+        }
+        if (lane == 31) most[warp] = before;
+        __syncthreads();
+        const uint32_t others = lane < warp ? most[lane & (kSelectWarps - 1)] : 0u;   // (warp <= 15)
+        before += __reduce_add_sync(kAllLanes, others) - sum;
+        if (before < need && need <= before + sum) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (before < need && need <= before + n4[j]) { found[0] = kSelectBins - 1 - 4 * tid - j; found[1] = need - before; found[2] = n4[j]; }
+                before += n4[j];
+            }
+        }
+        *reinterpret_cast<uint4 *>(histogram + kSelectBins - 4 - 4 * tid) = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
+        low += found[0] << shift;
+        span = (1u << shift) - 1u;
+        need = found[1];
+        all = found[2] == need;
+    }
+    // Wanted: everything above `nth`; where that is not enough, the first `need` of its equals.
+    const uint32_t nth = all ? low - 1u : low;
+    if (all) need = 0;
+    // ---- in order ----
+    uint2 done = make_uint2(0u, 0u);
+    for (int i0 = 0; i0 < pages; i0 += kChunks * kSelectThreads) {
+        uint32_t va[kChunks], ve[kChunks];
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int i = i0 + j * kSelectThreads + tid;
+            uint32_t k = 0;
+            if constexpr (ITEMS > 0) k = mine[j];
+            else if (i < pages) k = p.kept ? row_keys[i] : key_of(i, scores[i]);
+            va[j] = __ballot_sync(kAllLanes, i < pages && k > nth);
+            ve[j] = __ballot_sync(kAllLanes, i < pages && k == nth);
+            if (lane == 0) sums[j * kSelectWarps + warp] = make_uint2(__popc(va[j]), __popc(ve[j]));
         }
         __syncthreads();
-        if (warp == 0) {   // lane l holds bins 255 - 8 l .. 248 - 8 l, the highest first
-            uint32_t n[8], sum = 0;
+        if (warp == 0) {   // what comes before each: a lane adds up its own, the warp its lanes
+            uint2 s[kEach], own = make_uint2(0u, 0u);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { n[j] = histogram[255 - 8 * lane - j]; sum += n[j]; }
-            uint32_t before = sum;
+            for (int j = 0; j < kEach; ++j) {
+                s[j] = lane * kEach + j < kChunks * kSelectWarps ? sums[lane * kEach + j] : make_uint2(0u, 0u);
+                own.x += s[j].x; own.y += s[j].y;
+            }
+            uint2 x = own;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t x = __shfl_up_sync(kAllLanes, before, o);
-                if (lane >= o) before += x;
+                const uint32_t a = __shfl_up_sync(kAllLanes, x.x, o), e = __shfl_up_sync(kAllLanes, x.y, o);
+                if (lane >= o) { x.x += a; x.y += e; }
             }
-            before -= sum;
+            if (lane == 31) all_sums = make_uint2(done.x + x.x, done.y + x.y);
+            x.x += done.x - own.x; x.y += done.y - own.y;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (before < need && need <= before + n[j]) { chosen_bin = 255 - 8 * lane - j; left = need - before; }
-                before += n[j];
+            for (int j = 0; j < kEach; ++j) {
+                sums[lane * kEach + j] = x;
+                x.x += s[j].x; x.y += s[j].y;
             }
         }
         __syncthreads();
-        above |= chosen_bin << shift;
-        need = left;
-    }
-    // ---- in order: what lies above, and the first `need` of the equals ----
-    uint32_t done_above = 0, done_equal = 0;
-    for (int i0 = 0; i0 < pages; i0 += kSelectThreads) {
-        const int i = i0 + tid;
-        const uint32_t k = i < pages ? key(i) : 0u;
-        const bool is_above = i < pages && k > above, is_equal = i < pages && k == above;
-        const uint32_t va = __ballot_sync(kAllLanes, is_above), ve = __ballot_sync(kAllLanes, is_equal), before = (1u << lane) - 1u;
-        if (lane == 0) sums[warp] = make_uint2(__popc(va), __popc(ve));
-        __syncthreads();
-        uint32_t a = done_above, e = done_equal;
-        for (int w = 0; w < kSelectThreads / 32; ++w) {
-            const uint2 s = sums[w];
-            if (w < warp) { a += s.x; e += s.y; }
-            done_above += s.x; done_equal += s.y;
+        done = all_sums;
+        const uint32_t before = (1u << lane) - 1u;
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const uint2 s = sums[j * kSelectWarps + warp];
+            const uint32_t e = s.y + __popc(ve[j] & before);
+            if ((va[j] | (e < need ? ve[j] : 0u)) >> lane & 1u) {
+                const uint32_t at = s.x + __popc(va[j] & before) + min(e, need);
+                if (NNC_BC(at < (uint32_t)p.n, 3403)) out[at] = i0 + j * kSelectThreads + tid;
+            }
         }
         __syncthreads();
-        a += __popc(va & before);
-        e += __popc(ve & before);
-        if (is_above || (is_equal && e < need)) {
-            const uint32_t at = a + min(e, need);
-            if (NNC_BC(at < (uint32_t)p.n, 3403)) out[at] = i;
-        }
     }
 }
 
@@ -444,14 +525,20 @@ cudaError_t launch_select_pages(const LaunchCtx &lc, const float *scores, const 
     p.scores = scores; p.lens = lens; p.pages = pages; p.counts = counts;
     p.n_kv = n_kv; p.columns = columns; p.page_shift = __builtin_ctz((unsigned)page_size);
     p.n = n; p.first = first; p.last = last;
+    LaunchCtx early = lc;
+    early.pdl = true;
+    const dim3 grid((unsigned)((long long)batch * n_kv)), block(kSelectThreads);
+    p.kept = 1;
+    if (columns <= 2 * kSelectThreads) return launch(early, select_pages_kernel<2>, grid, block, p);
+    if (columns <= 5 * kSelectThreads) return launch(early, select_pages_kernel<5>, grid, block, p);
+    if (columns <= 9 * kSelectThreads) return launch(early, select_pages_kernel<9>, grid, block, p);
+    if (columns <= 16 * kSelectThreads) return launch(early, select_pages_kernel<16>, grid, block, p);
     p.kept = columns <= (160 << 10) / 4;
     const size_t smem = p.kept ? (size_t)columns * 4 : 0;
     static unsigned long long raised = 0;
     if (smem > 32 << 10)
-        if (cudaError_t e = ensure_dynamic_smem(select_pages_kernel, 160 << 10, &raised); e != cudaSuccess) return e;
-    LaunchCtx early = lc;
-    early.pdl = true;
-    return launch_smem(early, select_pages_kernel, dim3((unsigned)((long long)batch * n_kv)), dim3(kSelectThreads), smem, p);
+        if (cudaError_t e = ensure_dynamic_smem(select_pages_kernel<0>, 160 << 10, &raised); e != cudaSuccess) return e;
+    return launch_smem(early, select_pages_kernel<0>, grid, block, smem, p);
 }
 
 }  // namespace nnc
