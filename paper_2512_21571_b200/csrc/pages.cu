@@ -195,8 +195,12 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const Sco
         const int l = i & 31, s = i / 32 % (kSteps / 2), chunk = i / 32 / (kSteps / 2);
         const int g = chunk * 8 + (l >> 2), from = 32 * (s / 2) + 8 * (l & 3) + 4 * (s & 1);   // step s: half of the lanes' 16-byte pieces
         float x[4];
+        uint32_t minus[2] = {0u, 0u};   // all bits of negative elements, in pairs
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = query(g, from + e);
+        for (int e = 0; e < 4; ++e) {
+            x[e] = query(g, from + e);
+            if (x[e] < 0.f) minus[e / 2] |= 0xffffu << (16 * (e & 1));
+        }
         if constexpr (SCALED) {
             const float up = 1.f / undo[g];
 #pragma unroll
@@ -204,29 +208,22 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const Sco
         }
 #pragma unroll
         for (int t = 0; t < TERMS; ++t) {
-            uint32_t w[2][2];   // [negative, positive part][pair]
+            uint32_t both[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                uint32_t both;
                 if constexpr (BF) {
-                    both = pack_bf16x2(x[2 * e], x[2 * e + 1]);
-                    x[2 * e] -= bf16_lo(both); x[2 * e + 1] -= bf16_hi(both);
+                    both[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
+                    x[2 * e] -= bf16_lo(both[e]); x[2 * e + 1] -= bf16_hi(both[e]);
                 } else {
                     const __half2 h = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
-                    both = *reinterpret_cast<const uint32_t *>(&h);
+                    both[e] = *reinterpret_cast<const uint32_t *>(&h);
                     x[2 * e] -= __low2float(h); x[2 * e + 1] -= __high2float(h);
                 }
-                w[0][e] = w[1][e] = both;
             }
             // the sign of the query itself, not of a term, says which bound it meets
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t half = 0xffffu << (16 * (e & 1));
-                w[query(g, from + e) < 0.f ? 1 : 0][e / 2] &= ~half;
-            }
             uint2 *dst = operand + ((chunk * TERMS + t) * kSteps + s) * 32 + l;
-            dst[0] = make_uint2(w[0][0], w[0][1]);
-            dst[(kSteps / 2) * 32] = make_uint2(w[1][0], w[1][1]);
+            dst[0] = make_uint2(both[0] & minus[0], both[1] & minus[1]);
+            dst[(kSteps / 2) * 32] = make_uint2(both[0] & ~minus[0], both[1] & ~minus[1]);
         }
     }
     __syncthreads();
@@ -250,24 +247,30 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const Sco
             }
             float top[2] = {-INFINITY, -INFINITY};
             for (int chunk = 0; chunk < chunks; ++chunk) {
-                constexpr int kSums = TERMS > 1 ? 3 : 2;   // lower bounds, upper bounds, lower terms
-                float acc[kSums][4];
+                float acc[2][TERMS][4];   // lower bounds, upper bounds: a chain of products each
 #pragma unroll
-                for (int i = 0; i < kSums; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+                for (int i = 0; i < 2 * TERMS; ++i) acc[i & 1][i >> 1][0] = acc[i & 1][i >> 1][1] = acc[i & 1][i >> 1][2] = acc[i & 1][i >> 1][3] = 0.f;
                 const uint2 *w = operand + chunk * TERMS * kSteps * 32 + lane;
 #pragma unroll
-                for (int s = 0; s < kSteps / 2; ++s)
+                for (int s = 0; s < kSteps / 4; ++s)
 #pragma unroll
-                    for (int t = 0; t < TERMS; ++t) {
-                        float (&sum)[4] = acc[t ? 2 : s < kSteps / 4 ? 0 : 1];
-                        mma_step<BF>(sum, x[0][s].x, x[1][s].x, x[0][s].y, x[1][s].y, w[(t * kSteps + 2 * s) * 32]);
-                        mma_step<BF>(sum, x[0][s].z, x[1][s].z, x[0][s].w, x[1][s].w, w[(t * kSteps + 2 * s + 1) * 32]);
-                    }
+                    for (int side = 0; side < 2; ++side)
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t) {
+                            const int load = side * (kSteps / 4) + s;
+                            mma_step<BF>(acc[side][t], x[0][load].x, x[1][load].x, x[0][load].y, x[1][load].y, w[(t * kSteps + 2 * load) * 32]);
+                            mma_step<BF>(acc[side][t], x[0][load].z, x[1][load].z, x[0][load].w, x[1][load].w, w[(t * kSteps + 2 * load + 1) * 32]);
+                        }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {   // pages g8, g8 + 8; queries 2 t4, 2 t4 + 1
                     const int g = chunk * 8 + 2 * t4 + (e & 1);
-                    float s = acc[0][e] + acc[1][e];
-                    if constexpr (TERMS > 1) s += fabsf(s) == INFINITY ? 0.f : acc[2][e];   // (an infinity is the first terms')
+                    float s = acc[0][0][e] + acc[1][0][e];
+                    if constexpr (TERMS > 1) {
+                        float rest = 0.f;
+#pragma unroll
+                        for (int t = TERMS - 1; t > 0; --t) rest += acc[0][t][e] + acc[1][t][e];
+                        s += fabsf(s) == INFINITY ? 0.f : rest;   // (an infinity is the first terms')
+                    }
                     if constexpr (SCALED) s *= undo[g];
                     if (g < p.group) top[e >> 1] = max_nan(top[e >> 1], s);
                 }
