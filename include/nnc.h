@@ -396,10 +396,13 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
  * through the page table of the group's first sequence, whole pages of them (what is left of the last page counts as each sequence's own).
  * The cache holds all of them, whatever the sequences' lengths; a shorter sequence attends to its first lens[b].  Sequences of
  * no group, and of groups with shared[g] below a page, attend to their own rows alone.  A `starts` that descends or leaves 0 .. batch
- * and a shared[g] outside 0 .. the table's reach are cut to what is allowed and set the status word.  1 <= n_groups <= batch.
- *   q, out, lens, lse, scale, strides: as there, without a window.  fp32 queries and results are computed sequence by sequence.
+ * and a shared[g] outside 0 .. the table's reach are cut to what is allowed and, where the groups are looked at, set the status word.
+ * 1 <= n_groups <= batch.
+ *   q, out, lens, lse, scale, strides: as there, without a window.  Every sequence reads its own rows, and the groups are not looked at, where that
+ *   is faster (batch * pages_per_seq * page_size small, a group for every sequence), and for fp32 queries, E4M3 caches, more than 128
+ *   query heads per KV head and queries whose rows overlap.
  * scratch: DEVICE, 256-byte aligned, nnc_attn_prefix_scratch_bytes(batch, n_q_heads, head_dim); its first NNC_ATTN_PAGED_TICKET_BYTES as
- * there.  Three launches. */
+ * there.  Up to three launches. */
 size_t nnc_attn_prefix_scratch_bytes(int32_t batch, int32_t n_q_heads, int32_t head_dim);
 int nnc_op_attn_prefix_paged(const void *q, const nnc_paged_kv *cache, const int32_t *lens, const int32_t *starts, const int32_t *shared,
                              int32_t n_groups, void *out, float *lse, int32_t type, int32_t batch, int32_t n_q_heads, int64_t q_stride,

@@ -728,8 +728,14 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
                                const int32_t *shared, int n_groups, void *out, float *lse, int type, int batch, int n_q_heads, int64_t q_stride,
                                int64_t out_stride, float scale, void *scratch) {
     // Every sequence's own rows, the shared ones among them: fp32 and codes; more query heads than a tile has rows, which share rows among
-    // themselves; queries whose rows overlap, which a tensor map does not describe.
-    if (type == NNC_F32 || cache.type == NNC_E4M3 || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim))
+    // themselves; queries whose rows overlap, which a tensor map does not describe; groups of one.  And small batches: reading all of a table's
+    // rows for each sequence, mostly from L2, goes at some 10 TB/s per eight query heads behind 9 us, three launches take 17 to 25 us.  Both
+    // sides, us (three launches first), 4 query heads of 128 and 12 of 64 per KV head: 35 MB 19 and 15, 135 MB 27.6 and 27.6, 140 MB 26.0 and
+    // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.
+    const int eights = (n_q_heads / cache.n_kv_heads + 7) / 8;
+    const double rows_bytes = 4.0 * batch * cache.pages_per_seq * cache.page_size * cache.n_kv_heads * cache.head_dim;
+    if (type == NNC_F32 || cache.type == NNC_E4M3 || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
+        n_groups == batch || rows_bytes * eights < 140e6)
         return launch_attn_paged(lc, q, cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, 0, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     const int d = cache.head_dim, group = n_q_heads / cache.n_kv_heads;
     const bool bf = cache.type == NNC_BF16;

@@ -10,7 +10,7 @@ from test_gpu_paged import BF16, E4M3, F16, F32, TYPES, _check_attention, _gen, 
 pytestmark = pytest.mark.gpu
 
 
-def _grouped(nnc, kv, groups, page, heads, d, seed, spare=2):
+def _grouped(nnc, kv, groups, page, heads, d, seed, spare=2, wide=True):
     """groups: (shared positions, lengths of its sequences).  The cache (unused rows NaN), lengths, starts, shared, and what every
     sequence's rows are, 64 bits: two lists of [heads][n][d].  All shared rows are written, whatever the lengths."""
     lens = [n for _, of in groups for n in of]
@@ -21,6 +21,8 @@ def _grouped(nnc, kv, groups, page, heads, d, seed, spare=2):
     own = [max(0, -(-n // page) - whole[g]) for g, (_, of) in enumerate(groups) for n in of]
     total = sum(whole) + sum(own) + spare
     columns = max(max(-(-max(n, p) // page) for n in of) if of else 0 for p, of in groups) + 1
+    if wide:   # a table that could hold enough for the shared rows to be read once; otherwise small batches read them for each sequence
+        columns = max(columns, 150_000_000 // (4 * max(1, len(lens)) * page * heads * d))
     cache = nnc.PagedKV.empty(total, page, heads, d, kv, max(1, len(lens)), max(1, columns))
     for pool in (cache.k, cache.v):
         pool.view(torch.uint8).fill_(0x7f) if kv is E4M3 else pool.fill_(math.nan)
@@ -48,8 +50,8 @@ def _grouped(nnc, kv, groups, page, heads, d, seed, spare=2):
     return cache, lens, starts, [p for p, _ in groups], held
 
 
-def _check(nnc, kv, dtype, groups, page, heads, group, d, seed=1, scale=None, change=None):
-    cache, lens, starts, shared, held = _grouped(nnc, kv, groups, page, heads, d, seed)
+def _check(nnc, kv, dtype, groups, page, heads, group, d, seed=1, scale=None, change=None, wide=True):
+    cache, lens, starts, shared, held = _grouped(nnc, kv, groups, page, heads, d, seed, wide=wide)
     q = _randn(_gen(seed + 1), len(lens), heads * group, d)
     if change is not None:
         q = change(q)
@@ -74,7 +76,8 @@ def test_groups_of_any_size(nnc, kv, dtype, heads, group, d, page):
               (page - 1, [page, 4]),                                                               # less than one
               (5 * page, [5 * page + i for i in range(40)]),
               (page, [0, 0])]
-    _check(nnc, kv, dtype, groups, page, heads, group, d)
+    for wide in (True, False):
+        _check(nnc, kv, dtype, groups, page, heads, group, d, wide=wide)
 
 
 @pytest.mark.parametrize("kv,dtype", [(BF16, BF16), (F16, F16), (E4M3, BF16), (E4M3, F16)], ids=str)
