@@ -298,8 +298,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     load_queries(tile_q);
                     begins_q += part(tile_q);
                 }
-                if (j >= steps) continue;
             }
+            if (j >= steps) continue;
             if (left == 0) {   // this share's part of another tile
                 table = p.c.table + (long long)at.plan.b0 * p.c.pages_per_seq;
                 pos = at.step * kPrefixStep + r;

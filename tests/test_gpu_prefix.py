@@ -22,7 +22,7 @@ def _grouped(nnc, kv, groups, page, heads, d, seed, spare=2, wide=True):
     total = sum(whole) + sum(own) + spare
     columns = max(max(-(-max(n, p) // page) for n in of) if of else 0 for p, of in groups) + 1
     if wide:   # a table that could hold enough for the shared rows to be read once; otherwise small batches read them for each sequence
-        columns = max(columns, 150_000_000 // (4 * max(1, len(lens)) * page * heads * d))
+        columns = max(columns, 150_000_000 // (2 * max(1, len(lens)) * page * heads * d))
     cache = nnc.PagedKV.empty(total, page, heads, d, kv, max(1, len(lens)), max(1, columns))
     for pool in (cache.k, cache.v):
         pool.view(torch.uint8).fill_(0x7f) if kv is E4M3 else pool.fill_(math.nan)
@@ -85,6 +85,17 @@ def test_groups_of_any_size(nnc, kv, dtype, heads, group, d, page):
                                                                     (2, 2, 64, 32, 96, 300, 1), (4, 8, 128, 128, 1024, 16, 600), (1, 40, 128, 64, 2048, 13, 17)])
 def test_a_prefix_split_over_many_and_few_ctas(nnc, kv, dtype, heads, group, d, page, shared, members, tail):
     _check(nnc, kv, dtype, [(shared, [shared + 1 + (i * 37) % tail for i in range(members)])], page, heads, group, d, scale=0.2)
+
+
+@pytest.mark.parametrize("kv,dtype", [(BF16, BF16), (F16, F16), (E4M3, BF16)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_shares_of_few_steps_that_end_one_tile_and_begin_another(nnc, kv, dtype, d):
+    """Five tiles, 1 to 9 steps a share on 148 SMs: shares with fewer steps than there are stages, of two tiles each here and there."""
+    for share in range(1, 10):
+        for more in (0, 17):
+            shared = 64 * (148 * share // 5 + more)
+            _check(nnc, kv, dtype, [(shared, [shared + 1] * 40)], 64, 1, 16, d, scale=0.2)
+    _check(nnc, kv, dtype, [(64 * (1 + g % 5), [64 * (1 + g % 5) + 3] * (1 + g % 3)) for g in range(160)], 64, 1, 48, d, scale=0.2)
 
 
 def test_many_groups(nnc):
