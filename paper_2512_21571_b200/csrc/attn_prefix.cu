@@ -35,17 +35,19 @@ constexpr int kScoreBuffers = 4;
 constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then two accumulators of 128 columns
 constexpr float kLn2 = 0.69314718055994530942f;
 
-template <int D> struct Tiles {
+template <int D, bool CODES> struct Tiles {
     static constexpr int kHalves = D / 64;                        // slabs of 64 elements
     static constexpr int kQSlab = kPrefixRows * 128, kQ = kHalves * kQSlab;
     static constexpr int kSlabKV = kPrefixStep * 128, kKV = kHalves * kSlabKV;
-    // of K and of V.  At most kScoreBuffers: the producer takes a stage as free by the barriers of its step's score buffer, which then cannot move on
-    // by more than one phase before it has looked
-    static constexpr int kStages = 4;
+    // of K and of V.  At most kScoreBuffers: who fills a stage takes it as free by the barriers of its step's score buffer, which then cannot move on by
+    // more than one phase before it has looked
+    static constexpr int kStages = 4 - (CODES && D == 128);
     static_assert(kStages <= kScoreBuffers, "");
-    static constexpr int kBars = kQ + 2 * kStages * kKV;
+    // codes as they come: K, V, then a scale byte a row of each
+    static constexpr int kCodes = kPrefixStep * D, kRaw = 2 * kCodes + 2 * kPrefixStep, kRawStages = CODES ? 4 : 0, kRawAt = kQ + 2 * kStages * kKV;
+    static constexpr int kBars = kRawAt + kRawStages * kRaw;
     // more than an SM has left beside it for a CTA of the tail, which would take turns with the softmax (171 us instead of 89 + 14)
-    static constexpr int kSmem = (kBars > 160 << 10 ? kBars : 160 << 10) + 1024 /*alignment*/ + 256 /*barriers*/;
+    static constexpr int kSmem = (kBars > 160 << 10 ? kBars : 160 << 10) + 1024 /*alignment*/ + 512 /*barriers*/;
 };
 
 struct PrefixParams {
@@ -125,12 +127,22 @@ __device__ __forceinline__ void mma_commit(bool one, uint32_t bar) {
     asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"((uint32_t)one) : "memory");
 }
 
-// BF: bf16 caches, otherwise fp16; queries are of the cache's type
-template <int D, bool BF>
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_more(uint32_t bar, uint32_t bytes) {   // without arriving
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// KV: the cache's type; queries are of that type, or bf16 for codes.  Codes times their rows' scales are bf16 values exactly: they come to shared
+// memory as they are, and four warps (one softmax team's place) turn them into the rows that the products read.
+template <int D, int KV>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PrefixParams p) {
-    typedef Tiles<D> T;
-    constexpr int NS = T::kStages;
+    constexpr bool CODES = KV == NNC_E4M3, BF = KV != NNC_F16;
+    constexpr int kTeams = CODES ? 1 : 2;
+    typedef Tiles<D, CODES> T;
+    constexpr int NS = T::kStages, NC = T::kRawStages;
     // fp16 probabilities are scaled by 2^6, so that small ones keep their bits (at most 2^8 by the lazy maximum: below 2^15; sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 6.f;
     extern __shared__ uint8_t smem_raw[];
@@ -145,6 +157,11 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     auto p_full = [&](int j) { return q_ready + 8u * (1 + 2 * NS + kScoreBuffers + j % kScoreBuffers); };
     auto pv_done = [&](int j) { return q_ready + 8u * (1 + 2 * NS + 2 * kScoreBuffers + j % kScoreBuffers); };
     auto turn = [&](int j) { return (uint32_t)(j / kScoreBuffers & 1); };                                            // their parity
+    auto raw_full = [&](bool v, int st) { return q_ready + 8u * (1 + 2 * NS + 3 * kScoreBuffers + (v ? NC : 0) + st); };   // codes
+    auto raw_free = [&](bool v, int st) { return q_ready + 8u * (1 + 2 * NS + 3 * kScoreBuffers + 2 * NC + (v ? NC : 0) + st); };
+    auto raw_tile = [&](bool v, int st) { return base + (uint32_t)(T::kRawAt + st * T::kRaw + (v ? T::kCodes : 0)); };
+    auto raw_scales = [&](bool v, int st) { return base + (uint32_t)(T::kRawAt + st * T::kRaw + 2 * T::kCodes + (v ? kPrefixStep : 0)); };
+    constexpr int kFillers = CODES ? 64 : 1;   // arrivals that make a stage full: two warps, or the copy's
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s, first_g;
     __shared__ long long first_rest, sums[kThreads / 32];
@@ -155,7 +172,9 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (tid == 0) {
         abort_s = 0;
         mbar_init(q_ready, 1);
-        for (int st = 0; st < NS; ++st) { mbar_init(k_full(st), 1); mbar_init(v_full(st), 1); }
+        for (int st = 0; st < NS; ++st) { mbar_init(k_full(st), kFillers); mbar_init(v_full(st), kFillers); }
+        for (int st = 0; st < NC; ++st)
+            for (int v = 0; v < 2; ++v) { mbar_init(raw_full(v, st), 1); mbar_init(raw_free(v, st), 64); }
         for (int j = 0; j < kScoreBuffers; ++j) { mbar_init(s_full(j), 1); mbar_init(p_full(j), kSoftmaxRows); mbar_init(pv_done(j), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -267,37 +286,36 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     };
     auto wait = [&](uint32_t bar, uint32_t parity, int code) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.wait_status, code)); };
 
+    // Queries: a tile's first when the share begins, another's when the last scores of the tile before it are complete.  Whoever fills the stages of K
+    // sees that, and goes on looking until there is no tile left.
+    Step tile_q = at;
+    int begins_q = 0;   // the step where the next tile to load the queries of begins
+    auto load_queries = [&]() {   // [sequence][query head of the KV head][64]: a row of the tile after the other
+        if (lane == 0) mbar_expect_tx(q_ready, (uint32_t)(T::kHalves * p.per_tile * p.group * 128));
+        __syncwarp();
+        if (lane < T::kHalves) tma_load_3d(q_tile + lane * T::kQSlab, &map_q, q_ready, 64 * lane, tile_q.head * p.group, tile_q.plan.b0 + tile_q.tile * p.per_tile);
+        begins_q += part(tile_q);
+    };
+    // stage of step j (K's or V's) is free when the product that reads it is complete: the scores of step j - NS, or the output's
+    auto wait_stage = [&](bool v, int j) -> bool { return wait(v ? pv_done(j - NS) : s_full(j - NS), turn(j - NS), v ? 42 : 41); };
+
     if (warp <= 1) {   // ---------------- TMA producers, a lane a box: keys and queries; values ----------------
         const bool v = warp == 1;
-        const int half = lane & 1, r = (lane >> 1) * p.box;           // this lane's half of the head's elements, first position of a step
-        const bool loads = half < T::kHalves && r < kPrefixStep;
-        const uint32_t to = (v ? v_tile(0) : k_tile(0)) + (uint32_t)(half * T::kSlabKV + r * 128);
+        // this lane's half of the head's elements, first position of a step; of codes: the box, or its scales
+        const int half = lane & 1, r = (lane >> 1) * p.box;
+        const bool loads = (CODES || half < T::kHalves) && r < kPrefixStep;
         const CUtensorMap *const map = v ? &map_v : &map_k;
         const int absent = (int)min(paged_rows(p.c), 0x7fffffffll);   // a row outside the tensor: zeros
         const int page_rows = p.c.n_kv << p.c.page_shift, page_mask = (1 << p.c.page_shift) - 1;
-        auto load_queries = [&](const Step &x) {   // [sequence][query head of the KV head][64]: a row of the tile after the other
-            if (lane == 0) mbar_expect_tx(q_ready, (uint32_t)(T::kHalves * p.per_tile * p.group * 128));
-            __syncwarp();
-            if (lane < T::kHalves) tma_load_3d(q_tile + lane * T::kQSlab, &map_q, q_ready, 64 * lane, x.head * p.group, x.plan.b0 + x.tile * p.per_tile);
-        };
-        Step tile_q = at;
-        int begins_q = 0;   // the step where the next tile to load the queries of begins
-        if (steps > 0 && !v) {
-            load_queries(tile_q);
-            begins_q = part(tile_q);
-        }
-        // A stage is free when the product that reads it is complete: the scores of its step for K, the output's for V.  Queries are replaced when
-        // the tile's last scores are complete; so the keys' warp goes on looking until there is no tile left.
+        if (!CODES && steps > 0 && !v) load_queries();
         int left = 0, pos = 0, head_rows = 0, end = 0, page = 0;
         const int32_t *table = p.c.table;
-        for (int j = 0, st = 0; j < steps || (!v && begins_q < steps); ++j) {
-            if (j >= NS) {
-                const int done = j - NS;
-                if (!wait(v ? pv_done(done) : s_full(done), turn(done), v ? 42 : 41)) break;
-                if (!v && done + 1 == begins_q && begins_q < steps) {
-                    load_queries(tile_q);
-                    begins_q += part(tile_q);
-                }
+        for (int j = 0, st = 0, turn_st = 1; j < steps || (!CODES && !v && begins_q < steps); ++j) {
+            if constexpr (CODES) {
+                if (j >= NC && !wait(raw_free(v, st), (uint32_t)turn_st, 52)) break;
+            } else if (j >= NS) {
+                if (!wait_stage(v, j)) break;
+                if (!v && j - NS + 1 == begins_q && begins_q < steps) load_queries();
             }
             if (j >= steps) continue;
             if (left == 0) {   // this share's part of another tile
@@ -314,14 +332,69 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 else if (!v && half == 0) paged_complain(p.c);
             }
             if (!NNC_BC(row >= 0 && row <= absent, 3601)) row = absent;
-            const uint32_t bar = v ? v_full(st) : k_full(st);
-            if (lane == 0) mbar_expect_tx(bar, T::kKV);
-            __syncwarp();
-            if (loads) tma_load_2d(to + (uint32_t)(st * 2 * T::kKV), map, bar, 64 * half, row);
+            if constexpr (CODES) {
+                const uint32_t bar = raw_full(v, st), scales = raw_scales(v, st) + (uint32_t)r;
+                if (loads && half == 1) {
+                    if (row != absent) expect_more(bar, (uint32_t)p.box);
+                    else {
+                        for (int i = 0; i < p.box; i += 16) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(scales + i), "r"(0u) : "memory");
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // a later copy writes here, too
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_expect_tx(bar, T::kCodes);
+                __syncwarp();
+                if (loads && half == 0) tma_load_2d(raw_tile(v, st) + (uint32_t)(r * D), map, bar, 0, row);
+                if (loads && half == 1 && row != absent) bulk_load(scales, (v ? p.c.v_scale : p.c.k_scale) + row, (uint32_t)p.box, bar);
+            } else {
+                const uint32_t bar = v ? v_full(st) : k_full(st);
+                if (lane == 0) mbar_expect_tx(bar, T::kKV);
+                __syncwarp();
+                if (loads) tma_load_2d((v ? v_tile(st) : k_tile(st)) + (uint32_t)(half * T::kSlabKV + r * 128), map, bar, 64 * half, row);
+            }
             pos += kPrefixStep;
             --left;
             if (left > 0 && pos < end) page = table[pos >> p.c.page_shift];   // on its way while this warp waits for the next stage
+            if (++st == (CODES ? NC : NS)) { st = 0; turn_st ^= 1; }
+        }
+    } else if (CODES && warp >= 8) {   // ---------------- codes to bf16 rows: two warps for keys (the first of them asks for queries, too), two for values ----------------
+        const bool v = warp >= 10;
+        constexpr int kPieces = D / 16, kRowsAtOnce = 32 / kPieces;   // a row is so many lanes' 16 codes
+        const int piece = lane % kPieces, r0 = (warp & 1) * 32 + lane / kPieces;
+        if (warp == 8 && steps > 0) load_queries();
+        for (int j = 0, st = 0, raw = 0, turn_raw = 0; j < steps || (warp == 8 && begins_q < steps); ++j) {
+            if (j >= NS) {
+                if (!wait_stage(v, j)) break;
+                if (warp == 8 && j - NS + 1 == begins_q && begins_q < steps) load_queries();
+            }
+            if (j >= steps) continue;
+            if (!wait(raw_full(v, raw), (uint32_t)turn_raw, 53)) break;
+            const uint32_t from = raw_tile(v, raw) + (uint32_t)(r0 * D + piece * 16), scales = raw_scales(v, raw) + (uint32_t)r0, tile = v ? v_tile(st) : k_tile(st);
+#pragma unroll 2
+            for (int i = 0; i < 32; i += kRowsAtOnce) {
+                uint32_t x[4], byte, y[8];
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from + (uint32_t)(i * D)));
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(scales + (uint32_t)i));
+                const float scale = scale_from_byte(byte);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t h = e4m3x2_to_f16x2(x[e >> 1] >> (16 * (e & 1)) & 0xffffu);
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+                    y[e] = round_bf16x2(f.x * scale, f.y * scale);   // exact
+                }
+                const int row = r0 + i;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {   // 16-byte chunks; lanes of the second slab in the other order, for other banks
+                    const int which = e ^ (piece >> 2 & 1), chunk = 2 * piece + which;
+                    const uint32_t dst = tile + (uint32_t)((chunk >> 3) * T::kSlabKV + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(which ? y[4] : y[0]), "r"(which ? y[5] : y[1]), "r"(which ? y[6] : y[2]), "r"(which ? y[7] : y[3]) : "memory");
+                }
+            }
+            mbar_arrive(raw_free(v, raw));
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // generic-proxy writes, async-proxy (MMA) reads
+            mbar_arrive(v ? v_full(st) : k_full(st));
             if (++st == NS) st = 0;
+            if (++raw == NC) { raw = 0; turn_raw ^= 1; }
         }
     } else if (warp <= 3) {   // ---------------- MMA issuers: scores; outputs ----------------
         const bool one = lane == 0;
@@ -353,7 +426,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const uint64_t dv = make_smem_desc_mn(v_tile(0), T::kSlabKV);
             for (int j = 0, left = 0, nth = 0; j < steps; ++j) {
                 if (left == 0) { left = part(at); nth = 0; }
-                const bool begins = nth < 2;   // the accumulator of this step's team is empty
+                const bool begins = nth < kTeams;   // the accumulator of this step's team is empty
                 --left;
                 ++nth;
                 if (!wait(v_full(st), (uint32_t)turn_st, 47)) break;
@@ -364,7 +437,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int term = 0; term < 2; ++term)
 #pragma unroll
                     for (int ks = 0; ks < kPrefixStep / 16; ++ks)
-                        mma_ts(one, tmem_base + kColO + (uint32_t)(j & 1) * 128u, pa + (uint32_t)(term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
+                        mma_ts(one, tmem_base + kColO + (uint32_t)(j & (kTeams - 1)) * 128u, pa + (uint32_t)(term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
                                !begins || term != 0 || ks != 0);
                 mma_commit(one, pv_done(j));
                 if (++st == NS) { st = 0; turn_st ^= 1; }
@@ -386,19 +459,19 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int pos = (s0 + i) * kPrefixStep + 16 * (lane & 3);
                 return i >= n || pos >= at.plan.prefix || (unsigned)p.c.table[(long long)at.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)] < (unsigned)p.c.n_pages;
             };
-            const int first = (j0 ^ team) & 1;   // this team's first step
+            const int first = (j0 ^ team) & (kTeams - 1);   // this team's first step
             bool has = has_page(first);
             float m_used = -INFINITY, l = 0.f, ref = 0.f;
             // The first time once without effect, while rows and queries are on their way, on the empty accumulator instead of scores: fetching the
             // instructions of a step takes longer than the step
-            for (int i = j0 == 0 ? first - 2 : first; ok && i < n; i += 2) {
+            for (int i = j0 == 0 ? first - kTeams : first; ok && i < n; i += kTeams) {
                 const int j = j0 + i, p0 = (s0 + i) * kPrefixStep;
                 const bool dry = i < first;
                 if (!dry) ok = __all_sync(0xffffffffu, mbar_wait(s_full(j), turn(j), abort_flag, p.wait_status, 48));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t there = __ballot_sync(0xffffffffu, has) & 0xfu;   // per 16 positions
-                if (!dry) has = has_page(i + 2);
+                if (!dry) has = has_page(i + kTeams);
                 if (idle) {   // (its rows of P are whatever the scores' bits are, and nobody's)
                     if (!dry) mbar_arrive(p_full(j));
                     continue;
@@ -434,7 +507,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     // the maximum that O refers to moves only when a step passes it by 2^8
                     const bool need = valid && m_step > m_used + kLazyMax;
                     if (__any_sync(0xffffffffu, need)) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(pv_done(j - 2), turn(j - 2), abort_flag, p.wait_status, 49));
+                        ok = __all_sync(0xffffffffu, mbar_wait(pv_done(j - kTeams), turn(j - kTeams), abort_flag, p.wait_status, 49));
                         if (!ok) break;
                         tc_fence_after();
                         const float m_new = need ? m_step : m_used;
@@ -484,31 +557,34 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
             // ---- the part is done: each team writes half of the columns of both accumulators' sum ----
             if (first >= n) { m_used = -INFINITY; l = 0.f; }   // no step of this team's
-            ml_s[team][r] = make_float2(m_used == -INFINITY && l == 0.f ? -INFINITY : ref, l);
-            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+            const float2 x = make_float2(m_used == -INFINITY && l == 0.f ? -INFINITY : ref, l);
+            if constexpr (kTeams > 1) {
+                ml_s[team][r] = x;
+                asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+            }
             const int last = j0 + n - 1;
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last), turn(last), abort_flag, p.wait_status, 50));
-            if (ok && n > 1) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last - 1), turn(last - 1), abort_flag, p.wait_status, 51));
+            if (kTeams > 1 && ok && n > 1) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last - 1), turn(last - 1), abort_flag, p.wait_status, 51));
             if (ok && !idle) {
                 tc_fence_after();
                 const long long row = (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + head_row + kPrefixRows * cta;
                 const bool store = valid && NNC_BC(row < p.part_rows, 3602);
-                const float2 x = ml_s[team][r], y = ml_s[team ^ 1][r];
+                const float2 y = kTeams > 1 ? ml_s[team ^ 1][r] : make_float2(-INFINITY, 0.f);
                 const float m = fmaxf(x.x, y.x), ref_all = m == -INFINITY ? 0.f : m;
                 const float a = exp2f(x.x - ref_all), b = exp2f(y.x - ref_all);
                 if (store && team == 0) p.s.ml[row] = make_float2(m, fmaf(a, x.y, b * y.y));
-                const bool mine = first < n, other = n > 1 || !mine;   // which of the accumulators hold anything
-                const uint32_t at_mine = to + (uint32_t)(team * (D / 2)), at_other = at_mine + (team ? -128u : 128u);
-                float4 *dst = p.s.o + (team * (D / 8)) * p.part_rows + row;
+                const bool mine = first < n, other = kTeams > 1 && (n > 1 || !mine);   // which of the accumulators hold anything
+                const uint32_t at_mine = to + (uint32_t)(team * (D / kTeams)), at_other = at_mine + (team ? -128u : 128u);
+                float4 *dst = p.s.o + (team * (D / (4 * kTeams))) * p.part_rows + row;
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {   // 16 columns at a time
+                for (int c = 0; c < D / (16 * kTeams); ++c) {   // 16 columns at a time
                     uint32_t u[16], v[16];
                     tmem_ld16_nowait(at_mine + 16u * c, u);
-                    tmem_ld16_nowait(at_other + 16u * c, v);
+                    if constexpr (kTeams > 1) tmem_ld16_nowait(at_other + 16u * c, v);
                     tmem_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        u[e] = __float_as_uint((mine ? a * __uint_as_float(u[e]) : 0.f) + (other ? b * __uint_as_float(v[e]) : 0.f));
+                        u[e] = __float_as_uint((mine ? a * __uint_as_float(u[e]) : 0.f) + (kTeams > 1 && other ? b * __uint_as_float(v[e]) : 0.f));
                     if (store) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) store16(dst + (4 * c + e) * p.part_rows, u + 4 * e);
@@ -516,7 +592,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 tc_fence_before();
             }
-            asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");   // the accumulators and ml_s are free
+            if constexpr (kTeams > 1) asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");   // the accumulators and ml_s are free
             j0 += n;
             at.index += n - 1;
             at.step += n - 1;
@@ -555,7 +631,7 @@ struct JoinParams {
     int group, per_tile, n_q;
 };
 
-template <int D, bool BF>   // BF: results (and the cache) are bf16, otherwise fp16
+template <int D, bool BF, bool CODES>   // BF: results are bf16, otherwise fp16; the cache's type, or codes
 __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const JoinParams p) {
     constexpr int kFours = D / 4, kRows = kJoinThreads / kFours;   // of a row; rows at a time
     __shared__ float4 sums[kJoinThreads];
@@ -626,7 +702,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
         if (__syncthreads_or(store && !(fabsf((o.x + o.y) + (o.z + o.w)) < INFINITY))) {
             if (tid < D) {
                 uint32_t bits = 0;
-                const int end = n > 0 ? of.prefix : 0;
+                const int end = !CODES && n > 0 ? of.prefix : 0;   // (a code is never infinite, and NaN comes through by itself)
 #pragma unroll 4
                 for (int pos = 0; pos < end; ++pos) {
                     const int page = p.c.table[(long long)of.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
@@ -687,10 +763,11 @@ long long part_rows_of(int batch, int n_q) { return (long long)batch * n_q + (lo
 bool make_pool_map(CUtensorMap *map, const nnc_paged_kv &c, const void *pool, int box) {
     EncodeTiledFn enc = get_encode();
     if (!enc) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.n_pages * c.n_kv_heads * c.page_size}, strides[1] = {(cuuint64_t)c.head_dim * 2};
-    const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, one[2] = {1, 1};
-    return enc(map, c.type == NNC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pool), dims, strides, boxes, one,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const bool codes = c.type == NNC_E4M3;
+    const cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.n_pages * c.n_kv_heads * c.page_size}, strides[1] = {(cuuint64_t)c.head_dim * (codes ? 1 : 2)};
+    const cuuint32_t boxes[2] = {codes ? (cuuint32_t)c.head_dim : 64u, (cuuint32_t)box}, one[2] = {1, 1};
+    return enc(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : c.type == NNC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pool), dims, strides, boxes, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, codes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // the queries: [sequence][head][element], in boxes of a tile's
@@ -703,17 +780,23 @@ bool make_query_map(CUtensorMap *map, const void *q, bool bf, int d, int n_q, in
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF> cudaError_t launch_prefix_of(const LaunchCtx &lc, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const PrefixParams &p) {
+template <int D, int KV> cudaError_t launch_prefix_of(const LaunchCtx &lc, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const PrefixParams &p) {
+    typedef Tiles<D, KV == NNC_E4M3> T;
     static unsigned long long raised = 0;
-    auto kern = attn_prefix_kernel<D, BF>;
-    if (cudaError_t e = ensure_dynamic_smem(kern, Tiles<D>::kSmem, &raised); e != cudaSuccess) return e;
+    auto kern = attn_prefix_kernel<D, KV>;
+    if (cudaError_t e = ensure_dynamic_smem(kern, T::kSmem, &raised); e != cudaSuccess) return e;
     const int ctas = lc.sm_count < kPrefixMaxCtas ? lc.sm_count : kPrefixMaxCtas;
-    return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)Tiles<D>::kSmem, mq, mk, mv, p);
+    return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)T::kSmem, mq, mk, mv, p);
+}
+template <int D> cudaError_t launch_prefix_typed(const LaunchCtx &lc, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const PrefixParams &p, int kv) {
+    return kv == NNC_BF16 ? launch_prefix_of<D, NNC_BF16>(lc, mq, mk, mv, p) : kv == NNC_F16 ? launch_prefix_of<D, NNC_F16>(lc, mq, mk, mv, p) : launch_prefix_of<D, NNC_E4M3>(lc, mq, mk, mv, p);
 }
 
-template <int D> cudaError_t launch_join_of(const LaunchCtx &lc, const JoinParams &p, bool bf, long long ctas) {
-    return bf ? launch(lc, attn_prefix_join_kernel<D, true>, dim3((unsigned)ctas), dim3(kJoinThreads), p)
-              : launch(lc, attn_prefix_join_kernel<D, false>, dim3((unsigned)ctas), dim3(kJoinThreads), p);
+template <int D> cudaError_t launch_join_of(const LaunchCtx &lc, const JoinParams &p, int kv, long long ctas) {
+    const dim3 grid((unsigned)ctas), block(kJoinThreads);
+    if (kv == NNC_BF16) return launch(lc, attn_prefix_join_kernel<D, true, false>, grid, block, p);
+    if (kv == NNC_F16) return launch(lc, attn_prefix_join_kernel<D, false, false>, grid, block, p);
+    return launch(lc, attn_prefix_join_kernel<D, true, true>, grid, block, p);
 }
 
 }  // namespace
@@ -733,12 +816,12 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     // sides, us (three launches first), 4 query heads of 128 and 12 of 64 per KV head: 35 MB 19 and 15, 135 MB 27.6 and 27.6, 140 MB 26.0 and
     // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.
     const int eights = (n_q_heads / cache.n_kv_heads + 7) / 8;
-    const double rows_bytes = 4.0 * batch * cache.pages_per_seq * cache.page_size * cache.n_kv_heads * cache.head_dim;
-    if (type == NNC_F32 || cache.type == NNC_E4M3 || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
+    const double rows_bytes = (cache.type == NNC_E4M3 ? 2.0 : 4.0) * batch * cache.pages_per_seq * cache.page_size * cache.n_kv_heads * cache.head_dim;
+    if (type == NNC_F32 || (cache.type == NNC_E4M3 && type != NNC_BF16) || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
         n_groups == batch || rows_bytes * eights < 140e6)
         return launch_attn_paged(lc, q, cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, 0, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     const int d = cache.head_dim, group = n_q_heads / cache.n_kv_heads;
-    const bool bf = cache.type == NNC_BF16;
+    const bool bf = type == NNC_BF16;
     const PrefixScratch s = carve((char *)scratch + NNC_ATTN_PAGED_SCRATCH_BYTES, batch, n_q_heads, d, part_rows_of(batch, n_q_heads), nullptr);
     const PrefixGroups groups{starts, shared, n_groups, batch};
     PrefixParams p = {};
@@ -758,8 +841,7 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     if (!make_pool_map(&mk, cache, cache.k, p.box) || !make_pool_map(&mv, cache, cache.v, p.box)) return cudaErrorUnknown;
     LaunchCtx early = lc;
     early.pdl = true;
-    cudaError_t e = d == 64 ? (bf ? launch_prefix_of<64, true>(early, mq, mk, mv, p) : launch_prefix_of<64, false>(early, mq, mk, mv, p))
-                            : (bf ? launch_prefix_of<128, true>(early, mq, mk, mv, p) : launch_prefix_of<128, false>(early, mq, mk, mv, p));
+    cudaError_t e = d == 64 ? launch_prefix_typed<64>(early, mq, mk, mv, p, cache.type) : launch_prefix_typed<128>(early, mq, mk, mv, p, cache.type);
     if (e != cudaSuccess) return e;
     e = launch_attn_tail(lc, q, cache, lens, groups, s.tail, s.tail_lse, type, n_q_heads, q_stride, scale, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     if (e != cudaSuccess) return e;
@@ -767,7 +849,7 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     j.c = p.c; j.groups = groups; j.s = s; j.lens = lens;
     j.out = (char *)out; j.lse = lse; j.out_stride = out_stride; j.part_rows = p.part_rows; j.group = group; j.per_tile = p.per_tile; j.n_q = n_q_heads;
     const long long ctas = (long long)batch * cache.n_kv_heads;
-    return d == 64 ? launch_join_of<64>(early, j, bf, ctas) : launch_join_of<128>(early, j, bf, ctas);
+    return d == 64 ? launch_join_of<64>(early, j, cache.type, ctas) : launch_join_of<128>(early, j, cache.type, ctas);
 }
 
 }  // namespace nnc
