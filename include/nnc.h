@@ -399,8 +399,8 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
  * and a shared[g] outside 0 .. the table's reach are cut to what is allowed and, where the groups are looked at, set the status word.
  * 1 <= n_groups <= batch.
  *   q, out, lens, lse, scale, strides: as there, without a window.  Every sequence reads its own rows, and the groups are not looked at, where that
- *   is faster (batch * pages_per_seq * page_size small, a group for every sequence), and for fp32 queries, E4M3 caches, more than 128
- *   query heads per KV head and queries whose rows overlap.
+ *   is faster (batch * pages_per_seq * page_size small, a group for every sequence), and for fp32 queries, fp16 queries on E4M3 caches,
+ *   more than 128 query heads per KV head and queries whose rows overlap.
  * scratch: DEVICE, 256-byte aligned, nnc_attn_prefix_scratch_bytes(batch, n_q_heads, head_dim); its first NNC_ATTN_PAGED_TICKET_BYTES as
  * there.  Up to three launches. */
 size_t nnc_attn_prefix_scratch_bytes(int32_t batch, int32_t n_q_heads, int32_t head_dim);

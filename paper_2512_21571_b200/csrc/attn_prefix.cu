@@ -12,11 +12,14 @@
 // fills one tile, by the exponentials where it fills several.
 //   - The list of (group, KV head, tile, step of 64 positions) is cut into one contiguous share per CTA; the groups' lengths live on the
 //     device, so every CTA adds up the list itself.  A share may begin and end inside a tile.
-//   - One CTA of 384 threads per SM: a warp that fetches K (and Q), one that fetches V, one that issues S = Q K^T, one that issues O += P V (a
-//     single warp's instructions for two of these take longer than the step), and two teams of four softmax warps with a query row per thread, which take turns
-//     at the steps.  Four score buffers in tensor memory, so that scores run two steps ahead (with two, a step's scores wait for the product of
-//     the step before it).  Each team has an output accumulator and a running maximum of its own; they are joined where a share's part of a
-//     tile ends.
+//   - One CTA per SM: a warp that fetches K (and Q), one that fetches V, one that issues S = Q K^T, one that issues O += P V (a single warp's
+//     instructions for two of these take longer than the step), and two teams of four softmax warps with a query row per thread, which take
+//     turns at the steps.  Four score buffers in tensor memory, so that scores run two steps ahead (with two, a step's scores wait for the
+//     product of the step before it).  Each team has an output accumulator and a running maximum of its own; they are joined where a share's
+//     part of a tile ends.
+//   - E4M3: codes times their rows' scales are bf16 values exactly (down to 2^-133).  They come to shared memory as they are, eight warps make
+//     the rows of them that the products read, and there is one softmax team.  (Four such warps and two teams: 75 us instead of 70 for five
+//     groups of 12 behind 6000 codes; four and one team 73; every sequence's rows by themselves 112.)
 //   - Queries enter exactly.  Probabilities are two terms of the cache's type (bf16: 16 bits, fp16: 22), written over the scores they
 //     come from: one bf16 term alone would add an error of the size of the result's own rounding.  fp32 queries and results would need three
 //     terms and shorter sums; they go through the kernel that reads every sequence's rows.
@@ -29,13 +32,14 @@ namespace nnc {
 
 namespace {
 
-constexpr int kThreads = 384, kSoftmaxThreads = 256;
+constexpr int kSoftmaxThreads = 256;
 constexpr int kSoftmaxRows = 128;
 constexpr int kScoreBuffers = 4;
 constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then two accumulators of 128 columns
 constexpr float kLn2 = 0.69314718055994530942f;
 
 template <int D, bool CODES> struct Tiles {
+    static constexpr int kThreads = CODES ? 512 : 384;
     static constexpr int kHalves = D / 64;                        // slabs of 64 elements
     static constexpr int kQSlab = kPrefixRows * 128, kQ = kHalves * kQSlab;
     static constexpr int kSlabKV = kPrefixStep * 128, kKV = kHalves * kSlabKV;
@@ -114,7 +118,7 @@ __device__ __forceinline__ float top3(float a, float b, float c) {
 }
 
 // The products are issued by warp-wide code in which one lane's instruction counts: what they address then lies in uniform registers.  (Inside a
-// branch that one lane takes, every operand is moved there first: 85 to 115 cycles an instruction instead of .. .)
+// branch that one lane takes, every operand is moved there first: 85 to 115 cycles an instruction instead of 50.)
 __device__ __forceinline__ void mma_ss(bool one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)one) : "memory");
@@ -134,14 +138,14 @@ __device__ __forceinline__ void expect_more(uint32_t bar, uint32_t bytes) {   //
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// KV: the cache's type; queries are of that type, or bf16 for codes.  Codes times their rows' scales are bf16 values exactly: they come to shared
-// memory as they are, and four warps (one softmax team's place) turn them into the rows that the products read.
+// KV: the cache's type; queries are of that type, or bf16 for codes
 template <int D, int KV>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Tiles<D, KV == NNC_E4M3>::kThreads, 1)
 attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PrefixParams p) {
     constexpr bool CODES = KV == NNC_E4M3, BF = KV != NNC_F16;
-    constexpr int kTeams = CODES ? 1 : 2;
+    constexpr int kTeams = CODES ? 1 : 2;   // of softmax warps
     typedef Tiles<D, CODES> T;
+    constexpr int kThreads = T::kThreads;
     constexpr int NS = T::kStages, NC = T::kRawStages;
     // fp16 probabilities are scaled by 2^6, so that small ones keep their bits (at most 2^8 by the lazy maximum: below 2^15; sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 6.f;
@@ -161,7 +165,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     auto raw_free = [&](bool v, int st) { return q_ready + 8u * (1 + 2 * NS + 3 * kScoreBuffers + 2 * NC + (v ? NC : 0) + st); };
     auto raw_tile = [&](bool v, int st) { return base + (uint32_t)(T::kRawAt + st * T::kRaw + (v ? T::kCodes : 0)); };
     auto raw_scales = [&](bool v, int st) { return base + (uint32_t)(T::kRawAt + st * T::kRaw + 2 * T::kCodes + (v ? kPrefixStep : 0)); };
-    constexpr int kFillers = CODES ? 64 : 1;   // arrivals that make a stage full: two warps, or the copy's
+    constexpr int kConverters = 128, kFillers = CODES ? kConverters : 1;   // arrivals that make a stage full: four warps, or the copy's
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s, first_g;
     __shared__ long long first_rest, sums[kThreads / 32];
@@ -174,7 +178,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         mbar_init(q_ready, 1);
         for (int st = 0; st < NS; ++st) { mbar_init(k_full(st), kFillers); mbar_init(v_full(st), kFillers); }
         for (int st = 0; st < NC; ++st)
-            for (int v = 0; v < 2; ++v) { mbar_init(raw_full(v, st), 1); mbar_init(raw_free(v, st), 64); }
+            for (int v = 0; v < 2; ++v) { mbar_init(raw_full(v, st), 1); mbar_init(raw_free(v, st), kConverters); }
         for (int j = 0; j < kScoreBuffers; ++j) { mbar_init(s_full(j), 1); mbar_init(p_full(j), kSoftmaxRows); mbar_init(pv_done(j), 1); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -357,10 +361,10 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (left > 0 && pos < end) page = table[pos >> p.c.page_shift];   // on its way while this warp waits for the next stage
             if (++st == (CODES ? NC : NS)) { st = 0; turn_st ^= 1; }
         }
-    } else if (CODES && warp >= 8) {   // ---------------- codes to bf16 rows: two warps for keys (the first of them asks for queries, too), two for values ----------------
-        const bool v = warp >= 10;
+    } else if (CODES && warp >= 8) {   // ---------------- codes to bf16 rows: four warps for keys (the first of them asks for queries, too), four for values ----------------
+        const bool v = warp >= 12;
         constexpr int kPieces = D / 16, kRowsAtOnce = 32 / kPieces;   // a row is so many lanes' 16 codes
-        const int piece = lane % kPieces, r0 = (warp & 1) * 32 + lane / kPieces;
+        const int piece = lane % kPieces, r0 = (warp & 3) * 16 + lane / kPieces;
         if (warp == 8 && steps > 0) load_queries();
         for (int j = 0, st = 0, raw = 0, turn_raw = 0; j < steps || (warp == 8 && begins_q < steps); ++j) {
             if (j >= NS) {
@@ -370,8 +374,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (j >= steps) continue;
             if (!wait(raw_full(v, raw), (uint32_t)turn_raw, 53)) break;
             const uint32_t from = raw_tile(v, raw) + (uint32_t)(r0 * D + piece * 16), scales = raw_scales(v, raw) + (uint32_t)r0, tile = v ? v_tile(st) : k_tile(st);
-#pragma unroll 2
-            for (int i = 0; i < 32; i += kRowsAtOnce) {
+#pragma unroll 1   // the softmax's instructions want the room (four queries behind 32768 codes: 55.5 us; two at a time 57, all 58)
+            for (int i = 0; i < 16; i += kRowsAtOnce) {
                 uint32_t x[4], byte, y[8];
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from + (uint32_t)(i * D)));
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(scales + (uint32_t)i));
@@ -379,8 +383,8 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t h = e4m3x2_to_f16x2(x[e >> 1] >> (16 * (e & 1)) & 0xffffu);
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-                    y[e] = round_bf16x2(f.x * scale, f.y * scale);   // exact
+                    const float2 f = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2 *>(&h)), make_float2(scale, scale));
+                    y[e] = __byte_perm(__float_as_uint(f.x), __float_as_uint(f.y), 0x7632);   // the upper halves: the lower ones are 0
                 }
                 const int row = r0 + i;
 #pragma unroll
@@ -786,7 +790,7 @@ template <int D, int KV> cudaError_t launch_prefix_of(const LaunchCtx &lc, const
     auto kern = attn_prefix_kernel<D, KV>;
     if (cudaError_t e = ensure_dynamic_smem(kern, T::kSmem, &raised); e != cudaSuccess) return e;
     const int ctas = lc.sm_count < kPrefixMaxCtas ? lc.sm_count : kPrefixMaxCtas;
-    return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(kThreads), (size_t)T::kSmem, mq, mk, mv, p);
+    return launch_smem(lc, kern, dim3((unsigned)ctas), dim3(T::kThreads), (size_t)T::kSmem, mq, mk, mv, p);
 }
 template <int D> cudaError_t launch_prefix_typed(const LaunchCtx &lc, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const PrefixParams &p, int kv) {
     return kv == NNC_BF16 ? launch_prefix_of<D, NNC_BF16>(lc, mq, mk, mv, p) : kv == NNC_F16 ? launch_prefix_of<D, NNC_F16>(lc, mq, mk, mv, p) : launch_prefix_of<D, NNC_E4M3>(lc, mq, mk, mv, p);
@@ -810,11 +814,12 @@ size_t attn_prefix_scratch_bytes(int batch, int n_q_heads, int head_dim) {
 cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const int32_t *starts,
                                const int32_t *shared, int n_groups, void *out, float *lse, int type, int batch, int n_q_heads, int64_t q_stride,
                                int64_t out_stride, float scale, void *scratch) {
-    // Every sequence's own rows, the shared ones among them: fp32 and codes; more query heads than a tile has rows, which share rows among
-    // themselves; queries whose rows overlap, which a tensor map does not describe; groups of one.  And small batches: reading all of a table's
+    // Every sequence's own rows, the shared ones among them: fp32; codes with fp16 queries, which codes times their scales do not fit; more query
+    // heads than a tile has rows, which share rows among themselves; queries whose rows overlap, which a tensor map does not describe; groups of one.  And small batches: reading all of a table's
     // rows for each sequence, mostly from L2, goes at some 10 TB/s per eight query heads behind 9 us, three launches take 17 to 25 us.  Both
     // sides, us (three launches first), 4 query heads of 128 and 12 of 64 per KV head: 35 MB 19 and 15, 135 MB 27.6 and 27.6, 140 MB 26.0 and
-    // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.
+    // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.  Codes:
+    // 135 MB 35 and 34, 270 MB 38 and 52; 12 of 64, 135 MB 40 and 54.
     const int eights = (n_q_heads / cache.n_kv_heads + 7) / 8;
     const double rows_bytes = (cache.type == NNC_E4M3 ? 2.0 : 4.0) * batch * cache.pages_per_seq * cache.page_size * cache.n_kv_heads * cache.head_dim;
     if (type == NNC_F32 || (cache.type == NNC_E4M3 && type != NNC_BF16) || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
