@@ -20,7 +20,7 @@ struct ListedRows {
     static __device__ __forceinline__ int page(const PagedAttnParams &p, const Place &at, int pos, int &rows) {
         rows = 0;
         const int entry = pos >> p.c.page_shift;
-        if (!NNC_BC(entry < p.list_len && at.b < p.batch && at.head < p.c.n_kv, 3301)) return kNoPage;
+        if (!NNC_BC(entry < p.list_len && at.b < p.batch && at.head < p.c.n_kv, 3701)) return kNoPage;
         const int nth = p.list[((long long)at.b * p.c.n_kv + at.head) * p.list_len + entry];
         if ((unsigned)nth >= (unsigned)p.c.pages_per_seq) return kNoPage;
         rows = min(16, at.r.len - (nth << p.c.page_shift) - (pos & ((1 << p.c.page_shift) - 1)));

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kBoundsWarps * 32) page_bounds_kernel(const Bo
     const int piece = lane % kPieces, r0 = lane / kPieces;
     for (long long unit = (long long)blockIdx.x * kBoundsWarps + warp; unit < units; unit += (long long)gridDim.x * kBoundsWarps) {
         const int column = c_lo + (int)(unit / p.c.n_kv), head = (int)(unit % p.c.n_kv);
-        if (!NNC_BC(column < p.c.pages_per_seq && b < p.batch, 3401)) continue;
+        if (!NNC_BC(column < p.c.pages_per_seq && b < p.batch, 3801)) continue;
         const int page = p.c.table[(long long)b * p.c.pages_per_seq + column];
         if ((unsigned)page >= (unsigned)p.c.n_pages) {
             if (lane == 0) paged_complain(p.c);
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const Sco
         int page = -1;
         if (mine < pages) {
             page = p.c.table[(long long)b * columns + mine];
-            if ((unsigned)page >= (unsigned)p.c.n_pages || !NNC_BC(b < p.batch && head < p.c.n_kv, 3402)) { paged_complain(p.c); page = -1; }
+            if ((unsigned)page >= (unsigned)p.c.n_pages || !NNC_BC(b < p.batch && head < p.c.n_kv, 3802)) { paged_complain(p.c); page = -1; }
         }
         float best = -INFINITY;   // of page n0 + lane % 16
         if (n0 < pages) {
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_pages_kernel(const Sele
             const uint32_t e = s.y + __popc(ve[j] & before);
             if ((va[j] | (e < need ? ve[j] : 0u)) >> lane & 1u) {
                 const uint32_t at = s.x + __popc(va[j] & before) + min(e, need);
-                if (NNC_BC(at < (uint32_t)p.n, 3403)) out[at] = i0 + j * kSelectThreads + tid;
+                if (NNC_BC(at < (uint32_t)p.n, 3803)) out[at] = i0 + j * kSelectThreads + tid;
             }
         }
         __syncthreads();
