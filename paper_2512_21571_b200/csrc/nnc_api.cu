@@ -1124,7 +1124,7 @@ int nnc_op_select_pages(const float *scores, const int32_t *lens, int32_t *pages
     if (batch == 0) return NNC_OK;
     if (!scores || !lens || !pages || !counts) return NNC_ERR_INVALID_ARG;
     if (((uintptr_t)scores | (uintptr_t)lens | (uintptr_t)pages | (uintptr_t)counts) & 3) return NNC_ERR_INVALID_ARG;
-    if ((int64_t)batch * n_kv_heads > 0x7fffffff || n_columns > 0x7fffffff - 1024 || n > 0x7fffffff - 1024) return NNC_ERR_CAPACITY;
+    if ((int64_t)batch * n_kv_heads > 0x7fffffff || n_columns > 1 << 30 || n > 1 << 30) return NNC_ERR_CAPACITY;   // (indices run past the end by what a CTA looks at together)
     LaunchCtx lc;
     if (op_ctx(lc, cuda_stream)) return NNC_ERR_CUDA;
     return launch_select_pages(lc, scores, lens, pages, counts, batch, n_kv_heads, n_columns, page_size, n, first, last) == cudaSuccess ? NNC_OK : NNC_ERR_CUDA;

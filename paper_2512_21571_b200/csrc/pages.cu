@@ -160,7 +160,7 @@ template <int D, bool BF, int TYPE, int TERMS>
 __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const ScoreParams p) {
     constexpr int kSteps = 2 * D / 16;   // of the product: D / 16 of the lower bounds, as many of the upper
     extern __shared__ __align__(16) uint2 operand[];   // [groups of 8 queries][TERMS][kSteps][32 lanes]
-    __shared__ float undo[1024];   // fp16 terms of fp32 queries: what every query was multiplied by, inverted
+    __shared__ float undo[kMaxScoredGroup];   // fp16 terms of fp32 queries: what every query was multiplied by, inverted
     constexpr bool SCALED = !BF && TYPE == NNC_F32;
     pdl_launch_dependents();
     pdl_wait();

@@ -41,6 +41,8 @@ def test_selection_calls_that_are_refused_and_empty_ones(nnc):
                 dict(last=-1), dict(first=3, last=2), dict(first=2 ** 31 - 1, last=2 ** 31 - 1)):
         assert call(**bad) == INVALID, bad
     assert call(batch=1 << 20, heads=1 << 12) == CAPACITY and call(columns=2 ** 31 - 1) == CAPACITY
+    for n in (2 ** 30 + 1, 2 ** 31 - 1025):   # indices are 32-bit numbers, with room for a CTA's step behind the last one
+        assert call(columns=n) == CAPACITY and call(n=n) == CAPACITY
     assert call(batch=0) == 0 and call(batch=0, scores=None, pages=None) == 0
 
 
