@@ -14,7 +14,8 @@
 //     device, so every CTA adds up the list itself.  A share may begin and end inside a tile.
 //   - One CTA per SM: a warp that fetches K (and Q), one that fetches V, one that issues S = Q K^T, one that issues O += P V (a single warp's
 //     instructions for two of these take longer than the step), and two teams of four softmax warps with a query row per thread, which take
-//     turns at the steps.  Four score buffers in tensor memory, so that scores run two steps ahead (with two, a step's scores wait for the
+//     turns at the steps (three teams for heads of 64, whose accumulators leave room for a third: 48 sequences of 24 such heads behind 65536
+//     positions 65 us instead of 70).  Four score buffers in tensor memory, so that scores run two steps ahead (with two, a step's scores wait for the
 //     product of the step before it).  Each team has an output accumulator and a running maximum of its own; they are joined where a share's
 //     part of a tile ends.
 //   - E4M3: codes times their rows' scales are bf16 values exactly (down to 2^-133).  They come to shared memory as they are, eight warps make
@@ -32,14 +33,14 @@ namespace nnc {
 
 namespace {
 
-constexpr int kSoftmaxThreads = 256;
 constexpr int kSoftmaxRows = 128;
 constexpr int kScoreBuffers = 4;
 constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then two accumulators of 128 columns
 constexpr float kLn2 = 0.69314718055994530942f;
 
 template <int D, bool CODES> struct Tiles {
-    static constexpr int kThreads = CODES ? 512 : 384;
+    static constexpr int kTeams = CODES ? 1 : D == 64 ? 3 : 2;     // of four softmax warps; tensor memory has an accumulator for each
+    static constexpr int kThreads = 128 + 128 * kTeams + (CODES ? 256 : 0);
     static constexpr int kHalves = D / 64;                        // slabs of 64 elements
     static constexpr int kQSlab = kPrefixRows * 128, kQ = kHalves * kQSlab;
     static constexpr int kSlabKV = kPrefixStep * 128, kKV = kHalves * kSlabKV;
@@ -143,9 +144,8 @@ template <int D, int KV>
 __global__ void __launch_bounds__(Tiles<D, KV == NNC_E4M3>::kThreads, 1)
 attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PrefixParams p) {
     constexpr bool CODES = KV == NNC_E4M3, BF = KV != NNC_F16;
-    constexpr int kTeams = CODES ? 1 : 2;   // of softmax warps
     typedef Tiles<D, CODES> T;
-    constexpr int kThreads = T::kThreads;
+    constexpr int kThreads = T::kThreads, kTeams = T::kTeams;
     constexpr int NS = T::kStages, NC = T::kRawStages;
     // fp16 probabilities are scaled by 2^6, so that small ones keep their bits (at most 2^8 by the lazy maximum: below 2^15; sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 6.f;
@@ -169,7 +169,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s, first_g;
     __shared__ long long first_rest, sums[kThreads / 32];
-    __shared__ float2 ml_s[2][kPrefixRows];
+    __shared__ float2 ml_s[kTeams][kPrefixRows];
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     volatile int *abort_flag = &abort_s;
@@ -428,7 +428,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         } else {
             constexpr uint32_t idesc = make_idesc(D, !BF, true);
             const uint64_t dv = make_smem_desc_mn(v_tile(0), T::kSlabKV);
-            for (int j = 0, left = 0, nth = 0; j < steps; ++j) {
+            for (int j = 0, left = 0, nth = 0, team = 0; j < steps; ++j) {
                 if (left == 0) { left = part(at); nth = 0; }
                 const bool begins = nth < kTeams;   // the accumulator of this step's team is empty
                 --left;
@@ -441,15 +441,16 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int term = 0; term < 2; ++term)
 #pragma unroll
                     for (int ks = 0; ks < kPrefixStep / 16; ++ks)
-                        mma_ts(one, tmem_base + kColO + (uint32_t)(j & (kTeams - 1)) * 128u, pa + (uint32_t)(term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
+                        mma_ts(one, tmem_base + kColO + (uint32_t)(team * D), pa + (uint32_t)(term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
                                !begins || term != 0 || ks != 0);
                 mma_commit(one, pv_done(j));
+                if (++team == kTeams) team = 0;
                 if (++st == NS) { st = 0; turn_st ^= 1; }
             }
         }
     } else {   // ---------------- softmax: a query row per thread ----------------
         const int team = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;   // quarter: of tensor memory's lanes, which this warp may touch
-        const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, to = tmem_base + lane_addr + kColO + (uint32_t)team * 128u;
+        const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, to = tmem_base + lane_addr + kColO + (uint32_t)(team * D);
         const int member = r / p.group, head_row = r - member * p.group;
         bool ok = true;
         // Where a wait gave up, a warp still comes to the barriers below, once for every part of a tile, so that no other waits there for it
@@ -463,7 +464,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int pos = (s0 + i) * kPrefixStep + 16 * (lane & 3);
                 return i >= n || pos >= at.plan.prefix || (unsigned)p.c.table[(long long)at.plan.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)] < (unsigned)p.c.n_pages;
             };
-            const int first = (j0 ^ team) & (kTeams - 1);   // this team's first step
+            const int first = (team + kTeams - j0 % kTeams) % kTeams;   // this team's first step
             bool has = has_page(first);
             float m_used = -INFINITY, l = 0.f, ref = 0.f;
             // The first time once without effect, while rows and queries are on their way, on the empty accumulator instead of scores: fetching the
@@ -564,39 +565,52 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const float2 x = make_float2(m_used == -INFINITY && l == 0.f ? -INFINITY : ref, l);
             if constexpr (kTeams > 1) {
                 ml_s[team][r] = x;
-                asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");
             }
-            const int last = j0 + n - 1;
+            const int last = j0 + n - 1;   // its product is complete when all before it are
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last), turn(last), abort_flag, p.wait_status, 50));
-            if (kTeams > 1 && ok && n > 1) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last - 1), turn(last - 1), abort_flag, p.wait_status, 51));
-            if (ok && !idle) {
+            constexpr int kWriters = kTeams > 1 ? 2 : 1;   // each the same share of the columns
+            if (ok && !idle && team < kWriters) {
                 tc_fence_after();
                 const long long row = (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + head_row + kPrefixRows * cta;
                 const bool store = valid && NNC_BC(row < p.part_rows, 3602);
-                const float2 y = kTeams > 1 ? ml_s[team ^ 1][r] : make_float2(-INFINITY, 0.f);
-                const float m = fmaxf(x.x, y.x), ref_all = m == -INFINITY ? 0.f : m;
-                const float a = exp2f(x.x - ref_all), b = exp2f(y.x - ref_all);
-                if (store && team == 0) p.s.ml[row] = make_float2(m, fmaf(a, x.y, b * y.y));
-                const bool mine = first < n, other = kTeams > 1 && (n > 1 || !mine);   // which of the accumulators hold anything
-                const uint32_t at_mine = to + (uint32_t)(team * (D / kTeams)), at_other = at_mine + (team ? -128u : 128u);
-                float4 *dst = p.s.o + (team * (D / (4 * kTeams))) * p.part_rows + row;
+                float2 of[kTeams];
+                float m = -INFINITY, sum = 0.f, weight[kTeams];
+#pragma unroll
+                for (int t = 0; t < kTeams; ++t) {
+                    of[t] = kTeams > 1 ? ml_s[t][r] : x;
+                    m = fmaxf(m, of[t].x);
+                }
+#pragma unroll
+                for (int t = 0; t < kTeams; ++t) {
+                    weight[t] = exp2f(of[t].x - (m == -INFINITY ? 0.f : m));
+                    sum = fmaf(weight[t], of[t].y, sum);
+                }
+                if (store && team == 0) p.s.ml[row] = make_float2(m, sum);
+                const uint32_t from = tmem_base + lane_addr + kColO + (uint32_t)(team * (D / kWriters));
+                float4 *dst = p.s.o + (team * (D / (4 * kWriters))) * p.part_rows + row;
 #pragma unroll 1
-                for (int c = 0; c < D / (16 * kTeams); ++c) {   // 16 columns at a time
-                    uint32_t u[16], v[16];
-                    tmem_ld16_nowait(at_mine + 16u * c, u);
-                    if constexpr (kTeams > 1) tmem_ld16_nowait(at_other + 16u * c, v);
+                for (int c = 0; c < D / (16 * kWriters); ++c) {   // 16 columns at a time
+                    uint32_t u[kTeams][16];
+#pragma unroll
+                    for (int t = 0; t < kTeams; ++t) tmem_ld16_nowait(from + (uint32_t)(t * D + 16 * c), u[t]);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        u[e] = __float_as_uint((mine ? a * __uint_as_float(u[e]) : 0.f) + (kTeams > 1 && other ? b * __uint_as_float(v[e]) : 0.f));
+                    for (int e = 0; e < 16; ++e) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int t = 0; t < kTeams; ++t)   // (an accumulator that no step of this part wrote holds anything)
+                            if ((t + kTeams - j0 % kTeams) % kTeams < n) v = fmaf(weight[t], __uint_as_float(u[t][e]), v);
+                        u[0][e] = __float_as_uint(v);
+                    }
                     if (store) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) store16(dst + (4 * c + e) * p.part_rows, u + 4 * e);
+                        for (int e = 0; e < 4; ++e) store16(dst + (4 * c + e) * p.part_rows, u[0] + 4 * e);
                     }
                 }
                 tc_fence_before();
             }
-            if constexpr (kTeams > 1) asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory");   // the accumulators and ml_s are free
+            if constexpr (kTeams > 1) asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");   // the accumulators and ml_s are free
             j0 += n;
             at.index += n - 1;
             at.step += n - 1;
