@@ -462,3 +462,32 @@ def test_refusals_of_the_binding(nnc, scratch):
     same = q.clone()
     assert call(same, cache, lens, pages, counts, out=same, scratch=scratch) is same
     assert torch.equal(same, call(q, cache, lens, pages, counts, scratch=scratch))
+
+
+@pytest.mark.parametrize("kv", [BF16, E4M3], ids=str)
+def test_pages_far_in_a_pool_of_more_than_32_bits_of_elements(nnc, scratch, kv):
+    """The same rows at the pool's beginning and past its 2^31st (of codes: 2^32nd) element: the same results bit for bit."""
+    page, heads, d, lens, common = 256, 4, 128, [1100, 1024, 1290, 1030], 1024
+    whole, own = common // page, [-(-(n - common) // page) for n in lens]
+    far = (1 << (32 if kv is E4M3 else 31)) // (page * heads * d) + 3
+    results = []
+    for first in (1, far):
+        cache = nnc.PagedKV.empty(first + whole + sum(own), page, heads, d, kv, len(lens), 200)
+        at = first + whole
+        for b, x in enumerate(own):
+            cache.page_table[b, :whole] = torch.arange(first, first + whole, device="cuda")
+            cache.page_table[b, whole:whole + x] = torch.arange(at, at + x, device="cuda")
+            at += x
+        tokens = [(i, 0) for i in range(common)] + [(i, b) for b, n in enumerate(lens) for i in range(common, n)]
+        k, v = (_randn(_gen(s), len(tokens), heads, d, dtype=BF16) for s in (1, 2))
+        nnc.op_kv_write_paged(cache, k, v, _ints([t[0] for t in tokens]), _ints([t[1] for t in tokens]))
+        q, ends = _randn(_gen(3), len(lens), heads * 4, d, dtype=BF16), _ints(lens)
+        bounds = nnc.op_page_bounds(cache, nnc.page_bounds(cache), ends)
+        scores = nnc.op_score_pages(q, cache, bounds, ends)
+        pages, counts = nnc.op_select_pages(scores, ends, page, 3)
+        results.append([scores, pages, counts, *nnc.op_attn_selected_paged(q, cache, ends, pages, counts, scratch=scratch, want_lse=True),
+                        *nnc.op_attn_prefix_paged(q, cache, ends, _ints([0, 4]), _ints([common]), want_lse=True)])
+        assert nnc.op_status() == 0
+        del cache, bounds
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and not a.float().isnan().any()
