@@ -21,8 +21,9 @@
 //     product of the step before it).  Each team has an output accumulator and a running maximum of its own; they are joined where a share's
 //     part of a tile ends.
 //   - E4M3: codes times their rows' scales are bf16 values exactly (down to 2^-133).  They come to shared memory as they are, eight warps make
-//     the rows of them that the products read, and there is one softmax team.  (Five groups of 12 behind up to 6000 codes: 70 us; four such
-//     warps and one team 73, four and two 75, eight and two 70; every sequence's rows by themselves 112.)
+//     the rows of them that the products read, half of them a step each, and the two teams hold half of a step's scores at a time, which leaves
+//     room for the registers of 640 threads.  (Five groups of 12 behind up to 6000 codes: 66 us; all eight warps at every step, with one team or
+//     two, 70; four and one team 73, four and two 75; every sequence's rows by themselves 112.)
 //   - Queries enter exactly.  Probabilities are two terms of the cache's type (bf16: 16 bits, fp16: 22), written over the scores they
 //     come from: one bf16 term alone would add an error of the size of the result's own rounding.  fp32 queries and results would need three
 //     terms and shorter sums; they go through the kernel that reads every sequence's rows.
@@ -37,11 +38,11 @@ namespace {
 
 constexpr int kSoftmaxRows = 128;
 constexpr int kScoreBuffers = 4;
-constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then two accumulators of 128 columns
+constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then the teams' accumulators
 constexpr float kLn2 = 0.69314718055994530942f;
 
 template <int D, bool CODES> struct Tiles {
-    static constexpr int kTeams = CODES ? 1 : D == 64 ? 3 : 2;     // of four softmax warps; tensor memory has an accumulator for each
+    static constexpr int kTeams = D == 64 && !CODES ? 3 : 2;     // of four softmax warps; tensor memory has an accumulator for each
     static constexpr int kThreads = 128 + 128 * kTeams + (CODES ? 256 : 0);
     static constexpr int kHalves = D / 64;                        // slabs of 64 elements
     static constexpr int kQSlab = kPrefixRows * 128, kQ = kHalves * kQSlab;
@@ -148,6 +149,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     constexpr bool CODES = KV == NNC_E4M3, BF = KV != NNC_F16;
     typedef Tiles<D, CODES> T;
     constexpr int kThreads = T::kThreads, kTeams = T::kTeams;
+    constexpr int kHeld = CODES ? 1 : 2;           // halves of a step's scores that a thread holds at a time
     constexpr int NS = T::kStages, NC = T::kRawStages;
     // fp16 probabilities are scaled by 2^6, so that small ones keep their bits (at most 2^8 by the lazy maximum: below 2^15; sums are scaled alike)
     constexpr float kLift = BF ? 0.f : 6.f;
@@ -167,7 +169,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     auto raw_free = [&](bool v, int st) { return q_ready + 8u * (1 + 2 * NS + 3 * kScoreBuffers + 2 * NC + (v ? NC : 0) + st); };
     auto raw_tile = [&](bool v, int st) { return base + (uint32_t)(T::kRawAt + st * T::kRaw + (v ? T::kCodes : 0)); };
     auto raw_scales = [&](bool v, int st) { return base + (uint32_t)(T::kRawAt + st * T::kRaw + 2 * T::kCodes + (v ? kPrefixStep : 0)); };
-    constexpr int kConverters = 128, kFillers = CODES ? kConverters : 1;   // arrivals that make a stage full: four warps, or the copy's
+    constexpr int kConverters = 64, kFillers = CODES ? kConverters : 1;   // arrivals that make a stage full: two warps, or the copy's
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s, first_g;
     __shared__ long long first_rest, sums[kThreads / 32];
@@ -292,8 +294,9 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     };
     auto wait = [&](uint32_t bar, uint32_t parity, int code) -> bool { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, p.wait_status, code)); };
 
-    // Queries: a tile's first when the share begins, another's when the last scores of the tile before it are complete.  Whoever fills the stages of K
-    // sees that, and goes on looking until there is no tile left.
+    // Queries: a tile's first when the share begins, another's when the last scores of the tile before it are complete.  Rows of 16 bits: the warp that
+    // fetches K waits for that and goes on looking until there is no tile left.  Codes: that warp waits for conversions, which say too little of the
+    // scores (a barrier tells its last two phases apart), so the warp that issues the scores asks for the queries.
     Step tile_q = at;
     int begins_q = 0;   // the step where the next tile to load the queries of begins
     auto load_queries = [&]() {   // [sequence][query head of the KV head][64]: a row of the tile after the other
@@ -363,21 +366,17 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (left > 0 && pos < end) page = table[pos >> p.c.page_shift];   // on its way while this warp waits for the next stage
             if (++st == (CODES ? NC : NS)) { st = 0; turn_st ^= 1; }
         }
-    } else if (CODES && warp >= 8) {   // ---------------- codes to bf16 rows: four warps for keys (the first of them asks for queries, too), four for values ----------------
-        const bool v = warp >= 12;
+    } else if (CODES && warp >= 4 + 4 * kTeams) {   // ---------------- codes to bf16 rows: two warps for the keys of even steps, two for those of odd ones; the same for values ----------------
+        const bool v = warp >= 8 + 4 * kTeams;
         constexpr int kPieces = D / 16, kRowsAtOnce = 32 / kPieces;   // a row is so many lanes' 16 codes
-        const int piece = lane % kPieces, r0 = (warp & 3) * 16 + lane / kPieces;
-        if (warp == 8 && steps > 0) load_queries();
-        for (int j = 0, st = 0, raw = 0, turn_raw = 0; j < steps || (warp == 8 && begins_q < steps); ++j) {
-            if (j >= NS) {
-                if (!wait_stage(v, j)) break;
-                if (warp == 8 && j - NS + 1 == begins_q && begins_q < steps) load_queries();
-            }
-            if (j >= steps) continue;
-            if (!wait(raw_full(v, raw), (uint32_t)turn_raw, 53)) break;
+        const int piece = lane % kPieces, r0 = (warp & 1) * 32 + lane / kPieces;
+        for (int j = warp >> 1 & 1; j < steps; j += 2) {
+            const int st = j % NS, raw = j % NC;
+            if (!wait(raw_full(v, raw), (uint32_t)(j / NC & 1), 53)) break;
+            if (j >= NS && !wait_stage(v, j)) break;
             const uint32_t from = raw_tile(v, raw) + (uint32_t)(r0 * D + piece * 16), scales = raw_scales(v, raw) + (uint32_t)r0, tile = v ? v_tile(st) : k_tile(st);
-#pragma unroll 1   // the softmax's instructions want the room (four queries behind 32768 codes: 55.5 us; two at a time 57, all 58)
-            for (int i = 0; i < 16; i += kRowsAtOnce) {
+#pragma unroll 2
+            for (int i = 0; i < 32; i += kRowsAtOnce) {
                 uint32_t x[4], byte, y[8];
                 asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from + (uint32_t)(i * D)));
                 asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte) : "r"(scales + (uint32_t)i));
@@ -399,8 +398,6 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             mbar_arrive(raw_free(v, raw));
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // generic-proxy writes, async-proxy (MMA) reads
             mbar_arrive(v ? v_full(st) : k_full(st));
-            if (++st == NS) st = 0;
-            if (++raw == NC) { raw = 0; turn_raw ^= 1; }
         }
     } else if (warp <= 3) {   // ---------------- MMA issuers: scores; outputs ----------------
         const bool one = lane == 0;
@@ -412,6 +409,10 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             for (int j = 0, left = 0, tiles = 0; j < steps; ++j) {
                 if (left == 0) {   // a new tile's queries
                     left = part(at);
+                    if constexpr (CODES) {
+                        if (j > 0 && !wait(s_full(j - 1), turn(j - 1), 54)) break;
+                        load_queries();
+                    }
                     if (!wait(q_ready, (uint32_t)(tiles & 1), 43)) break;
                     ++tiles;
                 }
@@ -443,7 +444,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (int term = 0; term < 2; ++term)
 #pragma unroll
                     for (int ks = 0; ks < kPrefixStep / 16; ++ks)
-                        mma_ts(one, tmem_base + kColO + (uint32_t)(team * D), pa + (uint32_t)(term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
+                        mma_ts(one, tmem_base + kColO + (uint32_t)(team * D), pa + (uint32_t)(kHeld == 1 ? (ks >> 1) * 32 + term * 16 + (ks & 1) * 8 : term * 32 + ks * 8), stage(dv, st) + (uint64_t)(ks * (2048 >> 4)), idesc,
                                !begins || term != 0 || ks != 0);
                 mma_commit(one, pv_done(j));
                 if (++team == kTeams) team = 0;
@@ -484,28 +485,37 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     continue;
                 }
                 const uint32_t ts = dry ? to : tmem_base + lane_addr + kColS + (uint32_t)(j % kScoreBuffers * kPrefixStep);
-                uint32_t sv[2][32];
-                tmem_ld32_nowait(ts, sv[0]);
-                tmem_ld32_nowait(ts + 32u, sv[1]);
-                tmem_wait_ld();
-                if (p.flip) {
+                uint32_t held[kHeld][32];
+                auto fetch = [&](int c0) {   // columns from 32 c0 on
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) { sv[0][e] ^= p.flip; sv[1][e] ^= p.flip; }
-                }
-                if (p0 + kPrefixStep > at.plan.prefix || there != 0xfu) {
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                    for (int c = 0; c < kHeld; ++c) tmem_ld32_nowait(ts + 32u * (c0 + c), held[c]);
+                    tmem_wait_ld();
+                    if (p.flip) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (p0 + 32 * c + e >= at.plan.prefix || !(there >> (2 * c + e / 16) & 1u)) sv[c][e] = 0xff800000u;   // -infinity
-                }
+#pragma unroll
+                            for (int c = 0; c < kHeld; ++c) held[c][e] ^= p.flip;
+                    }
+                    if (p0 + kPrefixStep > at.plan.prefix || there != 0xfu) {
+#pragma unroll
+                        for (int c = 0; c < kHeld; ++c)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (p0 + 32 * (c0 + c) + e >= at.plan.prefix || !(there >> (2 * (c0 + c) + e / 16) & 1u)) held[c][e] = 0xff800000u;   // -infinity
+                    }
+                };
+                if constexpr (kHeld == 2) fetch(0);
+                auto scores_of = [&](int c) -> const uint32_t (&)[32] {
+                    if constexpr (kHeld == 1) fetch(c);
+                    return held[c & (kHeld - 1)];
+                };
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll kHeld
+                for (int c = 0; c < 2; ++c) {
+                    const auto &x = scores_of(c);
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) mx[x] = top3(mx[x], __uint_as_float(sv[c][e + 2 * x]), __uint_as_float(sv[c][e + 2 * x + 1]));
+                    for (int e = 0; e < 32; e += 2) mx[e / 2 & 3] = top3(mx[e / 2 & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                }
                 const float m_step = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
                 if (i <= first) {
                     m_used = m_step;
@@ -535,12 +545,13 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ref = (m_used == -INFINITY ? 0.f : m_used) - kLift;   // nothing attended so far: every weight is 0
                 const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), neg = make_float2(-ref, -ref);
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
+#pragma unroll kHeld
                 for (int c = 0; c < 2; ++c) {
                     uint32_t hi[16], lo[16];
+                    const auto &sv = scores_of(c);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv[c][2 * e]), __uint_as_float(sv[c][2 * e + 1])), scale2, neg);
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1])), scale2, neg);
                         const float2 w = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         sum[e & 1] = __fadd2_rn(sum[e & 1], w);
                         if constexpr (BF) {
@@ -554,24 +565,22 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             lo[e] = *reinterpret_cast<const uint32_t *>(&b);
                         }
                     }
-                    tmem_st16(ts + 16u * c, hi);
-                    tmem_st16(ts + 32u + 16u * c, lo);
+                    tmem_st16(ts + (kHeld == 1 ? 32u : 16u) * c, hi);
+                    tmem_st16(ts + (kHeld == 1 ? 32u * c + 16u : 32u + 16u * c), lo);
                 }
                 l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 tmem_wait_st();
                 tc_fence_before();
                 if (!dry) mbar_arrive(p_full(j));
             }
-            // ---- the part is done: each team writes half of the columns of both accumulators' sum ----
+            // ---- the part is done: two teams write half of the columns of the accumulators' sum each ----
             if (first >= n) { m_used = -INFINITY; l = 0.f; }   // no step of this team's
             const float2 x = make_float2(m_used == -INFINITY && l == 0.f ? -INFINITY : ref, l);
-            if constexpr (kTeams > 1) {
-                ml_s[team][r] = x;
-                asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");
-            }
+            ml_s[team][r] = x;
+            asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");
             const int last = j0 + n - 1;   // its product is complete when all before it are
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last), turn(last), abort_flag, p.wait_status, 50));
-            constexpr int kWriters = kTeams > 1 ? 2 : 1;   // each the same share of the columns
+            constexpr int kWriters = 2;   // teams, each half of the columns
             if (ok && !idle && team < kWriters) {
                 tc_fence_after();
                 const long long row = (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + head_row + kPrefixRows * cta;
@@ -580,7 +589,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 float m = -INFINITY, sum = 0.f, weight[kTeams];
 #pragma unroll
                 for (int t = 0; t < kTeams; ++t) {
-                    of[t] = kTeams > 1 ? ml_s[t][r] : x;
+                    of[t] = ml_s[t][r];
                     m = fmaxf(m, of[t].x);
                 }
 #pragma unroll
@@ -612,7 +621,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 tc_fence_before();
             }
-            if constexpr (kTeams > 1) asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");   // the accumulators and ml_s are free
+            asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");   // the accumulators and ml_s are free
             j0 += n;
             at.index += n - 1;
             at.step += n - 1;

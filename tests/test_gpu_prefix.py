@@ -98,6 +98,15 @@ def test_shares_of_few_steps_that_end_one_tile_and_begin_another(nnc, kv, dtype,
     _check(nnc, kv, dtype, [(64 * (1 + g % 5), [64 * (1 + g % 5) + 3] * (1 + g % 3)) for g in range(160)], 64, 1, 48, d, scale=0.2)
 
 
+@pytest.mark.parametrize("kv,dtype", [(BF16, BF16), (F16, F16), (E4M3, BF16)], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+def test_tiles_of_one_sequence_s_query_heads(nnc, kv, dtype, d):
+    """Every tile a sequence's 128 query heads, so queries change often; flat weights, where every row counts alike."""
+    groups = [(0, []), (3175, [3176]), (1535, [1536] * 9), (720, [0, 721, 721, 718, 721]), (232, [233]), (256, [257] * 60)]
+    for seed in range(8):
+        _check(nnc, kv, dtype, groups, 64, 5, 128, d, seed=seed, scale=0.01)
+
+
 def test_many_groups(nnc):
     for kv in (BF16, F16):
         _check(nnc, kv, kv, [(16 * (g % 9), [16 * (g % 9) + 1 + (i + g) % 30 for i in range(g % 4)]) for g in range(3, 250)], 16, 2, 4, 64)
