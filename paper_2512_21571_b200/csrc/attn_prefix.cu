@@ -29,6 +29,8 @@
 //     terms and shorter sums; they go through the kernel that reads every sequence's rows.
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "attn_prefill_common.cuh"
 #include "attn_prefix.cuh"
 
@@ -39,6 +41,8 @@ namespace {
 constexpr int kSoftmaxRows = 128;
 constexpr int kScoreBuffers = 4;
 constexpr uint32_t kColS = 0, kColO = kScoreBuffers * kPrefixStep, kTmemColumns = 512;   // score buffers, then the teams' accumulators
+// The reference of sums whose weights are all 0, where they are infinities or NaN all the same (of values); of sums of nothing it is -infinity
+constexpr float kNothing = -3e38f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 template <int D, bool CODES> struct Tiles {
@@ -174,6 +178,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __shared__ int abort_s, first_g;
     __shared__ long long first_rest, sums[kThreads / 32];
     __shared__ float2 ml_s[kTeams][kPrefixRows];
+    __shared__ uint32_t odd_s[CODES ? 1 : D];   // what a part's values hold besides finite numbers, where somebody looked: infinity 1, -infinity 2, NaN 4
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);   // the same in all lanes, which the compiler then knows
     volatile int *abort_flag = &abort_s;
@@ -456,6 +461,13 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16, to = tmem_base + lane_addr + kColO + (uint32_t)(team * D);
         const int member = r / p.group, head_row = r - member * p.group;
         bool ok = true;
+        // a barrier of all softmax warps that tells all of them whether any has seen something
+        auto any_of_all = [&](bool mine) -> bool {
+            uint32_t any;
+            __syncwarp();
+            asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbarrier.cta.red.or.aligned.pred p, 1, %2, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(any) : "r"((uint32_t)mine), "n"(128 * kTeams) : "memory");
+            return any != 0u;
+        };
         // Where a wait gave up, a warp still comes to the barriers below, once for every part of a tile, so that no other waits there for it
         for (int j0 = 0; j0 < steps;) {
             const int n = (int)min((long long)(at.plan.steps - at.step), t1 - at.index), s0 = at.step;   // this share's part of a tile: steps j0 .. j0 + n - 1
@@ -581,10 +593,11 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const int last = j0 + n - 1;   // its product is complete when all before it are
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(pv_done(last), turn(last), abort_flag, p.wait_status, 50));
             constexpr int kWriters = 2;   // teams, each half of the columns
+            const long long row = (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + head_row + kPrefixRows * cta;
+            const bool store = ok && valid && team < kWriters && NNC_BC(row < p.part_rows, 3602);
+            bool odd = false;   // a sum is no number, although the weights' is
             if (ok && !idle && team < kWriters) {
                 tc_fence_after();
-                const long long row = (long long)at.plan.b0 * p.n_q + ((long long)at.head * at.plan.members + nth) * p.group + head_row + kPrefixRows * cta;
-                const bool store = valid && NNC_BC(row < p.part_rows, 3602);
                 float2 of[kTeams];
                 float m = -INFINITY, sum = 0.f, weight[kTeams];
 #pragma unroll
@@ -600,6 +613,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (store && team == 0) p.s.ml[row] = make_float2(m, sum);
                 const uint32_t from = tmem_base + lane_addr + kColO + (uint32_t)(team * (D / kWriters));
                 float4 *dst = p.s.o + (team * (D / (4 * kWriters))) * p.part_rows + row;
+                float all_sums = 0.f;
 #pragma unroll 1
                 for (int c = 0; c < D / (16 * kWriters); ++c) {   // 16 columns at a time
                     uint32_t u[kTeams][16];
@@ -613,15 +627,59 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int t = 0; t < kTeams; ++t)   // (an accumulator that no step of this part wrote holds anything)
                             if ((t + kTeams - j0 % kTeams) % kTeams < n) v = fmaf(weight[t], __uint_as_float(u[t][e]), v);
                         u[0][e] = __float_as_uint(v);
+                        if constexpr (!CODES) all_sums += v;
                     }
                     if (store) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) store16(dst + (4 * c + e) * p.part_rows, u[0] + 4 * e);
                     }
                 }
+                if constexpr (!CODES) odd = store && !(fabsf(all_sums) < INFINITY) && sum == sum;
                 tc_fence_before();
             }
-            asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");   // the accumulators and ml_s are free
+            // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs,
+            // or NaN, leave no number).  The products cannot say so: a weight's lower term is of either sign or 0, and 0 times infinity is NaN.  So a
+            // part whose sums are not all finite looks through its value rows again, a row's 16-byte pieces on neighbouring lanes.  Not for rows whose
+            // weights' sum is itself no number, which their results then are, too; and not of codes, which are never infinite.
+            // From this barrier on the accumulators and ml_s are free.
+            if constexpr (CODES) asm volatile("bar.sync 1, %0;" ::"n"(128 * kTeams) : "memory");
+            else if (any_of_all(odd)) {
+                constexpr int kSoft = 128 * kTeams, kPieces = D / 8;
+                const int t = tid - 128;
+                if (t < D) odd_s[t] = 0u;
+                any_of_all(false);
+                uint32_t plus = 0, minus = 0, none = 0;   // a bit per column of this lane's piece
+                const int piece = t % kPieces, end = min((s0 + n) * kPrefixStep, at.plan.prefix);
+                const int32_t *const table = p.c.table + (long long)at.plan.b0 * p.c.pages_per_seq;
+#pragma unroll 4
+                for (int pos = s0 * kPrefixStep + t / kPieces; pos < end; pos += kSoft / kPieces) {
+                    const int page = table[pos >> p.c.page_shift];
+                    if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(p.c.v + paged_row(p.c, page, at.head, pos & ((1 << p.c.page_shift) - 1)) * (2 * D) + 16 * piece);
+                    const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+                        const uint32_t x = words[e / 2] >> (16 * (e & 1)) & 0xffffu, size = x & 0x7fffu;
+                        if (size >= kInf) (size > kInf ? none : x == size ? plus : minus) |= 1u << e;
+                    }
+                }
+                if (plus | minus | none)
+#pragma unroll 1
+                    for (int e = 0; e < 8; ++e)
+                        if (const uint32_t bits = (plus >> e & 1u) | (minus >> e & 1u) << 1 | (none >> e & 1u) << 2) atomicOr(&odd_s[8 * piece + e], bits);
+                any_of_all(false);
+                if (store) {
+#pragma unroll 1
+                    for (int c = 0; c < D / kWriters; ++c) {
+                        const int col = team * (D / kWriters) + c;
+                        const uint32_t bits = odd_s[col];
+                        if (bits) reinterpret_cast<float *>(p.s.o + (col >> 2) * p.part_rows + row)[col & 3] = bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
+                    }
+                    if (team == 0 && p.s.ml[row].x == -INFINITY) p.s.ml[row].x = kNothing;
+                }
+                any_of_all(false);
+            }
             j0 += n;
             at.index += n - 1;
             at.step += n - 1;
@@ -666,7 +724,6 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
     constexpr int kFours = D / 4, kRows = kJoinThreads / kFours;   // of a row; rows at a time
     __shared__ float4 sums[kJoinThreads];
     __shared__ float2 mls[kJoinThreads];
-    __shared__ uint32_t odd_bits[D];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, b = blockIdx.x / p.c.n_kv, head = blockIdx.x - b * p.c.n_kv;
@@ -694,15 +751,16 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
             l = fmaf(l, a, ml.y * w);
             o.x = fmaf(o.x, a, v.x * w); o.y = fmaf(o.y, a, v.y * w); o.z = fmaf(o.z, a, v.z * w); o.w = fmaf(o.w, a, v.w * w);
         };
+        const float2 *ml = p.s.ml + first_row + h0 + h;
+        const float4 *src = p.s.o + c4 * p.part_rows + first_row + h0 + h;
+        float2 tail_ml = make_float2(-INFINITY, 0.f);
+        float4 tail = o;
         if (mine) {
-            const float2 *ml = p.s.ml + first_row + h0 + h;
-            const float4 *src = p.s.o + c4 * p.part_rows + first_row + h0 + h;
             constexpr int kAhead = 8;   // pieces on their way at a time
-            float2 tail_ml = make_float2(-INFINITY, 0.f);
-            float4 tail = o;
             if (k == 0) {
                 tail_ml = make_float2(p.s.tail_lse[q_row + h] * 1.4426950408889634f, 1.f);
                 tail = *reinterpret_cast<const float4 *>(p.s.tail + (q_row + h) * D + 4 * c4);
+                if (!CODES && tail_ml.x == -INFINITY && !(fabsf((tail.x + tail.y) + (tail.z + tail.w)) < INFINITY)) tail_ml = make_float2(kNothing, 0.f);
             }
             for (int i0 = k; i0 < n; i0 += kAhead * apart) {
                 float2 x[kAhead];
@@ -727,34 +785,23 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
                 for (int j = 1; j < apart; ++j) add(mls[item + j * items], sums[item + j * items]);
         }
         const bool store = mine && k == 0;
-        // A column of values with an infinity in an attended row is that infinity, however small the row's weight (two of different signs,
-        // or NaN, leave no number); a weight of 0 made NaN of it.  So where a sum is no number the rows are looked through again.
-        if (__syncthreads_or(store && !(fabsf((o.x + o.y) + (o.z + o.w)) < INFINITY))) {
-            if (tid < D) {
-                uint32_t bits = 0;
-                const int end = !CODES && n > 0 ? of.prefix : 0;   // (a code is never infinite, and NaN comes through by itself)
+        if constexpr (!CODES)
+            if (store && l == l && !(fabsf((o.x + o.y) + (o.z + o.w)) < INFINITY)) {
+                // An infinite sum is its column's result, whatever it weighs (0 times it is no number): such columns once more, with the weights known
+                float4 again = make_float4(0.f, 0.f, 0.f, 0.f);
+                auto sum = [](float w, float v, float sum) { return fabsf(v) == INFINITY ? sum + v : fmaf(w, v, sum); };
+                auto weigh = [&](float x, float4 v) {
+                    const float w = m == -INFINITY ? 0.f : exp2f(x - m);
+                    again.x = sum(w, v.x, again.x); again.y = sum(w, v.y, again.y); again.z = sum(w, v.z, again.z); again.w = sum(w, v.w, again.w);
+                };
 #pragma unroll 4
-                for (int pos = 0; pos < end; ++pos) {
-                    const int page = p.c.table[(long long)of.b0 * p.c.pages_per_seq + (pos >> p.c.page_shift)];
-                    if ((unsigned)page >= (unsigned)p.c.n_pages) continue;
-                    constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
-                    const uint32_t x = reinterpret_cast<const uint16_t *>(p.c.v)[paged_row(p.c, page, head, pos & ((1 << p.c.page_shift) - 1)) * D + tid], size = x & 0x7fffu;
-                    if (size >= kInf) bits |= size > kInf ? 4u : x == size ? 1u : 2u;
-                }
-                odd_bits[tid] = bits;
+                for (int i = 0; i < n; ++i) weigh(ml[(long long)kPrefixRows * i].x, src[(long long)kPrefixRows * i]);
+                weigh(tail_ml.x, tail);
+                if (!(fabsf(o.x) < INFINITY)) o.x = again.x;
+                if (!(fabsf(o.y) < INFINITY)) o.y = again.y;
+                if (!(fabsf(o.z) < INFINITY)) o.z = again.z;
+                if (!(fabsf(o.w) < INFINITY)) o.w = again.w;
             }
-            __syncthreads();
-            if (store) {
-                float *const s[4] = {&o.x, &o.y, &o.z, &o.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t bits = odd_bits[4 * c4 + e];
-                    const float behind = p.s.tail[(q_row + h) * D + 4 * c4 + e];
-                    if (!(fabsf(behind) < INFINITY)) bits |= behind != behind ? 4u : behind > 0.f ? 1u : 2u;
-                    if (bits) *s[e] = bits == 1u ? INFINITY : bits == 2u ? -INFINITY : __uint_as_float(0x7fffffffu);
-                }
-            }
-        }
         if (store) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             const long long at = b * p.out_stride + ((long long)head * p.group + h0 + h) * D + 4 * c4;
