@@ -6,7 +6,7 @@ namespace nnc {
 namespace {
 
 struct WholeRows {
-    static constexpr bool kListed = false, kOutF32 = false, kTypeF32 = true, kConcurrent = false;
+    static constexpr bool kListed = false, kSums = false, kTypeF32 = true, kConcurrent = false;
     template <int TILE> static __device__ __forceinline__ Reach reach(const PagedAttnParams &p, int b, int) {
         const int len = length_of(p, p.lens[b]);
         return reach_between<TILE>((p.window > 0 && len > p.window) ? len - p.window : 0, len);

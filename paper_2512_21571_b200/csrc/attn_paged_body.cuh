@@ -50,7 +50,7 @@ struct PagedAttnParams {
     PagedView c;
     const char *q;
     char *out;
-    float *lse;
+    float *lse;   // where W::kSums, a pair of floats each: the weights' reference (log2 units) and their sum
     const int32_t *lens;
     float *part;
     uint32_t *tickets;
@@ -221,12 +221,13 @@ template <int TYPE> __device__ __forceinline__ void store_out(const PagedAttnPar
     else reinterpret_cast<__half *>(p.out)[at] = __float2half_rn(v);
 }
 
-// NT: groups of 8 query heads; TYPE: the queries' and (unless W wants them in 32 bits) the results'
+// NT: groups of 8 query heads; TYPE: the queries' and the results'.  W::kSums: results are the sums in 32 bits, not divided by the weights' sum, which
+// goes out beside them
 template <int D, int NT, int KV, int TYPE, typename W>
 __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
     typedef Shape<D, NT, KV, TYPE> S;
     constexpr bool BF = KV == NNC_BF16, CODES = KV == NNC_E4M3;
-    constexpr int OUT = W::kOutF32 ? NNC_F32 : TYPE;
+    constexpr int OUT = W::kSums ? NNC_F32 : TYPE;
     constexpr int PT = BF ? 3 : 2, QT = TYPE == NNC_F32 ? PT : 1;   // terms of the probabilities and of the queries
     constexpr int PB = S::kPB, TILE = S::kTile, ROW = S::kRow;
     // fp16 probabilities are scaled by 2^14, so that small ones keep their bits (the sums are scaled alike)
@@ -265,6 +266,11 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
         if (lane >= o) incl += x;
     }
     if (lane == 31) sh.sums[warp] = incl;
+    auto store_weights = [&](long long at, float m, float l) {
+        if constexpr (W::kSums) reinterpret_cast<float2 *>(p.lse)[at] = make_float2(m, l);
+        else p.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    };
+    auto inverse = [](float l) { return W::kSums ? 1.f : l == 0.f ? 0.f : 1.f / l; };
     if (__syncthreads_or(odd)) {   // zeros for sequences with nothing to attend to; lengths that do not fit are reported
         for (int b = blockIdx.y == 0 ? blockIdx.x : p.batch; b < p.batch; b += gridDim.x) {
             const int n_q = p.c.n_kv * p.group;
@@ -273,7 +279,7 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
                 if (W::template reach<TILE>(p, b, h).tiles > 0) continue;
                 const int first = h * p.group, end = W::kListed ? first + p.group : n_q;   // query heads
                 for (int i = first * D + tid; i < end * D; i += kWarps * 32) store_out<OUT>(p, b * p.out_stride + i, 0.f);
-                if (p.lse) for (int i = first + tid; i < end; i += kWarps * 32) p.lse[(long long)b * n_q + i] = -INFINITY;
+                if (p.lse) for (int i = first + tid; i < end; i += kWarps * 32) store_weights((long long)b * n_q + i, -INFINITY, 0.f);
             }
         }
     }
@@ -811,7 +817,7 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
                 for (int e = 0; e < 2; ++e) {
                     const int h = nt * 8 + 2 * t4 + e;
                     if (h >= heads_here) continue;
-                    const float inv = L[e] == 0.f ? 0.f : 1.f / L[e];
+                    const float inv = inverse(L[e]);
 #pragma unroll
                     for (int j = 0; j < S::kOnce; ++j) {
                         const int i = warp * S::kOwn + round * S::kOnce + j;
@@ -827,7 +833,7 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
                     }
                     if (round == 0 && warp == 0 && g8 == 0) {
                         if (!whole) *(reinterpret_cast<float2 *>(slot + 8 * NT * D) + h) = make_float2(M[e], L[e]);
-                        else if (p.lse) p.lse[lse_at + h] = L[e] == 0.f ? -INFINITY : (M[e] + log2f(L[e])) * kLn2;
+                        else if (p.lse) store_weights(lse_at + h, M[e], L[e]);
                     }
                 }
                 __syncthreads();
@@ -980,7 +986,7 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
                         if (hi == n && col % (D / 4) == 0) *(reinterpret_cast<float2 *>(slot_a + 8 * NT * D) + h) = ML;
                         continue;
                     }
-                    const float inv = ML.y == 0.f ? 0.f : 1.f / ML.y;
+                    const float inv = inverse(ML.y);
                     const long long at = b * p.out_stride + (long long)q_head * D + 4 * col;
                     if constexpr (OUT == NNC_F32) *reinterpret_cast<float4 *>(p.out + at * 4) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
                     else if constexpr (OUT == NNC_BF16)
@@ -989,8 +995,7 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
                         const __half2 lo2 = __floats2half2_rn(sum.x * inv, sum.y * inv), hi2 = __floats2half2_rn(sum.z * inv, sum.w * inv);
                         *reinterpret_cast<uint2 *>(p.out + at * 2) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo2), *reinterpret_cast<const uint32_t *>(&hi2));
                     }
-                    if (p.lse && col % (D / 4) == 0)
-                        p.lse[(long long)b * (p.c.n_kv * p.group) + q_head + h] = ML.y == 0.f ? -INFINITY : (ML.x + log2f(ML.y)) * kLn2;
+                    if (p.lse && col % (D / 4) == 0) store_weights((long long)b * (p.c.n_kv * p.group) + q_head + h, ML.x, ML.y);
                 }
             }
             __syncthreads();   // what is copied next goes where these weights and rows are

@@ -3,8 +3,8 @@
 //
 //   s_n = scale q.k_n,  o = sum_n exp(s_n - m) v_n / sum_n exp(s_n - m),  n < lens[b], in three launches:
 //   prefix   (this file)  m, l = sum exp(s_n - m), o~ = sum exp(s_n - m) v_n over the shared positions, for all queries of a group at a time
-//   tail     (attn_prefix_tail.cu)  the same, divided, over what lies behind them, sequence by sequence
-//   joining  (this file)  both, weighed by their sums
+//   tail     (attn_prefix_tail.cu)  the same over what lies behind them, sequence by sequence
+//   joining  (this file)  both; m and l go from one to the other as they are, so that a weight is as exact between parts as within one
 //
 // The queries of a group's sequences for one KV head are rows of one operand, so the prefix is a pair of matrix products with up to 128
 // rows, and tcgen05 does them: S = Q K^T and O += P V with S, P and O in tensor memory, K and V pages fetched by TMA (a page of a KV head is a
@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
         if (mine) {
             constexpr int kAhead = 8;   // pieces on their way at a time
             if (k == 0) {
-                tail_ml = make_float2(p.s.tail_lse[q_row + h] * 1.4426950408889634f, 1.f);
+                tail_ml = p.s.tail_ml[q_row + h];
                 tail = *reinterpret_cast<const float4 *>(p.s.tail + (q_row + h) * D + 4 * c4);
                 if (!CODES && tail_ml.x == -INFINITY && !(fabsf((tail.x + tail.y) + (tail.z + tail.w)) < INFINITY)) tail_ml = make_float2(kNothing, 0.f);
             }
@@ -829,7 +829,7 @@ PrefixScratch carve(char *at, int batch, int n_q, int d, long long part_rows, si
     s.of = (PrefixOf *)take(sizeof(PrefixOf) * batch);
     s.ml = (float2 *)take(8 * part_rows);
     s.o = (float4 *)take(4 * part_rows * d);
-    s.tail_lse = (float *)take(4ll * batch * n_q);
+    s.tail_ml = (float2 *)take(8ll * batch * n_q);
     s.tail = (float *)take(4ll * batch * n_q * d);
     if (bytes) *bytes = used;
     return s;
@@ -921,7 +921,7 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     early.pdl = true;
     cudaError_t e = d == 64 ? launch_prefix_typed<64>(early, mq, mk, mv, p, cache.type) : launch_prefix_typed<128>(early, mq, mk, mv, p, cache.type);
     if (e != cudaSuccess) return e;
-    e = launch_attn_tail(lc, q, cache, lens, groups, s.tail, s.tail_lse, type, n_q_heads, q_stride, scale, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
+    e = launch_attn_tail(lc, q, cache, lens, groups, s.tail, s.tail_ml, type, n_q_heads, q_stride, scale, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     if (e != cudaSuccess) return e;
     JoinParams j = {};
     j.c = p.c; j.groups = groups; j.s = s; j.lens = lens;

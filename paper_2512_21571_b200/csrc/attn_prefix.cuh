@@ -70,10 +70,11 @@ struct PrefixScratch {
     PrefixOf *of;                      // [batch]
     float2 *ml;                        // [rows]: reference in log2 units, sum
     float4 *o;                         // [D / 4][rows]: neighbouring threads hold neighbouring rows
-    float *tail_lse, *tail;            // [batch][n_q] and [batch][n_q][D]: what lies behind the prefix
+    float2 *tail_ml;                   // [batch][n_q]
+    float *tail;                       // [batch][n_q][D]: what lies behind the prefix, the same way
 };
 
 cudaError_t launch_attn_tail(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const PrefixGroups &groups, float *out,
-                             float *lse, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes);
+                             float2 *ml, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes);
 
 }  // namespace nnc

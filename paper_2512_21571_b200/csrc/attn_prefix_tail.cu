@@ -1,5 +1,5 @@
-// Attention of one new token per sequence over what lies behind the positions that its group shares, in 32 bits: one part of
-// the attention behind a shared prefix.  26 us for 80 MB behind 64 sequences' prefix, some of them while the prefix's last CTAs run.
+// Attention of one new token per sequence over what lies behind the positions that its group shares, as sums in 32 bits with their weights: one part
+// of the attention behind a shared prefix.  26 us for 80 MB behind 64 sequences' prefix, some of them while the prefix's last CTAs run.
 #include "attn_paged_body.cuh"
 #include "attn_prefix.cuh"
 
@@ -8,7 +8,7 @@ namespace nnc {
 namespace {
 
 struct TailRows {
-    static constexpr bool kListed = false, kOutF32 = true, kTypeF32 = false, kConcurrent = true;
+    static constexpr bool kListed = false, kSums = true, kTypeF32 = false, kConcurrent = true;
     template <int TILE> static __device__ __forceinline__ Reach reach(const PagedAttnParams &p, int b, int) {
         const PrefixGroups groups{p.starts, p.shared, p.n_groups, p.batch};
         const int len = length_of(p, p.lens[b]), g = group_of(groups, b);
@@ -25,8 +25,8 @@ struct TailRows {
 }  // namespace
 
 cudaError_t launch_attn_tail(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const PrefixGroups &groups, float *out,
-                             float *lse, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes) {
-    PagedAttnParams p = paged_attn_params(lc, q, cache, lens, out, lse, groups.batch, n_q_heads, q_stride, (int64_t)n_q_heads * cache.head_dim, scale, scratch,
+                             float2 *ml, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes) {
+    PagedAttnParams p = paged_attn_params(lc, q, cache, lens, out, (float *)ml, groups.batch, n_q_heads, q_stride, (int64_t)n_q_heads * cache.head_dim, scale, scratch,
                                           scratch_bytes);
     p.starts = groups.starts; p.shared = groups.shared; p.n_groups = groups.n_groups;
     return launch_paged_rows<TailRows>(lc, p, cache, type);

@@ -11,7 +11,7 @@ namespace nnc {
 namespace {
 
 struct ListedRows {
-    static constexpr bool kListed = true, kOutF32 = false, kTypeF32 = true, kConcurrent = false;
+    static constexpr bool kListed = true, kSums = false, kTypeF32 = true, kConcurrent = false;
     template <int TILE> static __device__ __forceinline__ Reach reach(const PagedAttnParams &p, int b, int head) {
         const int len = length_of(p, p.lens[b]);
         Reach r = reach_between<TILE>(0, len ? max(0, min(p.counts[(long long)b * p.c.n_kv + head], p.list_len)) << p.c.page_shift : 0);

@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_paged import BF16, F16, _gen, _ints, _randn, nnc  # noqa: F401
+from test_gpu_paged import BF16, E4M3, F16, _gen, _ints, _randn, nnc  # noqa: F401
 from test_gpu_prefix import _grouped
 
 pytestmark = pytest.mark.gpu
@@ -90,3 +90,40 @@ def test_columns_are_the_ordinary_attention_s(nnc, kv, d):
         assert torch.allclose(out[here].float(), want[here].float(), rtol=torch.finfo(kv).eps, atol=2.0 ** -10)
         assert torch.allclose(lse, want_lse, rtol=2.0 ** -18, atol=2.0 ** -18)
     assert nnc.op_status() == 0
+
+
+@pytest.mark.parametrize("kv,d", [(BF16, 128), (F16, 64), (E4M3, 128), (E4M3, 64)], ids=str)
+def test_weights_between_prefix_and_tail_are_exact_where_scores_are(nnc, kv, d):
+    """Every score is 2^14 (times a scale of 1: an exact product in log2 units, too), values are 1 in the prefix and -1 behind it: every weight is 1, and a
+    result differs from the counts' quotient by its own rounding, and 2^-16 for two terms of the weights, however large the scores are."""
+    shared, tails = 640, [640, 64, 1, 639, 5000]
+    cache, lens, starts, groups, _ = _grouped(nnc, kv, [(shared, [shared + t for t in tails])], 32, 1, d, 1)
+    k = torch.zeros(max(lens), 1, d, device="cuda")
+    k[:, 0, 0] = 1.0
+    v = torch.ones_like(k)
+    v[shared:] = -1.0
+    for b, n in enumerate(lens):
+        first = 0 if b == 0 else shared
+        nnc.op_kv_write_paged(cache, k[first:n].contiguous(), v[first:n].contiguous(), _ints(range(first, n)), _ints([b] * (n - first)))
+    q = torch.zeros(len(lens), 3, d, dtype=F16 if kv is F16 else BF16, device="cuda")
+    q[..., 0] = 2.0 ** 14
+    out, lse = nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(groups), scale=1.0, want_lse=True)
+    for b, t in enumerate(tails):
+        want = (shared - t) / (shared + t)
+        assert ((out[b].double() - want).abs() <= torch.finfo(out.dtype).eps / 2 * abs(want) + 2.0 ** -16).all(), (b, out[b, 0, 0].item(), want)
+        # the weights' reference and the result's own rounding: two half steps of 2^-9 (values up to 2^15)
+        assert ((lse[b].double() - (2.0 ** 14 + math.log(shared + t))).abs() <= 2.0 ** -9 + 2.0 ** -16).all()
+
+
+@pytest.mark.parametrize("kv,d", [(BF16, 128), (F16, 64)], ids=str)
+def test_an_infinity_behind_the_prefix_whose_row_weighs_nothing(nnc, kv, d):
+    """All keys behind the prefix are out of sight (scores of -infinity) and one of their values is infinite: its column is, as in the ordinary attention."""
+    cache, lens, starts, shared, _ = _grouped(nnc, kv, [(640, [700, 650, 640])], 32, 1, d, 4)
+    for pos in range(640, 700):
+        cache.k[cache.page_table[0, pos // 32].long(), :, pos % 32, 0] = -math.inf
+    cache.v[cache.page_table[0, 20].long(), 0, 9, 3] = -math.inf
+    q = _randn(_gen(5), 3, 4, d).abs().to(kv)
+    out, lse = nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(shared), want_lse=True)
+    want, want_lse = nnc.op_attn_decode_paged(q, cache, _ints(lens), want_lse=True)
+    assert (want[0, :, 3] == -math.inf).all() and torch.equal(out.isfinite(), want.isfinite()) and (out[0, :, 3] == -math.inf).all()
+    assert torch.allclose(lse, want_lse, rtol=2.0 ** -18, atol=2.0 ** -18)
