@@ -109,7 +109,7 @@ def test_shared_codes_behind_a_sequence_s_end_do_not_reach_it(nnc, d):
         cache, lens, starts, groups, held = _grouped(nnc, E4M3, [(shared, lens_of)], 16, 2, d, 2)
         last = cache.page_table[0, shared // 16 - 1].long()
         cache.v.view(torch.uint8)[last, :, 15, 4] = 0x7f                   # NaN
-        cache.k_scale[last, :, 15] = 255                                  # no number either
+        cache.k.view(torch.uint8)[last, :, 15, 0] = 0x7f
         q = _randn(_gen(4), len(lens), 6, d, dtype=BF16)
         out, lse = nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(groups), want_lse=True)
         short = [b for b, n in enumerate(lens) if n < shared]
