@@ -398,9 +398,11 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
  * no group, and of groups with shared[g] below a page, attend to their own rows alone.  A `starts` that descends or leaves 0 .. batch
  * and a shared[g] outside 0 .. the table's reach are cut to what is allowed and, where the groups are looked at, set the status word.
  * 1 <= n_groups <= batch.
- *   q, out, lens, lse, scale, strides: as there, without a window.  Every sequence reads its own rows, and the groups are not looked at, where that
- *   is faster (batch * pages_per_seq * page_size small, a group for every sequence), and for fp32 queries, fp16 queries on E4M3 caches,
- *   more than 128 query heads per KV head and queries whose rows overlap.
+ *   q, out, lens, lse, scale, strides: as there, without a window.  A group of few sequences reads each one's own rows (below two, on NNC_E4M3
+ *   caches below four; fewer with many query heads per KV head); groups of no sequences cost nothing, so that the arrays of a captured call may
+ *   have room for more groups than there are.  Every sequence reads its own rows, and the groups are not looked at, for one sequence, for fp32
+ *   queries, fp16 queries on NNC_E4M3 caches, more than 128 query heads per KV head, queries whose rows overlap, and where the table has room
+ *   for little: all rows that it could name, whatever the lengths are, times the query heads per KV head in eights are less than 140 MB.
  * scratch: DEVICE, 256-byte aligned, nnc_attn_prefix_scratch_bytes(batch, n_q_heads, head_dim); its first NNC_ATTN_PAGED_TICKET_BYTES as
  * there.  Up to three launches. */
 size_t nnc_attn_prefix_scratch_bytes(int32_t batch, int32_t n_q_heads, int32_t head_dim);

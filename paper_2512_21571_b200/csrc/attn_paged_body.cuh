@@ -61,7 +61,7 @@ struct PagedAttnParams {
     const int32_t *list, *counts;    // listed pages of every (sequence, KV head): [list_len], how many count
     int list_len;
     const int32_t *starts, *shared;  // groups of sequences: the first of each and the end; positions that they share
-    int n_groups;
+    int n_groups, least;
 };
 
 template <int D, int NT, int KV, int TYPE>

@@ -888,7 +888,7 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
                                const int32_t *shared, int n_groups, void *out, float *lse, int type, int batch, int n_q_heads, int64_t q_stride,
                                int64_t out_stride, float scale, void *scratch) {
     // Every sequence's own rows, the shared ones among them: fp32; codes with fp16 queries, which codes times their scales do not fit; more query
-    // heads than a tile has rows, which share rows among themselves; queries whose rows overlap, which a tensor map does not describe; groups of one.  And small batches: reading all of a table's
+    // heads than a tile has rows, which share rows among themselves; queries whose rows overlap, which a tensor map does not describe; one sequence.  And small batches: reading all of a table's
     // rows for each sequence, mostly from L2, goes at some 10 TB/s per eight query heads behind 9 us, three launches take 17 to 25 us.  Both
     // sides, us (three launches first), 4 query heads of 128 and 12 of 64 per KV head: 35 MB 19 and 15, 135 MB 27.6 and 27.6, 140 MB 26.0 and
     // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.  Codes:
@@ -896,12 +896,19 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     const int eights = (n_q_heads / cache.n_kv_heads + 7) / 8;
     const double rows_bytes = (cache.type == NNC_E4M3 ? 2.0 : 4.0) * batch * cache.pages_per_seq * cache.page_size * cache.n_kv_heads * cache.head_dim;
     if (type == NNC_F32 || (cache.type == NNC_E4M3 && type != NNC_BF16) || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
-        n_groups == batch || rows_bytes * eights < 140e6)
+        batch == 1 || rows_bytes * eights < 140e6)
         return launch_attn_paged(lc, q, cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, 0, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     const int d = cache.head_dim, group = n_q_heads / cache.n_kv_heads;
     const bool bf = type == NNC_BF16;
     const PrefixScratch s = carve((char *)scratch + NNC_ATTN_PAGED_SCRATCH_BYTES, batch, n_q_heads, d, part_rows_of(batch, n_q_heads), nullptr);
-    const PrefixGroups groups{starts, shared, n_groups, batch};
+    // Groups of few sequences read their own rows, through the kernel for what lies behind prefixes.  How many a group has is known to the device alone
+    // (n_groups may count groups of none, so that a captured call has room for them).  us, prefix of 8192 or 16384 at once / each its own: one sequence of
+    // 4 heads 191 / 177, of 16 81 / 68 and 64 / 43, of 24 85 / 97 and 60 / 58, of 32 92 / 108 and 65 / 65; two of 4 108 / 182, of 8 with heads of 64 86 / 95.
+    // Codes: one of 32 103 / 88 and 80 / 57, of 64 86 / 89 and 63 / 60; two of 4 140 / 106, of 16 61 / 54, of 24 62 / 79 and 52 / 54; three of 4 102 / 100,
+    // of 16 52 / 52; four of 4 88 / 105, of 8 with heads of 64 72 / 72.  Where no group has as many, three launches do what one would: 192 instead of 184 us
+    // for 32 of 8192, codes 115 instead of 106.
+    const int least = cache.type == NNC_E4M3 ? (group >= 48 ? 1 : group >= 24 ? 2 : group >= 16 ? 3 : 4) : group >= 32 ? 1 : 2;
+    const PrefixGroups groups{starts, shared, n_groups, batch, least};
     PrefixParams p = {};
     p.c = paged_view(cache, lc.status);
     p.groups = groups;

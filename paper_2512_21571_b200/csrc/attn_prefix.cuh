@@ -12,6 +12,7 @@ constexpr int kPrefixMaxCtas = 160;    // one per SM
 struct PrefixGroups {
     const int32_t *starts, *shared;
     int n_groups, batch;
+    int least;                         // sequences that a group has at least where its rows are read for all of them at once
 };
 
 // where a group's tiles stand in the list
@@ -28,8 +29,12 @@ struct PrefixOf {
     long long share;                   // places of a CTA
 };
 
-// positions of a group that its sequences share: whole pages
+__device__ __forceinline__ int first_of(const PrefixGroups &s, int g) { return min(max(s.starts[g], 0), s.batch); }
+__device__ __forceinline__ int members_of(const PrefixGroups &s, int g) { return max(first_of(s, g + 1) - first_of(s, g), 0); }
+
+// positions of a group that its sequences share: whole pages; none where there are too few sequences for it to pay
 __device__ __forceinline__ int prefix_of(const PagedView &c, const PrefixGroups &s, int g) {
+    if (members_of(s, g) < s.least) return 0;
     return min(max(s.shared[g], 0), c.pages_per_seq << c.page_shift) >> c.page_shift << c.page_shift;
 }
 
@@ -50,8 +55,8 @@ __device__ __forceinline__ int group_of(const PrefixGroups &s, int b) {
 
 __device__ __forceinline__ PrefixPlan plan_of(const PagedView &c, const PrefixGroups &s, int g, int per_tile) {   // per_tile: sequences
     PrefixPlan p;
-    p.b0 = min(max(s.starts[g], 0), s.batch);
-    p.members = max(min(max(s.starts[g + 1], 0), s.batch) - p.b0, 0);
+    p.b0 = first_of(s, g);
+    p.members = members_of(s, g);
     p.tiles = (p.members + per_tile - 1) / per_tile;
     p.prefix = prefix_of(c, s, g);
     p.steps = p.members ? (p.prefix + kPrefixStep - 1) / kPrefixStep : 0;

@@ -10,7 +10,7 @@ namespace {
 struct TailRows {
     static constexpr bool kListed = false, kSums = true, kTypeF32 = false, kConcurrent = true;
     template <int TILE> static __device__ __forceinline__ Reach reach(const PagedAttnParams &p, int b, int) {
-        const PrefixGroups groups{p.starts, p.shared, p.n_groups, p.batch};
+        const PrefixGroups groups{p.starts, p.shared, p.n_groups, p.batch, p.least};
         const int len = length_of(p, p.lens[b]), g = group_of(groups, b);
         const int prefix = g < 0 ? 0 : prefix_of(p.c, groups, g), start = takes_prefix(prefix, p.lens[b]) ? prefix : 0;
         return start < len ? reach_between<TILE>(start, len) : Reach{len, len, 0, len};
@@ -28,7 +28,7 @@ cudaError_t launch_attn_tail(const LaunchCtx &lc, const void *q, const nnc_paged
                              float2 *ml, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes) {
     PagedAttnParams p = paged_attn_params(lc, q, cache, lens, out, (float *)ml, groups.batch, n_q_heads, q_stride, (int64_t)n_q_heads * cache.head_dim, scale, scratch,
                                           scratch_bytes);
-    p.starts = groups.starts; p.shared = groups.shared; p.n_groups = groups.n_groups;
+    p.starts = groups.starts; p.shared = groups.shared; p.n_groups = groups.n_groups; p.least = groups.least;
     return launch_paged_rows<TailRows>(lc, p, cache, type);
 }
 
