@@ -1018,6 +1018,13 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<D, NT, KV, TYPE>::kCtas) at
         if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1) pdl_wait();
 }
 
+// the longest list that a table allows: its places are 32-bit numbers
+inline bool list_fits(long long most, int tile, int batch, int n_kv, long long *places = nullptr) {
+    const long long n = ((most + 15 + tile - 1) / tile + 1) * batch * n_kv;
+    if (places) *places = n;
+    return n <= 0x3fffffffll;
+}
+
 template <int D, int NT, int KV, int TYPE, typename W>
 cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     typedef Shape<D, NT, KV, TYPE> S;
@@ -1025,9 +1032,8 @@ cudaError_t launch_one(const LaunchCtx &lc, const PagedAttnParams &p) {
     auto kern = attn_paged_kernel<D, NT, KV, TYPE, W>;
     cudaError_t e = ensure_dynamic_smem(kern, S::kSmem, &raised);
     if (e != cudaSuccess) return e;
-    const long long most = W::most(p);
-    const long long tiles = ((most + 15 + S::kTile - 1) / S::kTile + 1) * p.batch * p.c.n_kv;   // the longest list the table allows
-    if (tiles > 0x3fffffffll) return cudaErrorInvalidValue;
+    long long tiles;
+    if (!list_fits(W::most(p), S::kTile, p.batch, p.c.n_kv, &tiles)) return cudaErrorInvalidValue;
     long long ctas = (long long)S::kCtas * lc.sm_count;
     if (ctas > kPagedMaxCtas) ctas = kPagedMaxCtas;
     const long long fit = (long long)(p.part_floats / (2 * S::kSlotFloats));

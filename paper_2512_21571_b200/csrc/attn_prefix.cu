@@ -898,6 +898,7 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     if (type == NNC_F32 || (cache.type == NNC_E4M3 && type != NNC_BF16) || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
         batch == 1 || rows_bytes * eights < 140e6)
         return launch_attn_paged(lc, q, cache, lens, out, lse, type, batch, n_q_heads, q_stride, out_stride, scale, 0, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
+    if (!attn_tail_fits(cache, batch)) return cudaErrorInvalidValue;
     const int d = cache.head_dim, group = n_q_heads / cache.n_kv_heads;
     const bool bf = type == NNC_BF16;
     const PrefixScratch s = carve((char *)scratch + NNC_ATTN_PAGED_SCRATCH_BYTES, batch, n_q_heads, d, part_rows_of(batch, n_q_heads), nullptr);

@@ -79,6 +79,8 @@ struct PrefixScratch {
     float *tail;                       // [batch][n_q][D]: what lies behind the prefix, the same way
 };
 
+// whether that kernel takes sequences of such a cache: asked before anything is launched
+bool attn_tail_fits(const nnc_paged_kv &cache, int batch);
 cudaError_t launch_attn_tail(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const PrefixGroups &groups, float *out,
                              float2 *ml, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes);
 

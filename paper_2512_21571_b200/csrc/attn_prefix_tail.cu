@@ -24,6 +24,12 @@ struct TailRows {
 
 }  // namespace
 
+bool attn_tail_fits(const nnc_paged_kv &c, int batch) {
+    const int tile = c.head_dim == 64 ? (c.type == NNC_E4M3 ? Shape<64, 1, NNC_E4M3, NNC_BF16>::kTile : Shape<64, 1, NNC_BF16, NNC_BF16>::kTile)
+                                      : (c.type == NNC_E4M3 ? Shape<128, 1, NNC_E4M3, NNC_BF16>::kTile : Shape<128, 1, NNC_BF16, NNC_BF16>::kTile);
+    return list_fits((long long)c.pages_per_seq * c.page_size, tile, batch, c.n_kv_heads);
+}
+
 cudaError_t launch_attn_tail(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const PrefixGroups &groups, float *out,
                              float2 *ml, int type, int n_q_heads, int64_t q_stride, float scale, void *scratch, size_t scratch_bytes) {
     PagedAttnParams p = paged_attn_params(lc, q, cache, lens, out, (float *)ml, groups.batch, n_q_heads, q_stride, (int64_t)n_q_heads * cache.head_dim, scale, scratch,

@@ -58,3 +58,16 @@ def test_groups_of_one(nnc, kv, group):
     out, lse = nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(shared), want_lse=True)
     _check_attention(out, lse, q, held, lens, 128 ** -0.5, 0, kv)
     assert nnc.op_status() == 0
+
+
+def test_a_refused_call_launches_nothing(nnc):
+    """A table of more positions than the rows behind prefixes are counted in: refused as the ordinary attention refuses it, before the first launch."""
+    batch, heads = 128, 64
+    cache = nnc.PagedKV.empty(1, 256, heads, 64, BF16, batch, 65600)
+    q = _randn(_gen(1), batch, heads, 64, dtype=BF16)
+    scratch = torch.zeros_like(nnc.attn_prefix_scratch(batch, heads, 64))
+    for call in (lambda: nnc.op_attn_prefix_paged(q, cache, _ints([0] * batch), _ints([0, batch]), _ints([0]), scratch=scratch),
+                 lambda: nnc.op_attn_decode_paged(q, cache, _ints([0] * batch), scratch=scratch)):
+        with pytest.raises(nnc.NncError) as e:
+            call()
+        assert e.value.status == -3 and not scratch.any()
