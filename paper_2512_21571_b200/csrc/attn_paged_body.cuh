@@ -362,7 +362,8 @@ __device__ __forceinline__ void attn_paged_cta(const PagedAttnParams &p) {
                     copy16(dst + PB * ROW, vs + i * 512);
                 }
             } else {
-                if (!there && (!W::kListed || pages[u] != kNoRows) && lane == 0) paged_complain(p.c);
+                // (a table may hold kNoRows, too: where the sequence has rows that is a page that the pool does not have)
+                if (!there && (!W::kListed || pages[u] != kNoRows || held[u] > 0) && lane == 0) paged_complain(p.c);
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
                     const int r = r0 + i * kRowsPerStep;
