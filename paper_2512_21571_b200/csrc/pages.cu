@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_pages_kernel(const Sele
     extern __shared__ uint32_t row_keys[];
     constexpr int kChunks = ITEMS ? ITEMS : 16;                  // runs of kSelectThreads pages that are counted at a time
     constexpr int kEach = (kChunks * kSelectWarps + 31) / 32;    // counts of a lane that adds them up
-    __shared__ uint32_t histogram[kSelectBins];
+    __shared__ __align__(16) uint32_t histogram[kSelectBins];    // read and cleared four at a time
     __shared__ uint2 sums[kEach * 32];                           // of a warp's pages of a run: above, equal; then of what came before
     __shared__ uint2 all_sums;
     __shared__ uint32_t most[kSelectWarps], least[kSelectWarps], found[3];
