@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kScoreWarps * 32) score_pages_kernel(const Sco
 
 // ---- selection ---------------------------------------------------------------------------------------------------------------
 //
-// A CTA a row.  Scores become whole numbers of the same order, in registers (up to 8192 pages) or in shared memory.  A histogram of 2048 equal
+// A CTA a row.  Scores become whole numbers of the same order, in registers (up to 8704 pages) or in shared memory.  A histogram of 2048 equal
 // parts of their range tells the part that the n-th largest lies in; that part is divided again, until all of it is wanted (scores of one
 // batch are spread well enough for one or two rounds) or its numbers are one.  Then the indices of what lies above, and of as many of the
 // equals as are missing, are written in order.  Bound by its chain of barriers: 5.4 us for 8 rows of 4097, 5.5 for 256 of 2049, the host's call among
@@ -535,10 +535,14 @@ cudaError_t launch_select_pages(const LaunchCtx &lc, const float *scores, const 
     early.pdl = true;
     const dim3 grid((unsigned)((long long)batch * n_kv)), block(kSelectThreads);
     p.kept = 1;
+    // Numbers of a thread in registers: 2, and one more than 4, 8 and 16, as tables of 2^k pages often have a column to spare.  us for 8 and 256 rows, at both ends
+    // of each form's widths: 512 and 1024 columns 5.5 and 5.6 | 1025 5.4 and 5.5, 2560 5.1 and 5.6 | 2561 5.1 and 9.4, 4608 5.5 and 9.9 | 4609 6.6 and 13.1,
+    // 8704 8.0 and 14.5.  (16 instead of 17: 3 % less up to 8192, 12.3 and 24.8 for 8193.)  In shared memory: 8705 12.7 and 25.8, 16384 19.4 and 36.4,
+    // 40960 42 and 81.  Made again from the scores each time: 40961 60 and 111, 131072 307 and 699.
     if (columns <= 2 * kSelectThreads) return launch(early, select_pages_kernel<2>, grid, block, p);
     if (columns <= 5 * kSelectThreads) return launch(early, select_pages_kernel<5>, grid, block, p);
     if (columns <= 9 * kSelectThreads) return launch(early, select_pages_kernel<9>, grid, block, p);
-    if (columns <= 16 * kSelectThreads) return launch(early, select_pages_kernel<16>, grid, block, p);
+    if (columns <= 17 * kSelectThreads) return launch(early, select_pages_kernel<17>, grid, block, p);
     p.kept = columns <= (160 << 10) / 4;
     const size_t smem = p.kept ? (size_t)columns * 4 : 0;
     static unsigned long long raised = 0;
