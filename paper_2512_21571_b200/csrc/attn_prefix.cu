@@ -218,7 +218,7 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     before += incl - mine;
     const long long share = max((total + gridDim.x - 1) / gridDim.x, 1ll), cta = blockIdx.x;
     const long long t0 = cta * share, t1 = min(t0 + share, total);
-    if (cta == gridDim.x - 1) {   // for the joining kernel; the last share is the shortest
+    if (cta == gridDim.x - 1) {   // this CTA, whose share is the shortest, writes what the joining kernel wants to know (below); and looks the groups over
         long long at = before;
         for (int g = g_lo; g < g_hi; ++g) {
             PrefixPlan plan = plan_of(p.c, p.groups, g, p.per_tile);
@@ -249,13 +249,11 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (g >= 0) {
                 const PrefixPlan plan = p.s.plan[g];
                 const int nth = b - plan.b0;
-                of.per_head = plan.tiles * (plan.steps + kPrefixFixed);
+                of.per_head = (long long)plan.tiles * (plan.steps + kPrefixFixed);
                 of.first = plan.base + (long long)(nth / p.per_tile) * (plan.steps + kPrefixFixed);
                 of.rows_per_head = plan.members * p.group;
                 of.row = (long long)plan.b0 * p.n_q + (long long)nth * p.group;
                 of.steps = takes_prefix(plan.prefix, p.lens[b]) ? plan.steps : 0;
-                of.prefix = plan.prefix;
-                of.b0 = plan.b0;
                 of.share = share;
             }
             p.s.of[b] = of;
@@ -277,7 +275,6 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             advance(p, at);
         }
     }
-    auto more = [&]() { return at.index < t1 && at.g < p.groups.n_groups; };
 
     long long all = 0;   // steps of this share
     for (Step s = at; s.index < t1 && s.g < p.groups.n_groups;) {   // a tile's at a time
@@ -709,14 +706,11 @@ attn_prefix_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 constexpr int kJoinThreads = 256;
 
 struct JoinParams {
-    PagedView c;
-    PrefixGroups groups;
     PrefixScratch s;
-    const int32_t *lens;
     char *out;
     float *lse;
     long long out_stride, part_rows;
-    int group, per_tile, n_q;
+    int n_kv, group, n_q;
 };
 
 template <int D, bool BF, bool CODES>   // BF: results are bf16, otherwise fp16; the cache's type, or codes
@@ -726,7 +720,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_prefix_join_kernel(const Jo
     __shared__ float2 mls[kJoinThreads];
     pdl_launch_dependents();
     pdl_wait();
-    const int tid = threadIdx.x, b = blockIdx.x / p.c.n_kv, head = blockIdx.x - b * p.c.n_kv;
+    const int tid = threadIdx.x, b = blockIdx.x / p.n_kv, head = blockIdx.x - b * p.n_kv;
     const PrefixOf of = p.s.of[b];
     long long first_row = 0;
     int n = 0;
@@ -887,8 +881,8 @@ size_t attn_prefix_scratch_bytes(int batch, int n_q_heads, int head_dim) {
 cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_paged_kv &cache, const int32_t *lens, const int32_t *starts,
                                const int32_t *shared, int n_groups, void *out, float *lse, int type, int batch, int n_q_heads, int64_t q_stride,
                                int64_t out_stride, float scale, void *scratch) {
-    // Every sequence's own rows, the shared ones among them: fp32; codes with fp16 queries, which codes times their scales do not fit; more query
-    // heads than a tile has rows, which share rows among themselves; queries whose rows overlap, which a tensor map does not describe; one sequence.  And small batches: reading all of a table's
+    // Every sequence's own rows, the shared ones among them: fp32; fp16 queries of codes, as the codes' operand is bf16 here and both operands of a product have one
+    // type; more query heads than a tile has rows, which share rows among themselves; queries whose rows overlap, which a tensor map does not describe; one sequence.  And small batches: reading all of a table's
     // rows for each sequence, mostly from L2, goes at some 10 TB/s per eight query heads behind 9 us, three launches take 17 to 25 us.  Both
     // sides, us (three launches first), 4 query heads of 128 and 12 of 64 per KV head: 35 MB 19 and 15, 135 MB 27.6 and 27.6, 140 MB 26.0 and
     // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.  Codes:
@@ -932,8 +926,8 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     e = launch_attn_tail(lc, q, cache, lens, groups, s.tail, s.tail_ml, type, n_q_heads, q_stride, scale, scratch, NNC_ATTN_PAGED_SCRATCH_BYTES);
     if (e != cudaSuccess) return e;
     JoinParams j = {};
-    j.c = p.c; j.groups = groups; j.s = s; j.lens = lens;
-    j.out = (char *)out; j.lse = lse; j.out_stride = out_stride; j.part_rows = p.part_rows; j.group = group; j.per_tile = p.per_tile; j.n_q = n_q_heads;
+    j.s = s; j.out = (char *)out; j.lse = lse; j.out_stride = out_stride; j.part_rows = p.part_rows;
+    j.n_kv = cache.n_kv_heads; j.group = group; j.n_q = n_q_heads;
     const long long ctas = (long long)batch * cache.n_kv_heads;
     return d == 64 ? launch_join_of<64>(early, j, cache.type, ctas) : launch_join_of<128>(early, j, cache.type, ctas);
 }

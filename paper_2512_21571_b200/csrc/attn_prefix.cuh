@@ -15,17 +15,17 @@ struct PrefixGroups {
     int least;                         // sequences that a group has at least where its rows are read for all of them at once
 };
 
-// where a group's tiles stand in the list
+// a group's tiles
 struct PrefixPlan {
-    long long base;                    // first place
+    long long base;                    // first place in the list, where it is known
     int b0, members, tiles, steps;     // first sequence, sequences, tiles per KV head, steps of a tile (0: no prefix)
-    int prefix, unused;                // positions
+    int prefix;                        // positions
 };
 // what the joining kernel wants to know of a sequence
 struct PrefixOf {
     long long first, row;              // first place of its tile of KV head 0, first row of its queries for KV head 0 (of CTA 0)
-    int per_head, rows_per_head;       // places and rows from one KV head to the next
-    int steps, prefix, b0, unused;     // steps 0: nothing from a prefix
+    long long per_head;                // places from one KV head to the next
+    int rows_per_head, steps;          // steps 0: nothing from a prefix
     long long share;                   // places of a CTA
 };
 
@@ -61,7 +61,6 @@ __device__ __forceinline__ PrefixPlan plan_of(const PagedView &c, const PrefixGr
     p.prefix = prefix_of(c, s, g);
     p.steps = p.members ? (p.prefix + kPrefixStep - 1) / kPrefixStep : 0;
     p.base = 0;
-    p.unused = 0;
     return p;
 }
 __device__ __forceinline__ long long places_of(const PagedView &c, const PrefixPlan &p) {
@@ -71,8 +70,8 @@ __device__ __forceinline__ long long places_of(const PagedView &c, const PrefixP
 // Partial results: a row for every query row of a (tile, CTA) pair that occurs.  Pairs in the list's order move on by a tile's rows or by
 // a CTA, so row (rows of earlier tiles) + 128 CTA is a pair's own.
 struct PrefixScratch {
-    PrefixPlan *plan;                  // [n_groups]
-    PrefixOf *of;                      // [batch]
+    PrefixPlan *plan;                  // [n_groups]: what the CTA that writes `of` makes it from
+    PrefixOf *of;                      // [batch]: for the joining kernel
     float2 *ml;                        // [rows]: reference in log2 units, sum
     float4 *o;                         // [D / 4][rows]: neighbouring threads hold neighbouring rows
     float2 *tail_ml;                   // [batch][n_q]
