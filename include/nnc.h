@@ -397,12 +397,15 @@ int nnc_op_attn_decode_paged(const void *q, const nnc_paged_kv *cache, const int
  * The cache holds all of them, whatever the sequences' lengths; a shorter sequence attends to its first lens[b].  Sequences of
  * no group, and of groups with shared[g] below a page, attend to their own rows alone.  A `starts` that descends or leaves 0 .. batch
  * and a shared[g] outside 0 .. the table's reach are cut to what is allowed and, where the groups are looked at, set the status word.
- * 1 <= n_groups <= batch.
+ * Overlapping groups leave the results of the sequences in them open.  1 <= n_groups <= batch.  n_pages * n_kv_heads * page_size is at most
+ * 2^31 - 256 (NNC_ERR_CAPACITY).
  *   q, out, lens, lse, scale, strides: as there, without a window.  A group of few sequences reads each one's own rows (below two, on NNC_E4M3
  *   caches below four; fewer with many query heads per KV head); groups of no sequences cost nothing, so that the arrays of a captured call may
  *   have room for more groups than there are.  Every sequence reads its own rows, and the groups are not looked at, for one sequence, for fp32
  *   queries, fp16 queries on NNC_E4M3 caches, more than 128 query heads per KV head, queries whose rows overlap, and where the table has room
  *   for little: all rows that it could name, whatever the lengths are, times the query heads per KV head in eights are less than 140 MB.
+ *   Numerics: fp32 scores, maxima and sums, as there; shared rows of bf16 and NNC_E4M3 caches are weighed by probabilities of 16 bits (two bf16 terms, each
+ *   off by at most 2^-16 of itself), of fp16 caches of 22, where nnc_op_attn_decode_paged has 24 and 22.
  * scratch: DEVICE, 256-byte aligned, nnc_attn_prefix_scratch_bytes(batch, n_q_heads, head_dim); its first NNC_ATTN_PAGED_TICKET_BYTES as
  * there.  Up to three launches. */
 size_t nnc_attn_prefix_scratch_bytes(int32_t batch, int32_t n_q_heads, int32_t head_dim);
@@ -416,7 +419,7 @@ int nnc_op_attn_prefix_paged(const void *q, const nnc_paged_kv *cache, const int
  * pages of the highest scores (nnc_op_select_pages), and the attention over them (nnc_op_attn_selected_paged). */
 
 /* bounds: 16-byte aligned, [n_pages][n_kv_heads][2][head_dim] of the cache's type (NNC_BF16 for an NNC_E4M3 cache, which holds its scaled codes
- * exactly): lowest, then highest.  Sets them for every page of sequences 0 .. batch - 1 (batch <= n_seqs) that holds a position in
+ * exactly down to 2^-133): lowest, then highest.  Sets them for every page of sequences 0 .. batch - 1 (batch <= n_seqs) that holds a position in
  * [first[b], lens[b]), from all positions of that page below lens[b]; other pages' bounds stay.  lens, first: int32 [batch]; first NULL: 0.
  * NaN where a key is NaN.  Sequences that share such a page give it the same bounds if both have all of it, which shared pages want
  * anyway.  A length beyond the table's reach counts as the longest the table holds, a page out of range is left out; both set the
