@@ -422,7 +422,9 @@ PyObject *attn_prefix(PyObject *const *a) {
     const int64_t groups = shared.dim() == 1 ? shared.size(0) : -1;
     if (groups < 0 || groups > x.in.tokens || (groups == 0 && x.in.tokens > 0)) refuse("shared: contiguous int32 numbers, one a group, at most one group a sequence");
     const int32_t *at_starts = index_of(starts, groups + 1, x.device, "starts"), *at_shared = index_of(shared, groups, x.device, "shared");
-    x.take_scratch(a[7], (int64_t)prefix_scratch_bytes((int32_t)x.in.tokens, (int32_t)x.in.heads, (int32_t)x.in.d), NNC_ATTN_PAGED_TICKET_BYTES,
+    // (0 bytes for sizes that the call refuses)
+    const int64_t bytes = (int64_t)prefix_scratch_bytes((int32_t)x.in.tokens, (int32_t)x.in.heads, (int32_t)x.in.d);
+    x.take_scratch(a[7], std::max<int64_t>(bytes, NNC_ATTN_PAGED_TICKET_BYTES), NNC_ATTN_PAGED_TICKET_BYTES,
                    "scratch: a contiguous tensor on the call's CUDA device (attn_prefix_scratch)");
     launch(x.device, "nnc_op_attn_prefix_paged", [&](void *stream) {
         return call_prefix(x.q.data_ptr(), &x.c, at_lens, at_starts, at_shared, (int32_t)groups, x.out.data_ptr(), x.lse_at(), x.in.type, (int32_t)x.in.tokens,

@@ -71,3 +71,12 @@ def test_a_refused_call_launches_nothing(nnc):
         with pytest.raises(nnc.NncError) as e:
             call()
         assert e.value.status == -3 and not scratch.any()
+
+
+def test_queries_without_heads_are_refused_as_the_ordinary_attention_refuses_them(nnc):
+    cache, lens, starts, shared, _ = _grouped(nnc, BF16, [(32, [40, 40])], 16, 2, 64, 1)
+    q = _randn(_gen(1), 2, 0, 64, dtype=BF16)
+    for call in (lambda: nnc.op_attn_prefix_paged(q, cache, _ints(lens), _ints(starts), _ints(shared)), lambda: nnc.op_attn_decode_paged(q, cache, _ints(lens))):
+        with pytest.raises(nnc.NncError) as e:
+            call()
+        assert e.value.status == -1
