@@ -22,7 +22,7 @@
 //     part of a tile ends.
 //   - E4M3: codes times their rows' scales are bf16 values exactly (down to 2^-133).  They come to shared memory as they are, eight warps make
 //     the rows of them that the products read, half of them a step each, and the two teams hold half of a step's scores at a time, which leaves
-//     room for the registers of 640 threads.  (Five groups of 12 behind up to 6000 codes: 66 us; all eight warps at every step, with one team or
+//     room for the registers of 640 threads.  (Five groups of 12 behind up to 6000 codes: 65 us; all eight warps at every step, with one team or
 //     two, 70; four and one team 73, four and two 75; every sequence's rows by themselves 112.)
 //   - Queries enter exactly.  Probabilities are two terms of the cache's type (bf16: 16 bits, fp16: 22), written over the scores they
 //     come from: one bf16 term alone would add an error of the size of the result's own rounding.  fp32 queries and results would need three
@@ -886,7 +886,8 @@ cudaError_t launch_attn_prefix(const LaunchCtx &lc, const void *q, const nnc_pag
     // rows for each sequence, mostly from L2, goes at some 10 TB/s per eight query heads behind 9 us, three launches take 17 to 25 us.  Both
     // sides, us (three launches first), 4 query heads of 128 and 12 of 64 per KV head: 35 MB 19 and 15, 135 MB 27.6 and 27.6, 140 MB 26.0 and
     // 24.5, 155 MB 27.7 and 25.8, 540 MB 32 and 64; 34 MB 31 and 17, 70 MB 23.3 and 25.0, 78 MB 29 and 27, 270 MB 37 and 58.  Codes:
-    // 135 MB 35 and 34, 270 MB 38 and 52; 12 of 64, 135 MB 40 and 54.
+    // 135 MB 35 and 34, 270 MB 38 and 52; 12 of 64, 135 MB 40 and 54.  (Lengths are the device's: three of 500 under a table for 65536 take three launches, 12.8
+    // us instead of 8.4.)
     const int eights = (n_q_heads / cache.n_kv_heads + 7) / 8;
     const double rows_bytes = (cache.type == NNC_E4M3 ? 2.0 : 4.0) * batch * cache.pages_per_seq * cache.page_size * cache.n_kv_heads * cache.head_dim;
     if (type == NNC_F32 || (cache.type == NNC_E4M3 && type != NNC_BF16) || n_q_heads / cache.n_kv_heads > kPrefixRows || (batch > 1 && q_stride < (int64_t)n_q_heads * cache.head_dim) ||
